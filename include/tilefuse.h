@@ -50,7 +50,8 @@ enum tf_status {
     TF_OK = 0,
     TF_ERR_NULL = -1,   /* a required pointer is NULL                          */
     TF_ERR_SHAPE = -2,  /* M < 1, K or N <= 0, K % group != 0, N % 8 != 0,
-                           or a dimension above TF_MAX_DIM                      */
+                           or a dimension above TF_MAX_DIM; heads, strides,
+                           pages or batch out of range                          */
     TF_ERR_GROUP = -3,  /* group is not a positive multiple of 32              */
     TF_ERR_ALIGN = -4,  /* a pointer is not 16-byte aligned                    */
     TF_ERR_ARG = -5,    /* other bad argument: bits not 4/8, GEMV with M > 8,
@@ -260,6 +261,140 @@ int tf_dequant(int bits, const void* packed, int64_t K, int64_t N, int group,
 int tf_silu_mul(const uint16_t* GU_f16, int64_t M, int64_t N, uint16_t* H_f16, void* stream);
 /* The same with bfloat16 GU and H (the layer composite in the paper's dtype). */
 int tf_silu_mul_bf16(const uint16_t* GU_bf16, int64_t M, int64_t N, uint16_t* H_bf16, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * The rest of a decoder layer around the quantized linear layers (not part of
+ * the paper's method): the norm between two blocks, a 4-bit paged key/value
+ * cache, attention of single tokens over it, and attention over whole prompts.
+ * With the matmuls above they make a decoder layer run end to end.
+ *
+ * `dtype` is TF_F16 or TF_BF16, the type of every 16-bit tensor of a call.
+ * Activations are [tokens, heads, head_dim] with head_dim contiguous, heads
+ * head_dim apart and tokens `stride` elements apart (a multiple of 8, at least
+ * heads * head_dim), so that the parts of one packed q, k, v projection are
+ * operands as they are.  head_dim is 64, 128 or 256; q_heads is a multiple of
+ * kv_heads, and query head h reads key/value head h / (q_heads / kv_heads).
+ * Sequences are packed one after the other: sequence b has the tokens
+ * cu[b] .. cu[b + 1] - 1 (int32 [batch + 1] on the device, not decreasing).
+ * Lengths, offsets and page tables stay on the device; the kernels check them
+ * against the sizes given here and never leave the buffers.
+ * ---------------------------------------------------------------------------
+ */
+
+/* Largest accepted numbers of sequences and heads. */
+#define TF_MAX_BATCH 65536
+#define TF_MAX_HEADS 1024
+
+/*
+ * The residual sum and the norms around it, in fp32 with one rounding per
+ * output:
+ *   y = X                     or  rms(X) * (post_weight + weight_offset)
+ *   r = residual + scale * gate * y           -> residual_out
+ *   Y = rms(r) * (weight + weight_offset),    rms(t) = t / sqrt(mean(t^2) + eps)
+ * over rows of N.  Y is computed from r before r's rounding.  residual,
+ * post_weight and gate may be NULL (absent); so may residual_out or (with
+ * weight) Y, not both.  weights are [N]; gate is [N] (gate_stride 0) or [M, N]
+ * with rows gate_stride apart.  residual_out may be residual itself and Y may
+ * be X; nothing else may overlap.  N % 8 == 0, gate_stride % 8 == 0, 16-byte
+ * aligned pointers.
+ */
+int tf_add_rms_norm(int dtype, const void* X, const void* residual, const void* post_weight, const void* gate,
+                    int64_t gate_stride, float scale, const void* weight, float weight_offset, float eps,
+                    int64_t M, int64_t N, void* residual_out, void* Y, void* stream);
+
+/*
+ * A 4-bit paged key/value cache.  Each key and each value of a head is a row
+ * of head_dim codes of 4 bits with a scale s and a zero-point z of its own
+ * (dtype, rounded to nearest even), standing for s * (q - z):
+ *   s = (max - min) / 15,  z = -min / s,  q = round(x / s + z) within 0..15
+ * in fp32 from the row's fp32 values, with s and z as rounded.  A row whose
+ * values are one within the type's precision (s under 2^-100, or |min| over
+ * 32768 s) is stored as its minimum, one with a value that is not finite reads
+ * back as NaN.  `data` holds tf_kv4_cache_bytes(...) bytes, 256-byte aligned,
+ * in `pages` pages of page_size positions (a multiple of 32); its layout is
+ * opaque.  It needs no initial value: only appended positions are read.
+ * Positions of sequence b live on the pages table[b * table_stride + p],
+ * p = position / page_size < max_pages (int32; an entry outside 0..pages-1 is
+ * no page: nothing is stored there, and attention leaves its positions out).
+ */
+typedef struct tf_kv4_cache {
+    void* data;
+    int64_t pages;
+    int32_t page_size;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t dtype;
+    const int32_t* table;
+    int64_t table_stride;
+    int64_t max_pages;
+} tf_kv4_cache;
+
+/* Bytes of a cache of that many pages, or a negative tf_status. */
+int64_t tf_kv4_cache_bytes(int64_t pages, int page_size, int kv_heads, int head_dim);
+
+/*
+ * Rotates the queries and keys of `tokens` packed tokens and appends keys and
+ * values to the cache.  Token i of sequence b has the position starts[b] + i.
+ * With cos and sin (fp32 [positions, head_dim / 2]) the pair (x[d],
+ * x[d + head_dim / 2]) turns by the position's angle:
+ *   (x1 cos - x2 sin, x2 cos + x1 sin) in fp32
+ * and the cached key is quantized from that; NULL for both leaves q and k as
+ * they are.  Q may be NULL (with Q_out, q_heads = 0); K_out may be NULL.  Q_out
+ * [tokens, q_heads, head_dim] and K_out [tokens, kv_heads, head_dim]
+ * (contiguous) receive the rotated rows rounded to dtype.  A token that no
+ * sequence owns, or whose position is outside the tables of angles, has NaN in
+ * Q_out and K_out and is not cached.  No two tokens of a call may share a position.
+ */
+int tf_kv4_append(const tf_kv4_cache* cache, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                  const void* V, int64_t v_stride, const float* cos, const float* sin, int64_t positions,
+                  const int32_t* cu, const int32_t* starts, int64_t batch, int64_t tokens, int q_heads,
+                  void* Q_out, void* K_out, void* stream);
+
+/*
+ * Reads the cached rows of positions starts[b] + i, i < cu[b + 1] - cu[b], back
+ * as values s * (q - z) rounded to dtype: K_out and V_out are [tokens, kv_heads,
+ * head_dim], packed as cu says.  A position without a page reads as NaN.
+ */
+int tf_kv4_read(const tf_kv4_cache* cache, const int32_t* cu, const int32_t* starts, int64_t batch, int64_t tokens,
+                void* K_out, void* V_out, void* stream);
+
+/*
+ * Attention of the last q_len tokens of each sequence over its cache (decode;
+ * q_len above 1 for speculated tokens, at most TF_KV4_MAX_Q):
+ *   O[b, i, h] = sum_j softmax_j(scale * Q[b, i, h] . K[j]) V[j]
+ * over the positions j <= lens[b] - q_len + i, j >= 0.  A query that sees none
+ * gives zeros.  Q is [batch * q_len, q_heads, head_dim] with rows q_stride
+ * apart, O contiguous.  lens[b] (int32) counts the appended tokens, the asking
+ * ones among them; more than max_pages * page_size counts as that.  Codes are
+ * multiplied as they are; scales and zero-points act in fp32, except that
+ * softmax weights times the value's scale are rounded to dtype for the matrix
+ * cores.  workspace: tf_kv4_attention_workspace_bytes(...) bytes, 16-byte
+ * aligned and ZERO-FILLED before its first use; each call returns its counters
+ * to zero, so that one buffer serves any later call of these sizes or smaller
+ * need.  Calls that may run concurrently must not share one, and no matmul
+ * call may use it.  The result is the same from run to run.
+ */
+#define TF_KV4_MAX_Q 8
+int64_t tf_kv4_attention_workspace_bytes(int64_t batch, int q_len, int q_heads, int kv_heads, int head_dim);
+int tf_kv4_attention(const tf_kv4_cache* cache, const void* Q, int64_t q_stride, const int32_t* lens, int64_t batch,
+                     int q_len, int q_heads, float scale, void* O, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/*
+ * Attention over whole packed prompts:
+ *   O[i, h] = sum_j softmax_j(scale * Q[i, h] . K[j]) V[j]
+ * for query i of sequence b over its keys j; with causal, only j <= i + n_k - n_q
+ * (the queries are the last n_q of n_k tokens).  A query that sees no key gives
+ * zeros.  cu_q and cu_k: int32 [batch + 1].  Q, K, V strided as above, O
+ * [tokens_q, q_heads, head_dim] contiguous.  Scores and sums in fp32, softmax
+ * weights rounded to dtype for the matrix cores.  Rows of O that no sequence
+ * owns are not written.
+ */
+int tf_prompt_attention(int dtype, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
+                        int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t tokens_q,
+                        int64_t tokens_k, int q_heads, int kv_heads, int head_dim, float scale, int causal, void* O,
+                        void* stream);
 
 #ifdef __cplusplus
 }

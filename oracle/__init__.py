@@ -24,3 +24,12 @@ from .bf16_oracle import (  # noqa: F401
     w4a16_bf16,
     w8a16_bf16,
 )
+from .decoder_oracle import (  # noqa: F401
+    attend,
+    attend_bound,
+    cached_rows,
+    quant_rows,
+    rms_norm_block,
+    rotate,
+    round16,
+)

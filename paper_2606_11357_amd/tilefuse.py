@@ -34,7 +34,16 @@ EXPORTS = (
     "tf_pack_w8_sym", "tf_workspace_bytes", "tf_gemm_workspace_bytes", "tf_w4a16_gemm",
     "tf_w8a16_gemm", "tf_w4a16_gemv", "tf_w8a16_gemv", "tf_w4a16_gemv_noalloc", "tf_w4a16_gemm_bf16", "tf_w8a16_gemm_bf16", "tf_w4a16_gemv_bf16",
     "tf_w8a16_gemv_bf16", "tf_unpack", "tf_dequant", "tf_silu_mul", "tf_silu_mul_bf16",
+    "tf_add_rms_norm", "tf_kv4_cache_bytes", "tf_kv4_append", "tf_kv4_read",
+    "tf_kv4_attention_workspace_bytes", "tf_kv4_attention", "tf_prompt_attention",
 )
+
+
+class _Kv4Struct(ctypes.Structure):
+    """tf_kv4_cache"""
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int64)]
 
 
 class TileFuseError(RuntimeError):
@@ -55,7 +64,8 @@ def load() -> ctypes.CDLL:
         raise ImportError(f"{LIB_PATH} is missing; build it with "
                           "`python -m paper_2606_11357_amd.build`")
     lib = ctypes.CDLL(LIB_PATH)
-    P, I64, I, SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+    P, I64, I, SZ, F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
+    C = ctypes.POINTER(_Kv4Struct)
     sig = {
         "tf_layout_version": (I, []),
         "tf_status_str": (ctypes.c_char_p, [I]),
@@ -78,6 +88,13 @@ def load() -> ctypes.CDLL:
         "tf_dequant": (I, [I, P, I64, I64, I, I, P, P]),
         "tf_silu_mul": (I, [P, I64, I64, P, P]),
         "tf_silu_mul_bf16": (I, [P, I64, I64, P, P]),
+        "tf_add_rms_norm": (I, [I, P, P, P, P, I64, F, P, F, F, I64, I64, P, P, P]),
+        "tf_kv4_cache_bytes": (I64, [I64, I, I, I]),
+        "tf_kv4_append": (I, [C, P, I64, P, I64, P, I64, P, P, I64, P, P, I64, I64, I, P, P, P]),
+        "tf_kv4_read": (I, [C, P, P, I64, I64, P, P, P]),
+        "tf_kv4_attention_workspace_bytes": (I64, [I64, I, I, I, I]),
+        "tf_kv4_attention": (I, [C, P, I64, P, I64, I, I, F, P, P, SZ, P]),
+        "tf_prompt_attention": (I, [I, P, I64, P, I64, P, I64, P, P, I64, I64, I64, I, I, I, F, I, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -330,4 +347,286 @@ def silu_mul(gu, out=None):
         raise ValueError("out must have gu's dtype")
     name = "tf_silu_mul_bf16" if gu.dtype == torch.bfloat16 else "tf_silu_mul"
     _check(getattr(load(), name)(_ptr(gu), M, N, _ptr(out), _stream(gu.device)), name)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# the rest of a decoder layer: norm, 4-bit paged cache, attention
+# ---------------------------------------------------------------------------
+def _dtype_code(dtype, what):
+    torch = _torch()
+    if dtype == torch.float16:
+        return TF_F16
+    if dtype == torch.bfloat16:
+        return TF_BF16
+    raise ValueError(f"{what} must be fp16 or bf16")
+
+
+def _same(t, dtype, device, shape, what):
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {dtype} {list(shape)} on {device}")
+
+
+def _heads_of(t, what):
+    """Checks a [tokens, heads, head_dim] operand whose tokens may be strided;
+    its token stride."""
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU (the library has no CPU path)")
+    if t.dim() != 3:
+        raise ValueError(f"{what} must be [tokens, heads, head_dim]")
+    T, H, D = t.shape
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+        raise ValueError(f"the heads of {what} must be contiguous")
+    return t.stride(0) if T > 1 else H * D
+
+
+def _int32(t, shape, device, what):
+    torch = _torch()
+    _need_cuda(t)
+    _same(t, torch.int32, device, shape, what)
+
+
+def add_rms_norm(x, residual=None, weight=None, *, post_weight=None, gate=None, scale=1.0, offset=0.0, eps=1e-6,
+                 out=None, residual_out=None):
+    """The residual sum and the norms around it, for fp16 or bf16 [M, N]:
+
+        y = x, or rms(x) * (post_weight + offset)
+        r = residual + scale * gate * y
+        out = rms(r) * (weight + offset)
+
+    in fp32, each output rounded once.  gate is [N] or [M, N].  Returns (out, r);
+    without a weight out is None, and with nothing that changes x (no residual,
+    post_weight, gate or scale) r is x.  residual_out may be residual itself and
+    out may be x: both are then updated in place."""
+    torch = _torch()
+    _need_cuda(x, residual, weight, post_weight, out, residual_out)
+    if x.dim() != 2:
+        raise ValueError("x must be fp16 or bf16 [M, N]")
+    code = _dtype_code(x.dtype, "x")
+    M, N = x.shape
+    for t, shape, what in ((residual, (M, N), "residual"), (weight, (N,), "weight"),
+                           (post_weight, (N,), "post_weight"), (out, (M, N), "out"),
+                           (residual_out, (M, N), "residual_out")):
+        if t is not None:
+            _same(t, x.dtype, x.device, shape, what)
+    gate_stride = 0
+    if gate is not None:
+        if gate.dtype != x.dtype or gate.device != x.device or tuple(gate.shape) not in ((N,), (M, N)):
+            raise ValueError(f"gate must be {x.dtype} [{N}] or [{M}, {N}] on {x.device}")
+        if N > 1 and gate.stride(-1) != 1:
+            raise ValueError("the rows of gate must be contiguous")
+        gate_stride = gate.stride(0) if gate.dim() == 2 and M > 1 else 0
+    if weight is None and out is not None:
+        raise ValueError("out needs a weight")
+    keep = residual is None and post_weight is None and gate is None and scale == 1.0 and residual_out is None
+    if keep and weight is None:
+        return None, x
+    if out is None and weight is not None:
+        out = torch.empty_like(x)
+    if residual_out is None and not keep:
+        residual_out = torch.empty_like(x)
+    if M > 0:
+        _check(load().tf_add_rms_norm(code, _ptr(x), _ptr(residual), _ptr(post_weight), _ptr(gate), gate_stride, scale,
+                                      _ptr(weight), offset, eps, M, N, _ptr(residual_out), _ptr(out),
+                                      _stream(x.device)), "tf_add_rms_norm")
+    return out, x if keep else residual_out
+
+
+def kv4_cache_bytes(pages: int, page_size: int, kv_heads: int, head_dim: int) -> int:
+    n = load().tf_kv4_cache_bytes(pages, page_size, kv_heads, head_dim)
+    if n < 0:
+        raise TileFuseError(int(n), "tf_kv4_cache_bytes")
+    return int(n)
+
+
+class KV4Cache:
+    """A pool of pages of 4-bit keys and values (made by kv4_cache): `data` in the
+    library's layout, and the sizes it was made for."""
+    __slots__ = ("data", "pages", "page_size", "kv_heads", "head_dim", "dtype", "_code")
+
+    def __init__(self, data, pages, page_size, kv_heads, head_dim, dtype):
+        self._code = _dtype_code(dtype, "dtype")
+        self.data, self.pages, self.page_size = data, pages, page_size
+        self.kv_heads, self.head_dim, self.dtype = kv_heads, head_dim, dtype
+
+    def _with(self, table, batch):
+        torch = _torch()
+        if not table.is_cuda or table.device != self.data.device:
+            raise ValueError("the page table must be on the cache's GPU")
+        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != batch:
+            raise ValueError(f"the page table must be int32 [{batch}, pages]")
+        if table.shape[1] > 1 and table.stride(1) != 1:
+            raise ValueError("the rows of the page table must be contiguous")
+        n = table.shape[1]
+        return _Kv4Struct(self.data.data_ptr(), self.pages, self.page_size, self.kv_heads, self.head_dim, self._code,
+                          table.data_ptr(), table.stride(0) if batch > 1 else n, n)
+
+
+def kv4_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=None, device="cuda"):
+    """A 4-bit cache of `pages` pages of page_size positions (a multiple of 32)
+    for keys and values of `dtype` (fp16 or bf16); uninitialised."""
+    torch = _torch()
+    dtype = dtype or torch.float16
+    _dtype_code(dtype, "dtype")
+    data = torch.empty(kv4_cache_bytes(pages, page_size, kv_heads, head_dim), dtype=torch.uint8, device=device)
+    return KV4Cache(data, pages, page_size, kv_heads, head_dim, dtype)
+
+
+def kv4_append(cache, table, cu, starts, k, v, cos=None, sin=None, q=None, keys=False, q_out=None, k_out=None):
+    """Rotates q and k by their positions and appends k and v to the cache.
+
+    k, v: [tokens, kv_heads, head_dim], q: [tokens, q_heads, head_dim] (parts of
+    one packed projection are fine), cu: int32 [batch + 1] offsets of the
+    sequences' tokens, starts: int32 [batch] position of each sequence's first
+    token, table: int32 [batch, pages].  cos, sin: fp32 [positions, head_dim / 2],
+    or None for no rotation.  Returns (q, k) rotated, as new tensors or in q_out
+    and k_out; q is None where it is not given, k unless keys is true or k_out
+    is given."""
+    torch = _torch()
+    dev = cache.data.device
+    k_stride, v_stride = _heads_of(k, "k"), _heads_of(v, "v")
+    T, B = k.shape[0], starts.shape[0]
+    shape = (T, cache.kv_heads, cache.head_dim)
+    _same(k, cache.dtype, dev, shape, "k")
+    _same(v, cache.dtype, dev, shape, "v")
+    _int32(cu, (B + 1,), dev, "cu")
+    _int32(starts, (B,), dev, "starts")
+    st = cache._with(table, B)
+    q_stride = q_heads = positions = 0
+    if q is not None:
+        q_stride, q_heads = _heads_of(q, "q"), q.shape[1]
+        _same(q, cache.dtype, dev, (T, q_heads, cache.head_dim), "q")
+        if q_out is None:
+            q_out = torch.empty((T, q_heads, cache.head_dim), dtype=q.dtype, device=dev)
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    if keys and k_out is None:
+        k_out = torch.empty(shape, dtype=k.dtype, device=dev)
+    for t, n, what in ((q_out, q_heads, "q_out"), (k_out, cache.kv_heads, "k_out")):
+        if t is not None:
+            _need_cuda(t)
+            _same(t, cache.dtype, dev, (T, n, cache.head_dim), what)
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin come together")
+    if cos is not None:
+        _need_cuda(cos, sin)
+        positions = cos.shape[0]
+        for t, what in ((cos, "cos"), (sin, "sin")):
+            _same(t, torch.float32, dev, (positions, cache.head_dim // 2), what)
+    if T > 0:
+        _check(load().tf_kv4_append(st, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(cos), _ptr(sin),
+                                    positions, _ptr(cu), _ptr(starts), B, T, q_heads, _ptr(q_out), _ptr(k_out),
+                                    _stream(dev)), "tf_kv4_append")
+    return q_out, k_out
+
+
+def kv4_read(cache, table, cu, starts, tokens: int, k_out=None, v_out=None):
+    """The cached keys and values of positions starts[b] .. as [tokens, kv_heads,
+    head_dim] each, packed as cu (int32 [batch + 1], cu[-1] == tokens) says."""
+    torch = _torch()
+    dev = cache.data.device
+    B = starts.shape[0]
+    _int32(cu, (B + 1,), dev, "cu")
+    _int32(starts, (B,), dev, "starts")
+    st = cache._with(table, B)
+    shape = (tokens, cache.kv_heads, cache.head_dim)
+    k_out = torch.empty(shape, dtype=cache.dtype, device=dev) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=cache.dtype, device=dev) if v_out is None else v_out
+    for t, what in ((k_out, "k_out"), (v_out, "v_out")):
+        _need_cuda(t)
+        _same(t, cache.dtype, dev, shape, what)
+    if tokens > 0:
+        _check(load().tf_kv4_read(st, _ptr(cu), _ptr(starts), B, tokens, _ptr(k_out), _ptr(v_out), _stream(dev)),
+               "tf_kv4_read")
+    return k_out, v_out
+
+
+def kv4_attention_workspace_bytes(batch: int, q_len: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    n = load().tf_kv4_attention_workspace_bytes(batch, q_len, q_heads, kv_heads, head_dim)
+    if n < 0:
+        raise TileFuseError(int(n), "tf_kv4_attention_workspace_bytes")
+    return int(n)
+
+
+_attention_ws = {}
+
+
+def _attention_workspace(device, nbytes):
+    """A zero-filled workspace for kv4_attention, cached per device; like the
+    matmuls' (default_workspace) it must not be shared by calls that run
+    concurrently on different streams."""
+    torch = _torch()
+    buf = _attention_ws.get(device.index)
+    if buf is None or buf.numel() < nbytes:
+        buf = _attention_ws[device.index] = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+    return buf
+
+
+def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
+    """Attention of each sequence's last tokens over its cached keys and values.
+
+    q: [batch, q_heads, head_dim] or [batch, q_len, q_heads, head_dim] (q_len up
+    to 8), lens: int32 [batch], the cached tokens with the asking ones; token i
+    sees the positions up to lens - q_len + i.  scale: 1 / sqrt(head_dim) unless
+    given.  workspace: None for the cached per-device one, or zero-filled bytes
+    (kv4_attention_workspace_bytes) of the caller's for calls on several
+    streams.  Returns a tensor of q's shape."""
+    torch = _torch()
+    dev = cache.data.device
+    if q.dim() not in (3, 4):
+        raise ValueError("q must be [batch, q_heads, head_dim] or [batch, q_len, q_heads, head_dim]")
+    B, q_len = q.shape[0], 1 if q.dim() == 3 else q.shape[1]
+    q_heads, D = q.shape[-2:]
+    _same(q, cache.dtype, dev, (*q.shape[:-1], cache.head_dim), "q")
+    if q.dim() == 4 and B > 1 and q.stride(0) != q_len * q.stride(1):
+        raise ValueError("the tokens of q must be equally spaced")
+    rows = q if q.dim() == 3 else q.as_strided((B * q_len, q_heads, D), q.stride()[1:])
+    stride = _heads_of(rows, "q")
+    _int32(lens, (B,), dev, "lens")
+    st = cache._with(table, B)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    else:
+        _need_cuda(out)
+        _same(out, q.dtype, dev, q.shape, "out")
+    if B == 0:
+        return out
+    if workspace is None:
+        workspace = _attention_workspace(dev, kv4_attention_workspace_bytes(B, q_len, q_heads, cache.kv_heads, D))
+    else:
+        _need_cuda(workspace)
+    _check(load().tf_kv4_attention(st, _ptr(q), stride, _ptr(lens), B, q_len, q_heads, D ** -0.5 if scale is None else scale, _ptr(out),
+                                   _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev)),
+           "tf_kv4_attention")
+    return out
+
+
+def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None):
+    """Attention over packed prompts: q [tokens, q_heads, head_dim], k and v
+    [keys, kv_heads, head_dim] (parts of one packed projection are fine), cu_q and
+    cu_k int32 [batch + 1] (cu_k is cu_q unless given).  causal: the queries are
+    the last of their sequence's keys.  Returns [tokens, q_heads, head_dim]."""
+    torch = _torch()
+    strides = [_heads_of(t, what) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
+    code = _dtype_code(q.dtype, "q")
+    T, q_heads, D = q.shape
+    Tk, kv_heads, _ = k.shape
+    _same(k, q.dtype, q.device, (Tk, kv_heads, D), "k")
+    _same(v, q.dtype, q.device, (Tk, kv_heads, D), "v")
+    B = cu_q.shape[0] - 1
+    cu_k = cu_q if cu_k is None else cu_k
+    _int32(cu_q, (B + 1,), q.device, "cu_q")
+    _int32(cu_k, (B + 1,), q.device, "cu_k")
+    if out is None:
+        out = torch.empty((T, q_heads, D), dtype=q.dtype, device=q.device)
+    else:
+        _need_cuda(out)
+        _same(out, q.dtype, q.device, (T, q_heads, D), "out")
+    if T > 0 and Tk == 0:
+        return out.zero_()
+    if T > 0:
+        _check(load().tf_prompt_attention(code, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v), strides[2],
+                                          _ptr(cu_q), _ptr(cu_k), B, T, Tk, q_heads, kv_heads, D,
+                                          D ** -0.5 if scale is None else scale, int(causal), _ptr(out), _stream(q.device)),
+               "tf_prompt_attention")
     return out
