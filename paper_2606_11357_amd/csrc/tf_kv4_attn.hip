@@ -18,7 +18,7 @@ Kv4 kv4_view(const tf_kv4_cache& c);
 namespace {
 
 constexpr int kRoundKeys = 128;          // keys of one round: a tile of 32 for each of 4 waves
-constexpr int kWgPerCu = 4;
+constexpr int kMostWgs = 2048;           // workgroups of a launch, at most
 
 struct AttnArgs {
     Kv4 cache;
@@ -26,10 +26,11 @@ struct AttnArgs {
     int64_t q_stride;
     const int32_t* lens;
     int batch, q_len, group, row_blocks;  // group: query heads per key/value head
+    uint32_t wgs;                         // workgroups that share the rounds
     int64_t capacity;                     // positions a table row can hold
     float scale2;                         // softmax scale * log2(e)
     uint16_t* out;
-    uint32_t* counters;
+    uint32_t* counters;                   // null: kv4_join_kernel adds the parts
     float* parts;
 };
 
@@ -55,9 +56,9 @@ __device__ __forceinline__ u32x4 code_pairs(uint32_t w, const Magic& m) {
     u32x4 o;
     if constexpr (BF) {
         o[0] = (w & 0x000F000Fu) | m.a;
-        o[1] = (w >> 4 & 0x000F000Fu) | m.b;
+        o[1] = (w >> 4 & 0x000F000Fu) | m.a;
         o[2] = (w >> 8 & 0x000F000Fu) | m.a;
-        o[3] = (w >> 12 & 0x000F000Fu) | m.b;
+        o[3] = (w >> 12 & 0x000F000Fu) | m.a;
     } else {
         const uint32_t w8 = w >> 8;
         o[0] = (w & 0x000F000Fu) | m.a;
@@ -72,26 +73,29 @@ __device__ __forceinline__ float over_groups(float v) {       // sum over the fo
     v += __shfl_xor(v, 16);
     return v + __shfl_xor(v, 32);
 }
+// max over the four 16-lane groups: swaps of 16- and 32-lane rows, no LDS
+__device__ __forceinline__ float max_over_groups(float v) {
+    const uint32_t a = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    v = fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return fmaxf(__builtin_bit_cast(float, s[0]), __builtin_bit_cast(float, s[1]));
+}
 
+// 16-byte pieces of a lane's K (or V) codes, and word w of key half u in them
+// as kv4_word places it.
+template <int D> constexpr int kPieces = D == 64 ? 1 : D / 64;
 template <int D>
-struct TileRegs {
-    static constexpr int P = D == 64 ? 1 : D / 64;    // 16-byte pieces of a lane
-    u32x4 k[P], v[P], meta[4];                        // meta: k scale, k zero, v scale, v zero
-    __device__ __forceinline__ void load(const uint8_t* tile, int lane) {
+__device__ __forceinline__ uint32_t code_word(const u32x4* x, int u, int w) {
+    if constexpr (D == 64) return x[0][2 * u + w];
+    else return x[u * (D / 128) + w / 4][w % 4];
+}
+template <int D>
+__device__ __forceinline__ void load_codes(u32x4* x, const uint8_t* codes, int lane) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) k[p] = *reinterpret_cast<const u32x4*>(tile + p * 1024 + lane * 16);
-#pragma unroll
-        for (int p = 0; p < P; ++p) v[p] = *reinterpret_cast<const u32x4*>(tile + 16 * D + p * 1024 + lane * 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            meta[i] = *reinterpret_cast<const u32x4*>(tile + 32 * D + (lane >> 4) * 64 + i * 16);
-    }
-    // word w of key half u, as kv4_word places it
-    static __device__ __forceinline__ uint32_t word(const u32x4* x, int u, int w) {
-        if constexpr (D == 64) return x[0][2 * u + w];
-        else return x[u * (D / 128) + w / 4][w % 4];
-    }
-};
+    for (int p = 0; p < kPieces<D>; ++p) x[p] = *reinterpret_cast<const u32x4*>(codes + p * 1024 + lane * 16);
+}
 
 // Value i (0..7) of eight packed 16-bit floats.
 template <bool BF>
@@ -101,100 +105,208 @@ __device__ __forceinline__ float meta_f32(const u32x4& m, int i) {
     else return scale_f32<false>(i & 1 ? w >> 16 : w & 0xFFFFu);
 }
 
-// One workgroup of four waves takes a contiguous share of all rounds of all
-// items, an item being one (sequence, key/value head, block of 16 NR query
-// rows) and a round 128 keys of it, a tile for each wave.  Shares differ by at
-// most one round whatever the lengths are.  Items that lie inside one share are
-// written directly; the others' partial sums go through the workspace, and the
-// workgroup that arrives last adds them in order.
-template <bool BF, int D, int NR>
-__global__ __launch_bounds__(256) void kv4_attn_kernel(AttnArgs a) {
-    constexpr int NT = D / 16;            // 16-dim tiles of the output
-    constexpr int NW = D / 32;            // words of codes per lane and key half
-    constexpr int ROWS = 16 * NR;
-    constexpr int PITCH = D + 4;
-    constexpr int64_t TB = kv4_tile_bytes(D);
-    constexpr int64_t SLOT = (int64_t)ROWS * (D + 2);
-    __shared__ uint32_t wave_total[4];
-    __shared__ uint32_t before[257];      // rounds of one head before each thread's sequences
-    __shared__ float ms[4][ROWS], ls[2][ROWS];
-    __shared__ float acc[2][ROWS * PITCH];
-    __shared__ int last;
+// How the rounds of all items are shared out.  An item is one (sequence,
+// key/value head, block of query rows); its rounds are 128 keys each, at least
+// one (which writes the zeros of an empty row).  Workgroup w of `wgs` takes a
+// contiguous share of all rounds, in the order of sequence, head and block, and
+// shares differ by at most one round whatever the lengths are.
+struct Shares {
+    const AttnArgs& a;
+    const uint32_t* before;               // LDS: rounds of one head before each thread's sequences
+    int seg;                              // sequences of a thread in `before`
+    uint32_t heads, share, extra;
 
-    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-    // ---- this workgroup's share
-    const int seg = (a.batch + 255) / 256;
-    auto length_of = [&](int b) {
+    __device__ __forceinline__ static uint32_t length_of(const AttnArgs& a, int b) {
         const int64_t n = a.lens[b];
         return (uint32_t)(n < 0 ? 0 : n > a.capacity ? a.capacity : n);
-    };
-    auto rounds_of = [&](uint32_t n) { return n == 0 ? 1u : (n + kRoundKeys - 1) / kRoundKeys; };
-    {
-        uint32_t mine = 0;
-        for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) mine += rounds_of(length_of(b));
-        uint32_t sum = mine;
+    }
+    __device__ __forceinline__ static uint32_t rounds_of(uint32_t n) {
+        return n == 0 ? 1u : (n + kRoundKeys - 1) / kRoundKeys;
+    }
+    // All 256 threads; before: 257 words of LDS, scratch: 4.
+    __device__ __forceinline__ Shares(const AttnArgs& args, uint32_t* lds, uint32_t* scratch) : a(args), before(lds) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        seg = (a.batch + 255) / 256;
+        uint32_t sum = 0;
+        for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) sum += rounds_of(length_of(a, b));
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t o = __shfl_up(sum, d);
             if (lane >= d) sum += o;
         }
-        if (lane == 63) wave_total[wave] = sum;
+        if (lane == 63) scratch[wave] = sum;
         __syncthreads();
-        uint32_t base = 0;
-        for (int w = 0; w < wave; ++w) base += wave_total[w];
-        before[tid + 1] = base + sum;
-        if (tid == 0) before[0] = 0;
+        for (int w = 0; w < wave; ++w) sum += scratch[w];
+        lds[tid + 1] = sum;
+        if (tid == 0) lds[0] = 0;
         __syncthreads();
+        heads = (uint32_t)a.cache.kv_heads * a.row_blocks;
+        const uint32_t total = lds[256] * heads;
+        share = total / a.wgs;
+        extra = total % a.wgs;
     }
-    const uint32_t heads = (uint32_t)a.cache.kv_heads * a.row_blocks;
-    const uint32_t total = before[256] * heads;
-    const uint32_t share = total / gridDim.x, extra = total % gridDim.x;
-    const uint32_t wg = blockIdx.x;
-    uint32_t at = wg * share + (wg < extra ? wg : extra);
-    const uint32_t end = at + share + (wg < extra ? 1 : 0);
-    if (at >= end) return;
-    auto owner_wg = [&](uint32_t x) {
+    __device__ __forceinline__ uint32_t begin_of(uint32_t w) const { return w * share + (w < extra ? w : extra); }
+    // the workgroup that takes round x
+    __device__ __forceinline__ uint32_t owner(uint32_t x) const {
         const uint32_t big = extra * (share + 1);
         return x < big ? x / (share + 1) : extra + (x - big) / share;
-    };
-    int b;
-    uint32_t seq_start;                   // rounds (of all heads) before sequence b
-    {
-        const uint32_t x = at / heads;
+    }
+    // the sequence of round x, and the rounds before its first
+    __device__ __forceinline__ int sequence(uint32_t x, uint32_t& seq_start) const {
+        x /= heads;
         int s0 = 0, s1 = 256;
         while (s1 - s0 > 1) {
             const int mid = (s0 + s1) >> 1;
             if (before[mid] <= x) s0 = mid;
             else s1 = mid;
         }
-        b = s0 * seg;
+        int b = s0 * seg;
         uint32_t done = before[s0];
         for (;; ++b) {
-            const uint32_t n = rounds_of(length_of(b));
+            const uint32_t n = rounds_of(length_of(a, b));
             if (x < done + n) break;
             done += n;
         }
-        seq_start = done * heads;
-        b = __builtin_amdgcn_readfirstlane(b);
-        seq_start = __builtin_amdgcn_readfirstlane(seq_start);
+        seq_start = __builtin_amdgcn_readfirstlane(done * heads);
+        return __builtin_amdgcn_readfirstlane(b);
     }
+};
+
+// One part of an item that several workgroups share: `rows` rows of D sums,
+// their maxima and their sums of weights.  A workgroup has at most two: of the
+// item that it ends (slot 0) and of the one that it begins (slot 1).
+template <int D, int ROWS>
+struct Parts {
+    static constexpr int64_t kSlot = (int64_t)ROWS * (D + 2);
+    static __device__ __forceinline__ float* at(float* parts, uint32_t w, uint32_t first) {
+        return parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * kSlot;
+    }
+};
+
+// Adds the parts of workgroups first..final at two neighbouring sums of row r,
+// in their order, and returns the two outputs.  load2: two floats at an even
+// address.
+template <int D, int ROWS, typename Load2, typename Load1>
+__device__ __forceinline__ float2_t join_parts(float* parts, uint32_t first, uint32_t final, int r, int d, Load2 load2,
+                                               Load1 load1) {
+    using P = Parts<D, ROWS>;
+    constexpr int AHEAD = 8;              // parts in flight
+    float top = -__builtin_inff(), sum = 0.f;
+    float2_t v = {0.f, 0.f};
+    for (uint32_t w0 = first; w0 <= final; w0 += AHEAD) {
+        float mw[AHEAD], lw[AHEAD];
+        float2_t vw[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const uint32_t w = w0 + i <= final ? w0 + i : final;
+            const float* p = P::at(parts, w, first);
+            mw[i] = load1(p + ROWS * D + r);
+            lw[i] = load1(p + ROWS * (D + 1) + r);
+            vw[i] = load2(p + r * D + d);
+        }
+        float next = top;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (w0 + i <= final) next = fmaxf(next, mw[i]);
+        if (next == -__builtin_inff()) continue;
+        const float f = __builtin_amdgcn_exp2f(top - next);
+        top = next;
+        sum *= f;
+        v *= f;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (w0 + i <= final) {
+                const float e = __builtin_amdgcn_exp2f(mw[i] - top);
+                sum = fmaf(lw[i], e, sum);
+                v[0] = fmaf(vw[i][0], e, v[0]);
+                v[1] = fmaf(vw[i][1], e, v[1]);
+            }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    return float2_t{v[0] * inv, v[1] * inv};
+}
+
+// Output row `row` (of the q_len * group that read one head) of an item.
+template <int D>
+__device__ __forceinline__ uint16_t* out_row(const AttnArgs& a, int b, int h, int row) {
+    const int tq = row / a.group;
+    return a.out + ((int64_t)b * a.q_len + tq) * ((int64_t)a.cache.kv_heads * a.group * D) +
+           (int64_t)(h * a.group + row - tq * a.group) * D;
+}
+
+// One workgroup of four waves on its share of the rounds (see Shares), a tile
+// for each wave a round.  Items that lie inside one share are written directly;
+// the others' partial sums go through the workspace, and the workgroup that
+// arrives last adds them in order (or kv4_join_kernel does).
+template <bool BF, int D, int NR>
+__global__ __launch_bounds__(256, D <= 128 && NR == 1 ? 4 : D <= 128 ? 2 : NR == 1 ? 2 : 1)
+void kv4_attn_kernel(AttnArgs a) {
+    constexpr int NT = D / 16;            // 16-dim tiles of the output
+    constexpr int NW = D / 32;            // words of codes per lane and key half
+    constexpr int ROWS = 16 * NR;
+    constexpr int PITCH = D + 4;
+    constexpr int64_t TB = kv4_tile_bytes(D);
+    using P = Parts<D, ROWS>;
+    __shared__ uint32_t scratch[4], before[257];
+    __shared__ float ms[4][ROWS], ls[2][ROWS];
+    __shared__ float acc[2][ROWS * PITCH];
+    __shared__ u32x4 qs[NR][NW][64];
+    __shared__ int last;
+
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Shares sh(a, before, scratch);
+    const uint32_t wg = blockIdx.x;
+    uint32_t at = __builtin_amdgcn_readfirstlane(sh.begin_of(wg));
+    const uint32_t end = __builtin_amdgcn_readfirstlane(sh.begin_of(wg + 1));
+    if (at >= end) return;
+    uint32_t seq_start;                   // rounds (of all heads) before sequence b
+    int b = sh.sequence(at, seq_start);
 
     const Magic mk = magics<BF>(0), mv = magics<BF>(0x80000000u);
+    // Row 0 of a further operand beside the values' codes takes the values'
+    // zero-points, row 1 and 2 the offsets of the low and high dims' codes: one
+    // matrix instruction sums the rounded weights with each of them.
+    const uint32_t off_a = BF ? 0xC30F4300u : 0xE40F6400u;    // -(off + 15), off
+    const uint32_t off_b = BF ? 0xC30F4300u : 0xD4F05400u;
+    const uint32_t off_row = c == 1 ? off_a : c == 2 ? off_b : 0u;
     const int q_rows = a.q_len * a.group;
 
     while (at < end) {
         // ---- the item at `at`
-        const uint32_t len = __builtin_amdgcn_readfirstlane(length_of(b));
-        const uint32_t n_rounds = rounds_of(len);
+        const uint32_t len = __builtin_amdgcn_readfirstlane(Shares::length_of(a, b));
+        const uint32_t n_rounds = Shares::rounds_of(len);
         const uint32_t item = (at - seq_start) / n_rounds;
         const uint32_t item_start = seq_start + item * n_rounds;
         const int h = (int)(item / a.row_blocks), rb = (int)(item % a.row_blocks);
         const uint32_t r0 = at - item_start;
         const uint32_t r1 = end - item_start < n_rounds ? end - item_start : n_rounds;
 
-        u32x4 q[NR][NW];
+        // ---- the wave's tiles: 4 r + wave for r0 <= r < r1, those that begin before len
+        const uint32_t tiles = (len + kKvTile - 1) / kKvTile;
+        // a tile without a page: some memory of the cache, and every key hidden
+        bool here = true;
+        auto tile_at = [&](uint32_t t, bool& found) -> const uint8_t* {
+            const uint8_t* p = kv4_tile(a.cache, b, t * kKvTile, h, TB);
+            found = p != nullptr;
+            return found ? p : a.cache.data;
+        };
+        u32x4 kc[kPieces<D>], vc[kPieces<D>], meta[4];        // meta: k scale, k zero, v scale, v zero
+        auto load_k = [&](const uint8_t* tile) { load_codes<D>(kc, tile, lane); };
+        auto load_meta = [&](const uint8_t* tile) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) meta[i] = *reinterpret_cast<const u32x4*>(tile + 32 * D + g * 64 + i * 16);
+        };
+        auto load_v = [&](const uint8_t* tile) { load_codes<D>(vc, tile + 16 * D, lane); };
+        uint32_t t = 4 * r0 + wave;
+        const uint32_t t_end = 4 * r1 < tiles ? 4 * r1 : tiles;
+        const uint8_t* tile = t < t_end ? tile_at(t, here) : a.cache.data;
+        load_k(tile);
+        load_meta(tile);
+        load_v(tile);
+
+        // The queries as the matrix cores take them, in LDS (the registers hold
+        // sums and codes); wave n % 4 brings row tile n.
         float sum_q[NR], off_q[NR];
         int limit[NR];                    // last visible position of the lane's row
 #pragma unroll
@@ -209,7 +321,7 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(AttnArgs a) {
             for (int w = 0; w < NW; ++w) {
                 u32x4 v = *reinterpret_cast<const u32x4*>(src + 8 * w);
                 if (!real) v = u32x4{0, 0, 0, 0};
-                q[n][w] = v;
+                if (wave == n) qs[n][w][lane] = v;
                 sa += meta_f32<BF>(v, 0) + meta_f32<BF>(v, 1) + meta_f32<BF>(v, 4) + meta_f32<BF>(v, 5);
                 sb += meta_f32<BF>(v, 2) + meta_f32<BF>(v, 3) + meta_f32<BF>(v, 6) + meta_f32<BF>(v, 7);
             }
@@ -218,100 +330,104 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(AttnArgs a) {
             sum_q[n] = sa + sb;
             off_q[n] = sa * kOffA<BF> + sb * kOffB<BF>;
         }
-        float4_t o[NR][NT];
-        float m[NR], l[NR], pe[NR], po[NR], pz[NR];   // max; sums of P, P' over even and odd keys, P' z
+        __syncthreads();
+        float4_t o[NR][NT], osum[NR];     // osum: rows 0..2 of the further operand
+        float m[NR], l[NR];               // maximum of scale-free scores; sum of weights
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             m[n] = -__builtin_inff();
-            l[n] = pe[n] = po[n] = pz[n] = 0.f;
+            l[n] = 0.f;
+            osum[n] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int t = 0; t < NT; ++t) o[n][t] = float4_t{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < NT; ++k) o[n][k] = float4_t{0.f, 0.f, 0.f, 0.f};
         }
 
-        // ---- the wave's tiles: 4 r + wave for r0 <= r < r1, those that begin before len
-        const uint32_t tiles = (len + kKvTile - 1) / kKvTile;
-        auto tile_at = [&](uint32_t t) { return kv4_tile(a.cache, b, t * kKvTile, h, TB); };
-        uint32_t t = 4 * r0 + wave;
-        const uint32_t t_end = 4 * r1 < tiles ? 4 * r1 : tiles;
-        TileRegs<D> cur, nxt;
-        const uint8_t* cur_p = t < t_end ? tile_at(t) : nullptr;
-        if (cur_p) cur.load(cur_p, lane);
         for (; t < t_end; t += 4) {
-            const uint8_t* nxt_p = t + 4 < t_end ? tile_at(t + 4) : nullptr;
-            if (nxt_p) nxt.load(nxt_p, lane);
-            if (cur_p) {
+            // each piece of the next tile is fetched as soon as its registers
+            // are free (after the last tile, of that one again)
+            bool next_here = here;
+            if (t + 4 < t_end) tile = tile_at(t + 4, next_here);
+            {
                 float4_t s[NR][2];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
 #pragma unroll
-                    for (int n = 0; n < NR; ++n) s[n][u] = float4_t{0.f, 0.f, 0.f, 0.f};
+                    for (int n = 0; n < NR; ++n) s[n][u] = float4_t{-off_q[n], -off_q[n], -off_q[n], -off_q[n]};
 #pragma unroll
                     for (int w = 0; w < NW; ++w) {
-                        const u32x4 kc = code_pairs<BF>(TileRegs<D>::word(cur.k, u, w), mk);
+                        const u32x4 kf = code_pairs<BF>(code_word<D>(kc, u, w), mk);
 #pragma unroll
-                        for (int n = 0; n < NR; ++n) s[n][u] = mfma16<BF>(kc, q[n][w], s[n][u]);
+                        for (int n = 0; n < NR; ++n) s[n][u] = mfma16<BF>(kf, qs[n][w][lane], s[n][u]);
                     }
                 }
+                load_k(tile);
                 // slot i of the lane: key 16 (i / 4) + 4 g + i % 4 of the tile
-                float sk[8], zk[8], sv[8], zv[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    sk[i] = meta_f32<BF>(cur.meta[0], i) * a.scale2;
-                    zk[i] = meta_f32<BF>(cur.meta[1], i);
-                    sv[i] = meta_f32<BF>(cur.meta[2], i);
-                    zv[i] = meta_f32<BF>(cur.meta[3], i);
-                }
                 const int key0 = (int)(t * kKvTile) + 4 * g;
-                const bool masked = (int)(t * kKvTile) + kKvTile - 1 > (int)len - a.q_len;
-                u32x4 p[NR];
+                const bool edge = !here || (int)(t * kKvTile) + kKvTile - 1 > (int)len - a.q_len;
+                u32x4 p[NR], zrow = meta[3];
+                float x[NR][8];
 #pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    float x[8];
-                    float top = -__builtin_inff();
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        x[n][i] = fmaf(-meta_f32<BF>(meta[1], i), sum_q[n], s[n][i / 4][i % 4]) *
+                                  meta_f32<BF>(meta[0], i);
+                if (edge) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        x[i] = fmaf(-zk[i], sum_q[n], s[n][i / 4][i % 4] - off_q[n]) * sk[i];
-                        if (masked && key0 + 16 * (i / 4) + i % 4 > limit[n]) x[i] = -__builtin_inff();
-                        top = fmaxf(top, x[i]);
+                        const int key = here ? key0 + 16 * (i / 4) + i % 4 : INT32_MAX;
+#pragma unroll
+                        for (int n = 0; n < NR; ++n)
+                            if (key > limit[n]) x[n][i] = -__builtin_inff();
+                        // no zero-points of positions that were never written
+                        if (key >= (int)len) zrow[i / 2] &= i & 1 ? 0xFFFFu : 0xFFFF0000u;
                     }
-                    top = fmaxf(top, __shfl_xor(top, 16));
-                    top = fmaxf(top, __shfl_xor(top, 32));
+                }
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    float top = m[n];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[n][i]);
+                    top = max_over_groups(top);
                     if (__any(top > m[n])) {
-                        const float next = fmaxf(m[n], top);
-                        const float f = next == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[n] - next);
-                        m[n] = next;
+                        const float f =
+                            top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m[n] - top) * a.scale2);
+                        m[n] = top;
                         l[n] *= f;
-                        pe[n] *= f;
-                        po[n] *= f;
-                        pz[n] *= f;
+                        osum[n] *= f;
 #pragma unroll
                         for (int k = 0; k < NT; ++k) o[n][k] *= f;
                     }
-                    const float base = m[n] == -__builtin_inff() ? 0.f : m[n];
+                    const float base = m[n] == -__builtin_inff() ? 0.f : m[n] * a.scale2;
 #pragma unroll
-                    for (int i = 0; i < 8; i += 2) {
-                        float w2[2], z2[2];
+                    for (int i = 0; i < 8; ++i) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(x[n][i], a.scale2, -base));
+                        l[n] += e;
+                        x[n][i] = e * meta_f32<BF>(meta[2], i);
+                    }
+                }
+                if (edge) {               // a hidden value's scale may be anything
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float e = __builtin_amdgcn_exp2f(x[i + j] - base);
-                            l[n] += e;
-                            const bool hidden = masked && key0 + 16 * (i / 4) + (i + j) % 4 > limit[n];
-                            w2[j] = hidden ? 0.f : e * sv[i + j];
-                            z2[j] = hidden ? 0.f : zv[i + j];
-                        }
-                        const uint32_t pr = round_out2<BF>(w2[0], w2[1]);
-                        p[n][i / 2] = pr;
-                        // the sums use P' as the matrix cores see it
-                        const float ra = scale_f32<BF>(pr & 0xFFFFu), rc = scale_f32<BF>(pr >> 16);
-                        pe[n] += ra;
-                        po[n] += rc;
-                        pz[n] = fmaf(ra, z2[0], fmaf(rc, z2[1], pz[n]));
+                    for (int i = 0; i < 8; ++i) {
+                        const int key = here ? key0 + 16 * (i / 4) + i % 4 : INT32_MAX;
+#pragma unroll
+                        for (int n = 0; n < NR; ++n)
+                            if (key > limit[n]) x[n][i] = 0.f;
                     }
                 }
 #pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[n][i] = round_out2<BF>(x[n][2 * i], x[n][2 * i + 1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) zrow[i] = c == 0 ? zrow[i] : off_row;
+                load_meta(tile);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) osum[n] = mfma16<BF>(zrow, p[n], osum[n]);
+#pragma unroll
                 for (int w = 0; w < NW; ++w) {
-                    const u32x4 a0 = code_pairs<BF>(TileRegs<D>::word(cur.v, 0, w), mv);
-                    const u32x4 a1 = code_pairs<BF>(TileRegs<D>::word(cur.v, 1, w), mv);
+                    const u32x4 a0 = code_pairs<BF>(code_word<D>(vc, 0, w), mv);
+                    const u32x4 a1 = code_pairs<BF>(code_word<D>(vc, 1, w), mv);
                     const u32x4 lo{a0[0], a0[2], a1[0], a1[2]}, hi{a0[1], a0[3], a1[1], a1[3]};
 #pragma unroll
                     for (int n = 0; n < NR; ++n) {
@@ -319,25 +435,24 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(AttnArgs a) {
                         o[n][NW + w] = mfma16<BF>(hi, p[n], o[n][NW + w]);
                     }
                 }
+                load_v(tile);
             }
-            cur = nxt;
-            cur_p = nxt_p;
+            here = next_here;
         }
 
         // ---- the wave's sums: offsets and zero-points leave
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             l[n] = over_groups(l[n]);
-            pe[n] = over_groups(pe[n]);
-            po[n] = over_groups(po[n]);
-            pz[n] = over_groups(pz[n]);
-            const float ca = kOffA<BF> * pe[n] - (kOffA<BF> + 15.f) * po[n] + pz[n];
-            const float cb = kOffB<BF> * pe[n] - (kOffB<BF> + 15.f) * po[n] + pz[n];
+            // the three sums of column c are in lane c (group 0)
+            const float z = __shfl(osum[n][0], c);
+            const float ca = z + __shfl(osum[n][1], c), cb = z + __shfl(osum[n][2], c);
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 o[n][w] -= ca;
                 o[n][NW + w] -= cb;
             }
+            m[n] *= a.scale2;
             if (g == 0) ms[wave][n * 16 + c] = m[n];
         }
         __syncthreads();
@@ -376,19 +491,14 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(AttnArgs a) {
             __syncthreads();
         }
 
-        auto out_row = [&](int row) {
-            const int tq = row / a.group;
-            return a.out + ((int64_t)b * a.q_len + tq) * ((int64_t)a.cache.kv_heads * a.group * D) +
-                   (int64_t)(h * a.group + row - tq * a.group) * D;
-        };
         const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
-        const uint32_t first = owner_wg(item_start), final_wg = owner_wg(item_start + n_rounds - 1);
-        if (first == final_wg) {
+        const uint32_t first = sh.owner(item_start), final = sh.owner(item_start + n_rounds - 1);
+        if (first == final) {
             if (wave == 0) {
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     if (n * 16 + c >= rows_here) continue;
-                    uint16_t* dst = out_row(rb * ROWS + n * 16 + c) + 4 * g;
+                    uint16_t* dst = out_row<D>(a, b, h, rb * ROWS + n * 16 + c) + 4 * g;
                     const float inv = l[n] == 0.f ? 0.f : 1.f / l[n];
 #pragma unroll
                     for (int k = 0; k < NT; ++k) {
@@ -399,85 +509,111 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(AttnArgs a) {
                 }
             }
         } else {
-            // Partial sums and counters are touched only by agent-scope atomic
-            // accesses, which pass the per-XCD L2; the stores complete before
-            // the arrival is counted.
+            // Where the last workgroup adds the parts, they and the counters
+            // are touched only by agent-scope atomic accesses, which pass the
+            // per-XCD L2, and the stores complete before the arrival is counted.
+            auto store2 = [](float* p, float x, float y) {
+                __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, float2_t{x, y}),
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            };
             if (wave == 0) {
-                float* slot = a.parts + ((int64_t)wg * 2 + (wg == first ? 1 : 0)) * SLOT;
+                float* slot = P::at(a.parts, wg, first);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     const int r = n * 16 + c;
                     if (r >= rows_here) continue;
                     float* dst = slot + r * D + 4 * g;
 #pragma unroll
-                    for (int k = 0; k < NT; ++k)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            __hip_atomic_store(dst + 16 * k + i, o[n][k][i], __ATOMIC_RELAXED,
-                                               __HIP_MEMORY_SCOPE_AGENT);
+                    for (int k = 0; k < NT; ++k) {
+                        if (a.counters) {
+                            store2(dst + 16 * k, o[n][k][0], o[n][k][1]);
+                            store2(dst + 16 * k + 2, o[n][k][2], o[n][k][3]);
+                        } else {
+                            *reinterpret_cast<float4_t*>(dst + 16 * k) = o[n][k];
+                        }
+                    }
                     if (g == 0) {
                         __hip_atomic_store(slot + ROWS * D + r, m[n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                         __hip_atomic_store(slot + ROWS * (D + 1) + r, l[n], __ATOMIC_RELAXED,
                                            __HIP_MEMORY_SCOPE_AGENT);
                     }
                 }
-                __builtin_amdgcn_s_waitcnt(0);
-                if (lane == 0)
-                    last = __hip_atomic_fetch_add(&a.counters[first], 1u, __ATOMIC_RELAXED,
-                                                  __HIP_MEMORY_SCOPE_AGENT) == final_wg - first;
             }
-            __syncthreads();
-            if (last) {
-                auto part = [&](uint32_t w) {
-                    return a.parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * SLOT;
-                };
-                auto load = [](const float* p) {
-                    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                };
-                for (int i = tid; i < rows_here * D; i += 256) {
-                    const int r = i / D, d = i % D;
-                    float top = -__builtin_inff();
-                    for (uint32_t w = first; w <= final_wg; ++w) top = fmaxf(top, load(part(w) + ROWS * D + r));
-                    float sum = 0.f, v = 0.f;
-                    for (uint32_t w = first; w <= final_wg; ++w) {
-                        const float* p = part(w);
-                        const float mw = load(p + ROWS * D + r);
-                        const float f = mw == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mw - top);
-                        sum = fmaf(load(p + ROWS * (D + 1) + r), f, sum);
-                        v = fmaf(load(p + r * D + d), f, v);
-                    }
-                    out_row(rb * ROWS + r)[d] = round_out<BF>(sum == 0.f ? 0.f : v / sum);
+            if (a.counters) {
+                if (wave == 0) {
+                    __builtin_amdgcn_s_waitcnt(0);
+                    if (lane == 0)
+                        last = __hip_atomic_fetch_add(&a.counters[first], 1u, __ATOMIC_RELAXED,
+                                                      __HIP_MEMORY_SCOPE_AGENT) == final - first;
                 }
-                if (tid == 0)
-                    __hip_atomic_store(&a.counters[first], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __syncthreads();
+                if (last) {
+                    auto load1 = [](const float* p) {
+                        return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    };
+                    auto load2 = [](const float* p) {
+                        return __builtin_bit_cast(float2_t,
+                                                  __hip_atomic_load(reinterpret_cast<const uint64_t*>(p),
+                                                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+                    };
+                    for (int i = 2 * tid; i < rows_here * D; i += 512) {
+                        const float2_t v = join_parts<D, ROWS>(a.parts, first, final, i / D, i % D, load2, load1);
+                        *reinterpret_cast<uint32_t*>(out_row<D>(a, b, h, rb * ROWS + i / D) + i % D) =
+                            round_out2<BF>(v[0], v[1]);
+                    }
+                    if (tid == 0)
+                        __hip_atomic_store(&a.counters[first], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+                __syncthreads();          // `last` is read before the next item sets it
             }
-            __syncthreads();              // `last` is read before the next item sets it
         }
 
         at = item_start + r1;
-        if (item + 1 == heads && r1 == n_rounds) {
-            seq_start += heads * n_rounds;
+        if (item + 1 == sh.heads && r1 == n_rounds) {
+            seq_start += sh.heads * n_rounds;
             ++b;
         }
     }
 }
 
+// The parts of items that several workgroups share, added by a launch of its
+// own: workgroup (w, y) takes 512 sums, from y * 512 on, of the item that begins
+// in share w and does not end there.
+template <bool BF, int D, int NR>
+__global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a) {
+    constexpr int ROWS = 16 * NR;
+    __shared__ uint32_t scratch[4], before[257];
+    const Shares sh(a, before, scratch);
+    const uint32_t w = blockIdx.x, begin = sh.begin_of(w), end = sh.begin_of(w + 1);
+    if (begin >= end) return;
+    uint32_t seq_start;
+    const int b = sh.sequence(end - 1, seq_start);
+    const uint32_t n_rounds = Shares::rounds_of(Shares::length_of(a, b));
+    const uint32_t item = (end - 1 - seq_start) / n_rounds, item_start = seq_start + item * n_rounds;
+    const uint32_t final = sh.owner(item_start + n_rounds - 1);
+    if (item_start < begin || final == w) return;
+    const int h = (int)(item / a.row_blocks), rb = (int)(item % a.row_blocks);
+    const int q_rows = a.q_len * a.group;
+    const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
+    const int i = blockIdx.y * 512 + 2 * threadIdx.x;
+    if (i >= rows_here * D) return;
+    const float2_t v = join_parts<D, ROWS>(
+        a.parts, w, final, i / D, i % D, [](const float* p) { return *reinterpret_cast<const float2_t*>(p); },
+        [](const float* p) { return *p; });
+    *reinterpret_cast<uint32_t*>(out_row<D>(a, b, h, rb * ROWS + i / D) + i % D) = round_out2<BF>(v[0], v[1]);
+}
+
 // Rows per workgroup (16 or 32) and the blocks of them that q_rows need.
 int row_tiles(int q_rows) { return q_rows <= 16 ? 1 : 2; }
-
-// Most workgroups of a launch: the workspace is sized for them.
-constexpr int kMostCus = 304;
-int64_t most_wgs(int64_t items) {
-    (void)items;
-    return (int64_t)kMostCus * kWgPerCu;
-}
+// Workgroups that a compute unit holds: the launch bounds above.
+int wgs_per_cu(int D, int nr) { return D <= 128 ? (nr == 1 ? 4 : 2) : nr == 1 ? 2 : 1; }
 
 }  // namespace
 
 int64_t kv4_attention_workspace_bytes(int64_t batch, int q_len, int q_heads, int kv_heads, int D) {
-    const int rows = 16 * row_tiles(q_len * (q_heads / kv_heads));
-    const int64_t w = most_wgs(batch * kv_heads);
-    return align256(w * 4) + align256(w * 2 * rows * (D + 2) * 4);
+    (void)batch;
+    const int nr = row_tiles(q_len * (q_heads / kv_heads));
+    return align256(kMostWgs * 4) + align256((int64_t)kMostWgs * 2 * 16 * nr * (D + 2) * 4);
 }
 
 int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride, const int32_t* lens, int64_t batch,
@@ -495,26 +631,39 @@ int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride,
     a.capacity = c.max_pages * c.page_size;
     a.scale2 = scale * 1.4426950408889634f;
     a.out = static_cast<uint16_t*>(out);
-    const int64_t most = most_wgs(batch * c.kv_heads);
     a.counters = static_cast<uint32_t*>(ws);
-    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(most * 4));
+    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(kMostWgs * 4));
     // no more workgroups than rounds there can be
-    const int64_t rounds = batch * c.kv_heads * a.row_blocks * ((a.capacity + kRoundKeys - 1) / kRoundKeys);
-    int64_t wgs = (int64_t)device_cus(s) * kWgPerCu;
-    if (wgs > most) wgs = most;
-    if (wgs > rounds) wgs = rounds;
-    const dim3 grid((unsigned)wgs);
-    auto go = [&](auto d) {
-        constexpr int D = decltype(d)::value;
-        if (c.dtype == TF_BF16)
-            return nr == 1 ? launch(kv4_attn_kernel<true, D, 1>, grid, dim3(256), 0, s, a)
-                           : launch(kv4_attn_kernel<true, D, 2>, grid, dim3(256), 0, s, a);
-        return nr == 1 ? launch(kv4_attn_kernel<false, D, 1>, grid, dim3(256), 0, s, a)
-                       : launch(kv4_attn_kernel<false, D, 2>, grid, dim3(256), 0, s, a);
+    const int64_t item_rounds = (a.capacity + kRoundKeys - 1) / kRoundKeys;
+    const int64_t items = batch * c.kv_heads * a.row_blocks;
+    int64_t wgs = (int64_t)device_cus(s) * wgs_per_cu(c.head_dim, nr);
+    if (wgs > kMostWgs) wgs = kMostWgs;
+    if (wgs > items * item_rounds) wgs = items * item_rounds;
+    a.wgs = (uint32_t)wgs;
+    // Parts of one item, at most: as many as one long sequence among empty ones
+    // makes.  Many large ones are added by a launch of its own, many workgroups
+    // to an item.
+    const int64_t most = wgs / (c.kv_heads * a.row_blocks) < item_rounds ? wgs / (c.kv_heads * a.row_blocks) : item_rounds;
+    const int64_t part_rows = q_rows < 16 * nr ? q_rows : 16 * nr;
+    const bool join = most * part_rows * c.head_dim * 4 > 256 * 1024;
+    if (join) a.counters = nullptr;
+    const dim3 grid((unsigned)wgs), join_grid((unsigned)wgs, (unsigned)((part_rows * c.head_dim + 511) / 512));
+    auto go = [&](auto d, auto n, auto bf) {
+        constexpr int D = decltype(d)::value, NR = decltype(n)::value;
+        constexpr bool BF = decltype(bf)::value;
+        const int rc = launch(kv4_attn_kernel<BF, D, NR>, grid, dim3(256), 0, s, a);
+        if (rc || !join) return rc;
+        return launch(kv4_join_kernel<BF, D, NR>, join_grid, dim3(256), 0, s, a);
     };
-    if (c.head_dim == 64) return go(std::integral_constant<int, 64>{});
-    if (c.head_dim == 128) return go(std::integral_constant<int, 128>{});
-    return go(std::integral_constant<int, 256>{});
+    auto by_rows = [&](auto d, auto bf) {
+        return nr == 1 ? go(d, std::integral_constant<int, 1>{}, bf) : go(d, std::integral_constant<int, 2>{}, bf);
+    };
+    auto by_type = [&](auto d) {
+        return c.dtype == TF_BF16 ? by_rows(d, std::true_type{}) : by_rows(d, std::false_type{});
+    };
+    if (c.head_dim == 64) return by_type(std::integral_constant<int, 64>{});
+    if (c.head_dim == 128) return by_type(std::integral_constant<int, 128>{});
+    return by_type(std::integral_constant<int, 256>{});
 }
 
 }  // namespace tf
