@@ -18,6 +18,7 @@ Kv4 kv4_view(const tf_kv4_cache& c);
 namespace {
 
 constexpr int kRoundKeys = 128;          // keys of one round: a tile of 32 for each of 4 waves
+constexpr uint32_t kItemCost = 4;        // what beginning and ending an item costs, in rounds
 constexpr int kMostWgs = 2048;           // workgroups of a launch, at most
 
 struct AttnArgs {
@@ -91,10 +92,14 @@ __device__ __forceinline__ uint32_t code_word(const u32x4* x, int u, int w) {
     if constexpr (D == 64) return x[0][2 * u + w];
     else return x[u * (D / 128) + w / 4][w % 4];
 }
+typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
+__device__ __forceinline__ u32x4 load16(GlobalBytes p) {
+    return *(const __attribute__((address_space(1))) u32x4*)p;
+}
 template <int D>
-__device__ __forceinline__ void load_codes(u32x4* x, const uint8_t* codes, int lane) {
+__device__ __forceinline__ void load_codes(u32x4* x, GlobalBytes codes, uint32_t lane_offset) {
 #pragma unroll
-    for (int p = 0; p < kPieces<D>; ++p) x[p] = *reinterpret_cast<const u32x4*>(codes + p * 1024 + lane * 16);
+    for (int p = 0; p < kPieces<D>; ++p) x[p] = load16(codes + p * 1024 + lane_offset);
 }
 
 // Value i (0..7) of eight packed 16-bit floats.
@@ -105,14 +110,21 @@ __device__ __forceinline__ float meta_f32(const u32x4& m, int i) {
     else return scale_f32<false>(i & 1 ? w >> 16 : w & 0xFFFFu);
 }
 
+// A pointer to memory that no kernel writes while this one runs, as the scalar
+// loads take it.
+__device__ __forceinline__ const __attribute__((address_space(4))) int32_t* as_constant(const int32_t* p) {
+    return (const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
+}
+
 // How the rounds of all items are shared out.  An item is one (sequence,
 // key/value head, block of query rows); its rounds are 128 keys each, at least
-// one (which writes the zeros of an empty row).  Workgroup w of `wgs` takes a
-// contiguous share of all rounds, in the order of sequence, head and block, and
-// shares differ by at most one round whatever the lengths are.
+// one (which writes the zeros of an empty row), and it counts kItemCost units
+// of its own before them.  Workgroup w of `wgs` takes a contiguous share of all
+// units, in the order of sequence, head and block, and shares differ by at most
+// one unit whatever the lengths are.
 struct Shares {
     const AttnArgs& a;
-    const uint32_t* before;               // LDS: rounds of one head before each thread's sequences
+    const uint32_t* before;               // LDS: units of one head before each thread's sequences
     int seg;                              // sequences of a thread in `before`
     uint32_t heads, share, extra;
 
@@ -120,15 +132,21 @@ struct Shares {
         const int64_t n = a.lens[b];
         return (uint32_t)(n < 0 ? 0 : n > a.capacity ? a.capacity : n);
     }
+    // the same for a b that all lanes share
+    __device__ __forceinline__ static uint32_t uniform_length(const AttnArgs& a, int b) {
+        const int64_t n = as_constant(a.lens)[b];
+        return (uint32_t)(n < 0 ? 0 : n > a.capacity ? a.capacity : n);
+    }
     __device__ __forceinline__ static uint32_t rounds_of(uint32_t n) {
         return n == 0 ? 1u : (n + kRoundKeys - 1) / kRoundKeys;
     }
+    __device__ __forceinline__ static uint32_t units_of(uint32_t n) { return kItemCost + rounds_of(n); }
     // All 256 threads; before: 257 words of LDS, scratch: 4.
     __device__ __forceinline__ Shares(const AttnArgs& args, uint32_t* lds, uint32_t* scratch) : a(args), before(lds) {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         seg = (a.batch + 255) / 256;
         uint32_t sum = 0;
-        for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) sum += rounds_of(length_of(a, b));
+        for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) sum += units_of(length_of(a, b));
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t o = __shfl_up(sum, d);
@@ -146,12 +164,12 @@ struct Shares {
         extra = total % a.wgs;
     }
     __device__ __forceinline__ uint32_t begin_of(uint32_t w) const { return w * share + (w < extra ? w : extra); }
-    // the workgroup that takes round x
+    // the workgroup that takes unit x
     __device__ __forceinline__ uint32_t owner(uint32_t x) const {
         const uint32_t big = extra * (share + 1);
         return x < big ? x / (share + 1) : extra + (x - big) / share;
     }
-    // the sequence of round x, and the rounds before its first
+    // the sequence of unit x, and the units before its first
     __device__ __forceinline__ int sequence(uint32_t x, uint32_t& seq_start) const {
         x /= heads;
         int s0 = 0, s1 = 256;
@@ -160,15 +178,15 @@ struct Shares {
             if (before[mid] <= x) s0 = mid;
             else s1 = mid;
         }
-        int b = s0 * seg;
-        uint32_t done = before[s0];
+        int b = __builtin_amdgcn_readfirstlane(s0 * seg);
+        uint32_t done = __builtin_amdgcn_readfirstlane(before[s0]);
         for (;; ++b) {
-            const uint32_t n = rounds_of(length_of(a, b));
+            const uint32_t n = units_of(uniform_length(a, b));
             if (x < done + n) break;
             done += n;
         }
-        seq_start = __builtin_amdgcn_readfirstlane(done * heads);
-        return __builtin_amdgcn_readfirstlane(b);
+        seq_start = done * heads;
+        return b;
     }
 };
 
@@ -182,6 +200,12 @@ struct Parts {
         return parts + ((int64_t)w * 2 + (w == first ? 1 : 0)) * kSlot;
     }
 };
+
+// What sums under the maximum m weigh under the maximum `to`; nothing where
+// they hold nothing (a NaN among them stays one: it is multiplied, not skipped).
+__device__ __forceinline__ float weight_of(float m, float to) {
+    return m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - to);
+}
 
 // Adds the parts of workgroups first..final at two neighbouring sums of row r,
 // in their order, and returns the two outputs.  load2: two floats at an even
@@ -208,15 +232,14 @@ __device__ __forceinline__ float2_t join_parts(float* parts, uint32_t first, uin
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
             if (w0 + i <= final) next = fmaxf(next, mw[i]);
-        if (next == -__builtin_inff()) continue;
-        const float f = __builtin_amdgcn_exp2f(top - next);
+        const float f = weight_of(top, next);
         top = next;
         sum *= f;
         v *= f;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
             if (w0 + i <= final) {
-                const float e = __builtin_amdgcn_exp2f(mw[i] - top);
+                const float e = weight_of(mw[i], top);
                 sum = fmaf(lw[i], e, sum);
                 v[0] = fmaf(vw[i][0], e, v[0]);
                 v[1] = fmaf(vw[i][1], e, v[1]);
@@ -260,9 +283,11 @@ void kv4_attn_kernel(AttnArgs a) {
     uint32_t at = __builtin_amdgcn_readfirstlane(sh.begin_of(wg));
     const uint32_t end = __builtin_amdgcn_readfirstlane(sh.begin_of(wg + 1));
     if (at >= end) return;
-    uint32_t seq_start;                   // rounds (of all heads) before sequence b
+    uint32_t seq_start;                   // units (of all heads) before sequence b
     int b = sh.sequence(at, seq_start);
 
+    // the lane's place in a tile: 32-bit offsets from an address that all lanes share
+    const uint32_t lane_offset = lane * 16, meta_offset = g * 64;
     const Magic mk = magics<BF>(0), mv = magics<BF>(0x80000000u);
     // Row 0 of a further operand beside the values' codes takes the values'
     // zero-points, row 1 and 2 the offsets of the low and high dims' codes: one
@@ -274,33 +299,49 @@ void kv4_attn_kernel(AttnArgs a) {
 
     while (at < end) {
         // ---- the item at `at`
-        const uint32_t len = __builtin_amdgcn_readfirstlane(Shares::length_of(a, b));
-        const uint32_t n_rounds = Shares::rounds_of(len);
-        const uint32_t item = (at - seq_start) / n_rounds;
-        const uint32_t item_start = seq_start + item * n_rounds;
+        const uint32_t len = Shares::uniform_length(a, b);
+        const uint32_t n_rounds = Shares::rounds_of(len), n_units = Shares::units_of(len);
+        const uint32_t item = (at - seq_start) / n_units;
+        const uint32_t item_rounds = seq_start + item * n_units + kItemCost;      // unit of its first round
         const int h = (int)(item / a.row_blocks), rb = (int)(item % a.row_blocks);
-        const uint32_t r0 = at - item_start;
-        const uint32_t r1 = end - item_start < n_rounds ? end - item_start : n_rounds;
+        const uint32_t r0 = at > item_rounds ? at - item_rounds : 0;
+        const uint32_t item_end = item_rounds + n_rounds;
+        const uint32_t r1 = (end < item_end ? end : item_end) - item_rounds;
+        at = end < item_end ? end : item_end;
+        const int this_b = b;
+        if (item + 1 == sh.heads && at == item_end) {
+            seq_start += sh.heads * n_units;
+            ++b;
+        }
+        if (at <= item_rounds) continue;  // the share ends before the item's rounds
 
         // ---- the wave's tiles: 4 r + wave for r0 <= r < r1, those that begin before len
         const uint32_t tiles = (len + kKvTile - 1) / kKvTile;
-        // a tile without a page: some memory of the cache, and every key hidden
+        // Table entries are read through the scalar cache, an iteration ahead: a
+        // vector load would wait in line behind the codes.  A tile without a
+        // page is some memory of the cache, and every key of it hidden.
         bool here = true;
-        auto tile_at = [&](uint32_t t, bool& found) -> const uint8_t* {
-            const uint8_t* p = kv4_tile(a.cache, b, t * kKvTile, h, TB);
-            found = p != nullptr;
-            return found ? p : a.cache.data;
+        const uint32_t page_tiles = (uint32_t)a.cache.tiles;
+        const auto* row = as_constant(a.cache.table) + this_b * a.cache.table_stride;
+        auto entry_of = [&](uint32_t t) { return row[t / page_tiles]; };
+        auto tile_at = [&](uint32_t t, int32_t page, bool& found) {
+            found = page >= 0 && page < a.cache.pages;
+            const uint8_t* p = a.cache.data + (found ? (int64_t)page * a.cache.page_bytes +
+                                                           ((int64_t)h * page_tiles + t % page_tiles) * TB : 0);
+            asm("" : "+s"(p));            // in scalar registers, the lanes' offsets beside it
+            return (GlobalBytes)(uintptr_t)p;
         };
         u32x4 kc[kPieces<D>], vc[kPieces<D>], meta[4];        // meta: k scale, k zero, v scale, v zero
-        auto load_k = [&](const uint8_t* tile) { load_codes<D>(kc, tile, lane); };
-        auto load_meta = [&](const uint8_t* tile) {
+        auto load_k = [&](GlobalBytes tile) { load_codes<D>(kc, tile, lane_offset); };
+        auto load_meta = [&](GlobalBytes tile) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) meta[i] = *reinterpret_cast<const u32x4*>(tile + 32 * D + g * 64 + i * 16);
+            for (int i = 0; i < 4; ++i) meta[i] = load16(tile + 32 * D + i * 16 + meta_offset);
         };
-        auto load_v = [&](const uint8_t* tile) { load_codes<D>(vc, tile + 16 * D, lane); };
+        auto load_v = [&](GlobalBytes tile) { load_codes<D>(vc, tile + 16 * D, lane_offset); };
         uint32_t t = 4 * r0 + wave;
         const uint32_t t_end = 4 * r1 < tiles ? 4 * r1 : tiles;
-        const uint8_t* tile = t < t_end ? tile_at(t, here) : a.cache.data;
+        GlobalBytes tile = tile_at(t, t < t_end ? entry_of(t) : -1, here);
+        int32_t entry = t + 4 < t_end ? entry_of(t + 4) : -1;
         load_k(tile);
         load_meta(tile);
         load_v(tile);
@@ -314,7 +355,7 @@ void kv4_attn_kernel(AttnArgs a) {
             const int row = rb * ROWS + n * 16 + c;
             const bool real = row < q_rows;
             const int tq = real ? row / a.group : 0, hq = h * a.group + (real ? row - tq * a.group : 0);
-            const uint16_t* src = a.q + ((int64_t)b * a.q_len + tq) * a.q_stride + (int64_t)hq * D + g * (D / 4);
+            const uint16_t* src = a.q + ((int64_t)this_b * a.q_len + tq) * a.q_stride + (int64_t)hq * D + g * (D / 4);
             limit[n] = (int)len - a.q_len + tq;
             float sa = 0.f, sb = 0.f;
 #pragma unroll
@@ -346,7 +387,8 @@ void kv4_attn_kernel(AttnArgs a) {
             // each piece of the next tile is fetched as soon as its registers
             // are free (after the last tile, of that one again)
             bool next_here = here;
-            if (t + 4 < t_end) tile = tile_at(t + 4, next_here);
+            if (t + 4 < t_end) tile = tile_at(t + 4, entry, next_here);
+            if (t + 8 < t_end) entry = entry_of(t + 8);
             {
                 float4_t s[NR][2];
 #pragma unroll
@@ -461,7 +503,7 @@ void kv4_attn_kernel(AttnArgs a) {
         for (int n = 0; n < NR; ++n) {
             const int r = n * 16 + c;
             const float all = fmaxf(fmaxf(ms[0][r], ms[1][r]), fmaxf(ms[2][r], ms[3][r]));
-            const float f = m[n] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m[n] - all);
+            const float f = weight_of(m[n], all);
             m[n] = all;
             l[n] *= f;
 #pragma unroll
@@ -492,13 +534,13 @@ void kv4_attn_kernel(AttnArgs a) {
         }
 
         const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
-        const uint32_t first = sh.owner(item_start), final = sh.owner(item_start + n_rounds - 1);
+        const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_end - 1);
         if (first == final) {
             if (wave == 0) {
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     if (n * 16 + c >= rows_here) continue;
-                    uint16_t* dst = out_row<D>(a, b, h, rb * ROWS + n * 16 + c) + 4 * g;
+                    uint16_t* dst = out_row<D>(a, this_b, h, rb * ROWS + n * 16 + c) + 4 * g;
                     const float inv = l[n] == 0.f ? 0.f : 1.f / l[n];
 #pragma unroll
                     for (int k = 0; k < NT; ++k) {
@@ -558,7 +600,7 @@ void kv4_attn_kernel(AttnArgs a) {
                     };
                     for (int i = 2 * tid; i < rows_here * D; i += 512) {
                         const float2_t v = join_parts<D, ROWS>(a.parts, first, final, i / D, i % D, load2, load1);
-                        *reinterpret_cast<uint32_t*>(out_row<D>(a, b, h, rb * ROWS + i / D) + i % D) =
+                        *reinterpret_cast<uint32_t*>(out_row<D>(a, this_b, h, rb * ROWS + i / D) + i % D) =
                             round_out2<BF>(v[0], v[1]);
                     }
                     if (tid == 0)
@@ -567,40 +609,80 @@ void kv4_attn_kernel(AttnArgs a) {
                 __syncthreads();          // `last` is read before the next item sets it
             }
         }
-
-        at = item_start + r1;
-        if (item + 1 == sh.heads && r1 == n_rounds) {
-            seq_start += sh.heads * n_rounds;
-            ++b;
-        }
     }
 }
 
 // The parts of items that several workgroups share, added by a launch of its
-// own: workgroup (w, y) takes 512 sums, from y * 512 on, of the item that begins
-// in share w and does not end there.
+// own: workgroup (i, y) takes 128 sums, from 128 y on, of item i, its eight
+// groups of 32 threads every eighth part each.
 template <bool BF, int D, int NR>
 __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a) {
-    constexpr int ROWS = 16 * NR;
+    constexpr int ROWS = 16 * NR, AHEAD = 4;
+    using P = Parts<D, ROWS>;
     __shared__ uint32_t scratch[4], before[257];
+    __shared__ float4_t vals[8][32];
+    __shared__ float m8[8][32], l8[8][32];
     const Shares sh(a, before, scratch);
-    const uint32_t w = blockIdx.x, begin = sh.begin_of(w), end = sh.begin_of(w + 1);
-    if (begin >= end) return;
-    uint32_t seq_start;
-    const int b = sh.sequence(end - 1, seq_start);
-    const uint32_t n_rounds = Shares::rounds_of(Shares::length_of(a, b));
-    const uint32_t item = (end - 1 - seq_start) / n_rounds, item_start = seq_start + item * n_rounds;
-    const uint32_t final = sh.owner(item_start + n_rounds - 1);
-    if (item_start < begin || final == w) return;
+    const int tid = threadIdx.x, slice = tid >> 5;
+    const int b = blockIdx.x / sh.heads;
+    const uint32_t item = blockIdx.x % sh.heads;
+    uint32_t seq_units = before[b / sh.seg];
+    for (int i = b / sh.seg * sh.seg; i < b; ++i) seq_units += Shares::units_of(Shares::uniform_length(a, i));
+    const uint32_t len = Shares::uniform_length(a, b), n_rounds = Shares::rounds_of(len);
+    const uint32_t item_rounds = seq_units * sh.heads + item * Shares::units_of(len) + kItemCost;
+    const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_rounds + n_rounds - 1);
+    if (first == final) return;
     const int h = (int)(item / a.row_blocks), rb = (int)(item % a.row_blocks);
     const int q_rows = a.q_len * a.group;
-    const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
-    const int i = blockIdx.y * 512 + 2 * threadIdx.x;
-    if (i >= rows_here * D) return;
-    const float2_t v = join_parts<D, ROWS>(
-        a.parts, w, final, i / D, i % D, [](const float* p) { return *reinterpret_cast<const float2_t*>(p); },
-        [](const float* p) { return *p; });
-    *reinterpret_cast<uint32_t*>(out_row<D>(a, b, h, rb * ROWS + i / D) + i % D) = round_out2<BF>(v[0], v[1]);
+    const int i = blockIdx.y * 128 + 4 * (tid & 31), r = i / D, d = i % D;
+    if (blockIdx.y * 128 / D >= q_rows - rb * ROWS) return;   // the group of 128 lies in one row but for D = 64
+    float top = -__builtin_inff(), sum = 0.f;
+    float4_t v = {0.f, 0.f, 0.f, 0.f};
+    for (uint32_t w0 = first + slice; w0 <= final; w0 += 8 * AHEAD) {
+        float mw[AHEAD], lw[AHEAD];
+        float4_t vw[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const uint32_t w = w0 + 8 * k <= final ? w0 + 8 * k : w0;
+            const float* p = P::at(a.parts, w, first);
+            mw[k] = w0 + 8 * k <= final ? p[ROWS * D + r] : -__builtin_inff();
+            lw[k] = p[ROWS * (D + 1) + r];
+            vw[k] = *reinterpret_cast<const float4_t*>(p + r * D + d);
+        }
+        float next = top;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) next = fmaxf(next, mw[k]);
+        const float f = weight_of(top, next);
+        top = next;
+        sum *= f;
+        v *= f;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float e = weight_of(mw[k], top);
+            sum = fmaf(lw[k], e, sum);
+            v += vw[k] * e;
+        }
+    }
+    m8[slice][tid & 31] = top;
+    l8[slice][tid & 31] = sum;
+    vals[slice][tid & 31] = v;
+    __syncthreads();
+    if (slice != 0) return;
+    float all = -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) all = fmaxf(all, m8[k][tid]);
+    sum = 0.f;
+    v = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float e = weight_of(m8[k][tid], all);
+        sum = fmaf(l8[k][tid], e, sum);
+        v += vals[k][tid] * e;
+    }
+    if (rb * ROWS + r >= q_rows) return;
+    v *= sum == 0.f ? 0.f : 1.f / sum;
+    *reinterpret_cast<u32x2*>(out_row<D>(a, b, h, rb * ROWS + r) + d) =
+        u32x2{round_out2<BF>(v[0], v[1]), round_out2<BF>(v[2], v[3])};
 }
 
 // Rows per workgroup (16 or 32) and the blocks of them that q_rows need.
@@ -645,9 +727,9 @@ int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride,
     // to an item.
     const int64_t most = wgs / (c.kv_heads * a.row_blocks) < item_rounds ? wgs / (c.kv_heads * a.row_blocks) : item_rounds;
     const int64_t part_rows = q_rows < 16 * nr ? q_rows : 16 * nr;
-    const bool join = most * part_rows * c.head_dim * 4 > 256 * 1024;
+    const bool join = most * part_rows * c.head_dim * 4 > 256 * 1024 && items <= wgs;
     if (join) a.counters = nullptr;
-    const dim3 grid((unsigned)wgs), join_grid((unsigned)wgs, (unsigned)((part_rows * c.head_dim + 511) / 512));
+    const dim3 grid((unsigned)wgs), join_grid((unsigned)items, (unsigned)((part_rows * c.head_dim + 127) / 128));
     auto go = [&](auto d, auto n, auto bf) {
         constexpr int D = decltype(d)::value, NR = decltype(n)::value;
         constexpr bool BF = decltype(bf)::value;
