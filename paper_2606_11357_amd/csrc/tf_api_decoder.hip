@@ -131,8 +131,8 @@ int tf_kv4_attention(const tf_kv4_cache* cache, const void* Q, int64_t q_stride,
         tf_kv4_attention_workspace_bytes(batch, q_len, q_heads, cache->kv_heads, cache->head_dim);
     if (need < 0) return (int)need;
     if (bad_stride(q_stride, q_heads, cache->head_dim)) return TF_ERR_SHAPE;
-    // the kernel counts 128-key pieces of all sequences and heads in 32 bits
-    const int64_t pieces = (cache->max_pages * cache->page_size + 127) / 128;
+    // the kernel counts pieces of all sequences and heads in 32 bits
+    const int64_t pieces = cache->max_pages * cache->page_size / 128 + 4;
     if (attention_items(batch, q_len, q_heads, cache->kv_heads) > INT32_MAX / pieces) return TF_ERR_SHAPE;
     if (bad_scale(scale) || (int64_t)workspace_bytes < need) return TF_ERR_ARG;
     if (misaligned(Q) || misaligned(O) || misaligned(workspace) || misaligned(lens, 4)) return TF_ERR_ALIGN;

@@ -17,9 +17,11 @@ Kv4 kv4_view(const tf_kv4_cache& c);
 
 namespace {
 
-constexpr int kRoundKeys = 128;          // keys of one round: a tile of 32 for each of 4 waves
-constexpr uint32_t kItemCost = 4;        // what beginning and ending an item costs, in rounds
-constexpr int kMostWgs = 2048;           // workgroups of a launch, at most
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kRoundKeys = kKvTile * kWaves;   // keys of one round: a tile for each wave
+constexpr uint32_t kItemCost = 2;        // what beginning and ending an item costs, in rounds
+constexpr uint32_t kLeastRounds = 4;     // rounds of an item that one workgroup takes before a second helps
+constexpr int kMostWgs = 1024;           // workgroups of a launch, at most
 
 struct AttnArgs {
     Kv4 cache;
@@ -117,16 +119,19 @@ __device__ __forceinline__ const __attribute__((address_space(4))) int32_t* as_c
 }
 
 // How the rounds of all items are shared out.  An item is one (sequence,
-// key/value head, block of query rows); its rounds are 128 keys each, at least
+// key/value head, block of query rows); its rounds are 256 keys each, at least
 // one (which writes the zeros of an empty row), and it counts kItemCost units
 // of its own before them.  Workgroup w of `wgs` takes a contiguous share of all
 // units, in the order of sequence, head and block, and shares differ by at most
-// one unit whatever the lengths are.
+// one unit whatever the lengths are.  Where there are fewer items than
+// workgroups, no more of these work than give an item of average length
+// kLeastRounds rounds each: a few rounds cost less than joining parts (items of
+// one length then end where shares do).
 struct Shares {
     const AttnArgs& a;
     const uint32_t* before;               // LDS: units of one head before each thread's sequences
     int seg;                              // sequences of a thread in `before`
-    uint32_t heads, share, extra;
+    uint32_t heads, total, wgs;
 
     __device__ __forceinline__ static uint32_t length_of(const AttnArgs& a, int b) {
         const int64_t n = a.lens[b];
@@ -141,10 +146,10 @@ struct Shares {
         return n == 0 ? 1u : (n + kRoundKeys - 1) / kRoundKeys;
     }
     __device__ __forceinline__ static uint32_t units_of(uint32_t n) { return kItemCost + rounds_of(n); }
-    // All 256 threads; before: 257 words of LDS, scratch: 4.
+    // All kThreads threads; before: kThreads + 1 words of LDS, scratch: kWaves.
     __device__ __forceinline__ Shares(const AttnArgs& args, uint32_t* lds, uint32_t* scratch) : a(args), before(lds) {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        seg = (a.batch + 255) / 256;
+        seg = (a.batch + kThreads - 1) / kThreads;
         uint32_t sum = 0;
         for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) sum += units_of(length_of(a, b));
 #pragma unroll
@@ -159,25 +164,26 @@ struct Shares {
         if (tid == 0) lds[0] = 0;
         __syncthreads();
         heads = (uint32_t)a.cache.kv_heads * a.row_blocks;
-        const uint32_t total = lds[256] * heads;
-        share = total / a.wgs;
-        extra = total % a.wgs;
+        total = lds[kThreads] * heads;
+        const uint32_t items = heads * a.batch;
+        const uint32_t mean = (lds[kThreads] - kItemCost * a.batch) / a.batch;
+        const uint32_t pieces = (mean + kLeastRounds - 1) / kLeastRounds;
+        wgs = items < a.wgs && items * pieces < a.wgs ? items * (pieces ? pieces : 1) : a.wgs;
     }
-    __device__ __forceinline__ uint32_t begin_of(uint32_t w) const { return w * share + (w < extra ? w : extra); }
-    // the workgroup that takes unit x
+    // floor(w total / wgs)
+    __device__ __forceinline__ uint32_t begin_of(uint32_t w) const { return (uint32_t)((uint64_t)w * total / wgs); }
+    // the workgroup that takes unit x: the last w with begin_of(w) <= x
     __device__ __forceinline__ uint32_t owner(uint32_t x) const {
-        const uint32_t big = extra * (share + 1);
-        return x < big ? x / (share + 1) : extra + (x - big) / share;
+        return (uint32_t)((((uint64_t)x + 1) * wgs + total - 1) / total) - 1;
     }
     // the sequence of unit x, and the units before its first
     __device__ __forceinline__ int sequence(uint32_t x, uint32_t& seq_start) const {
         x /= heads;
-        int s0 = 0, s1 = 256;
-        while (s1 - s0 > 1) {
-            const int mid = (s0 + s1) >> 1;
-            if (before[mid] <= x) s0 = mid;
-            else s1 = mid;
-        }
+        // the last of the kThreads entries that is not above x: eight at a time, then one
+        const int lane = threadIdx.x & 63;
+        static_assert(kThreads == 512, "two steps of 64 and 8");
+        int s0 = 8 * (__popcll(__ballot(before[8 * lane] <= x)) - 1);
+        s0 += __popcll(__ballot(before[s0 + (lane & 7)] <= x) & 0xFF) - 1;
         int b = __builtin_amdgcn_readfirstlane(s0 * seg);
         uint32_t done = __builtin_amdgcn_readfirstlane(before[s0]);
         for (;; ++b) {
@@ -257,22 +263,31 @@ __device__ __forceinline__ uint16_t* out_row(const AttnArgs& a, int b, int h, in
            (int64_t)(h * a.group + row - tq * a.group) * D;
 }
 
-// One workgroup of four waves on its share of the rounds (see Shares), a tile
+// A barrier for what the workgroup shares in LDS: unlike __syncthreads it does
+// not wait for stores to memory.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Waves that a SIMD holds, as the registers of the sums allow.
+constexpr int waves_per_simd(int D, int nr) { return D <= 128 && nr == 1 ? 4 : 2; }
+
+// One workgroup of eight waves on its share of the rounds (see Shares), a tile
 // for each wave a round.  Items that lie inside one share are written directly;
 // the others' partial sums go through the workspace, and the workgroup that
 // arrives last adds them in order (or kv4_join_kernel does).
 template <bool BF, int D, int NR>
-__global__ __launch_bounds__(256, D <= 128 && NR == 1 ? 4 : D <= 128 ? 2 : NR == 1 ? 2 : 1)
-void kv4_attn_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kernel(AttnArgs a) {
     constexpr int NT = D / 16;            // 16-dim tiles of the output
     constexpr int NW = D / 32;            // words of codes per lane and key half
     constexpr int ROWS = 16 * NR;
+    // rows whose sums the waves add at a time, VW neighbouring dims a thread
+    constexpr int VW = NR == 2 ? 4 : 2, PASS = VW * kThreads / D;
+    typedef float vw_t __attribute__((ext_vector_type(VW)));
     constexpr int PITCH = D + 4;
     constexpr int64_t TB = kv4_tile_bytes(D);
     using P = Parts<D, ROWS>;
-    __shared__ uint32_t scratch[4], before[257];
-    __shared__ float ms[4][ROWS], ls[2][ROWS];
-    __shared__ float acc[2][ROWS * PITCH];
+    __shared__ uint32_t scratch[kWaves], before[kThreads + 1];
+    __shared__ float ms[kWaves][ROWS], ls[kWaves][ROWS];
+    __shared__ __align__(16) float acc[kWaves][PASS * PITCH];
     __shared__ u32x4 qs[NR][NW][64];
     __shared__ int last;
 
@@ -280,6 +295,7 @@ void kv4_attn_kernel(AttnArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Shares sh(a, before, scratch);
     const uint32_t wg = blockIdx.x;
+    if (wg >= sh.wgs) return;
     uint32_t at = __builtin_amdgcn_readfirstlane(sh.begin_of(wg));
     const uint32_t end = __builtin_amdgcn_readfirstlane(sh.begin_of(wg + 1));
     if (at >= end) return;
@@ -315,7 +331,7 @@ void kv4_attn_kernel(AttnArgs a) {
         }
         if (at <= item_rounds) continue;  // the share ends before the item's rounds
 
-        // ---- the wave's tiles: 4 r + wave for r0 <= r < r1, those that begin before len
+        // ---- the wave's tiles: 8 r + wave for r0 <= r < r1, those that begin before len
         const uint32_t tiles = (len + kKvTile - 1) / kKvTile;
         // Table entries are read through the scalar cache, an iteration ahead: a
         // vector load would wait in line behind the codes.  A tile without a
@@ -338,16 +354,16 @@ void kv4_attn_kernel(AttnArgs a) {
             for (int i = 0; i < 4; ++i) meta[i] = load16(tile + 32 * D + i * 16 + meta_offset);
         };
         auto load_v = [&](GlobalBytes tile) { load_codes<D>(vc, tile + 16 * D, lane_offset); };
-        uint32_t t = 4 * r0 + wave;
-        const uint32_t t_end = 4 * r1 < tiles ? 4 * r1 : tiles;
+        uint32_t t = kWaves * r0 + wave;
+        const uint32_t t_end = kWaves * r1 < tiles ? kWaves * r1 : tiles;
         GlobalBytes tile = tile_at(t, t < t_end ? entry_of(t) : -1, here);
-        int32_t entry = t + 4 < t_end ? entry_of(t + 4) : -1;
+        int32_t entry = t + kWaves < t_end ? entry_of(t + kWaves) : -1;
         load_k(tile);
         load_meta(tile);
         load_v(tile);
 
         // The queries as the matrix cores take them, in LDS (the registers hold
-        // sums and codes); wave n % 4 brings row tile n.
+        // sums and codes); wave n brings row tile n.
         float sum_q[NR], off_q[NR];
         int limit[NR];                    // last visible position of the lane's row
 #pragma unroll
@@ -383,12 +399,12 @@ void kv4_attn_kernel(AttnArgs a) {
             for (int k = 0; k < NT; ++k) o[n][k] = float4_t{0.f, 0.f, 0.f, 0.f};
         }
 
-        for (; t < t_end; t += 4) {
+        for (; t < t_end; t += kWaves) {
             // each piece of the next tile is fetched as soon as its registers
             // are free (after the last tile, of that one again)
             bool next_here = here;
-            if (t + 4 < t_end) tile = tile_at(t + 4, entry, next_here);
-            if (t + 8 < t_end) entry = entry_of(t + 8);
+            if (t + kWaves < t_end) tile = tile_at(t + kWaves, entry, next_here);
+            if (t + 2 * kWaves < t_end) entry = entry_of(t + 2 * kWaves);
             {
                 float4_t s[NR][2];
 #pragma unroll
@@ -407,29 +423,27 @@ void kv4_attn_kernel(AttnArgs a) {
                 const int key0 = (int)(t * kKvTile) + 4 * g;
                 const bool edge = !here || (int)(t * kKvTile) + kKvTile - 1 > (int)len - a.q_len;
                 u32x4 p[NR], zrow = meta[3];
-                float x[NR][8];
-#pragma unroll
-                for (int n = 0; n < NR; ++n)
+                if (edge) {               // no zero-points of positions that were never written
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        x[n][i] = fmaf(-meta_f32<BF>(meta[1], i), sum_q[n], s[n][i / 4][i % 4]) *
-                                  meta_f32<BF>(meta[0], i);
-                if (edge) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int key = here ? key0 + 16 * (i / 4) + i % 4 : INT32_MAX;
-#pragma unroll
-                        for (int n = 0; n < NR; ++n)
-                            if (key > limit[n]) x[n][i] = -__builtin_inff();
-                        // no zero-points of positions that were never written
-                        if (key >= (int)len) zrow[i / 2] &= i & 1 ? 0xFFFFu : 0xFFFF0000u;
-                    }
+                        if (!here || key0 + 16 * (i / 4) + i % 4 >= (int)len)
+                            zrow[i / 2] &= i & 1 ? 0xFFFFu : 0xFFFF0000u;
                 }
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
-                    float top = m[n];
+                    const int seen = (here ? limit[n] : -1) - key0;
+                    float x[8], top = m[n];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[n][i]);
+                    for (int i = 0; i < 8; ++i)
+                        x[i] = fmaf(-meta_f32<BF>(meta[1], i), sum_q[n], s[n][i / 4][i % 4]) *
+                               meta_f32<BF>(meta[0], i);
+                    if (edge) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (16 * (i / 4) + i % 4 > seen) x[i] = -__builtin_inff();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
                     top = max_over_groups(top);
                     if (__any(top > m[n])) {
                         const float f =
@@ -443,24 +457,18 @@ void kv4_attn_kernel(AttnArgs a) {
                     const float base = m[n] == -__builtin_inff() ? 0.f : m[n] * a.scale2;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float e = __builtin_amdgcn_exp2f(fmaf(x[n][i], a.scale2, -base));
+                        const float e = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale2, -base));
                         l[n] += e;
-                        x[n][i] = e * meta_f32<BF>(meta[2], i);
+                        x[i] = e * meta_f32<BF>(meta[2], i);
                     }
-                }
-                if (edge) {               // a hidden value's scale may be anything
+                    if (edge) {           // a hidden value's scale may be anything
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int key = here ? key0 + 16 * (i / 4) + i % 4 : INT32_MAX;
-#pragma unroll
-                        for (int n = 0; n < NR; ++n)
-                            if (key > limit[n]) x[n][i] = 0.f;
+                        for (int i = 0; i < 8; ++i)
+                            if (16 * (i / 4) + i % 4 > seen) x[i] = 0.f;
                     }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[n][i] = round_out2<BF>(x[2 * i], x[2 * i + 1]);
                 }
-#pragma unroll
-                for (int n = 0; n < NR; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p[n][i] = round_out2<BF>(x[n][2 * i], x[n][2 * i + 1]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) zrow[i] = c == 0 ? zrow[i] : off_row;
                 load_meta(tile);
@@ -494,134 +502,102 @@ void kv4_attn_kernel(AttnArgs a) {
                 o[n][w] -= ca;
                 o[n][NW + w] -= cb;
             }
-            m[n] *= a.scale2;
-            if (g == 0) ms[wave][n * 16 + c] = m[n];
-        }
-        __syncthreads();
-        // ---- the four waves' sums under a common maximum, added in a tree
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            const int r = n * 16 + c;
-            const float all = fmaxf(fmaxf(ms[0][r], ms[1][r]), fmaxf(ms[2][r], ms[3][r]));
-            const float f = weight_of(m[n], all);
-            m[n] = all;
-            l[n] *= f;
-#pragma unroll
-            for (int k = 0; k < NT; ++k) o[n][k] *= f;
-        }
-#pragma unroll
-        for (int step = 2; step >= 1; --step) {
-            if (wave >= step && wave < 2 * step) {
-#pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    float* dst = acc[wave - step] + (n * 16 + c) * PITCH + 4 * g;
-#pragma unroll
-                    for (int k = 0; k < NT; ++k) *reinterpret_cast<float4_t*>(dst + 16 * k) = o[n][k];
-                    if (g == 0) ls[wave - step][n * 16 + c] = l[n];
-                }
+            if (g == 0) {
+                ms[wave][n * 16 + c] = m[n] * a.scale2;
+                ls[wave][n * 16 + c] = l[n];
             }
-            __syncthreads();
-            if (wave < step) {
-#pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    const float* src = acc[wave] + (n * 16 + c) * PITCH + 4 * g;
-#pragma unroll
-                    for (int k = 0; k < NT; ++k) o[n][k] += *reinterpret_cast<const float4_t*>(src + 16 * k);
-                    l[n] += ls[wave][n * 16 + c];
-                }
-            }
-            __syncthreads();
         }
-
+        // ---- the waves' sums under a common maximum, PASS rows at a time
         const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
         const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_end - 1);
-        if (first == final) {
-            if (wave == 0) {
+        float* const slot = P::at(a.parts, wg, first);
+        for (int row0 = 0; row0 < rows_here; row0 += PASS) {
+            if (row0 > 0) lds_barrier();            // the rows before are read
 #pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    if (n * 16 + c >= rows_here) continue;
-                    uint16_t* dst = out_row<D>(a, this_b, h, rb * ROWS + n * 16 + c) + 4 * g;
-                    const float inv = l[n] == 0.f ? 0.f : 1.f / l[n];
+            for (int n = 0; n < NR; ++n) {
+                const int r = n * 16 + c - row0;
+                if (r < 0 || r >= PASS) continue;
+                float* dst = acc[wave] + r * PITCH + 4 * g;
 #pragma unroll
-                    for (int k = 0; k < NT; ++k) {
-                        const float4_t v = o[n][k] * inv;
-                        *reinterpret_cast<u32x2*>(dst + 16 * k) =
-                            u32x2{round_out2<BF>(v[0], v[1]), round_out2<BF>(v[2], v[3])};
-                    }
-                }
+                for (int k = 0; k < NT; ++k) *reinterpret_cast<float4_t*>(dst + 16 * k) = o[n][k];
             }
-        } else {
-            // Where the last workgroup adds the parts, they and the counters
-            // are touched only by agent-scope atomic accesses, which pass the
-            // per-XCD L2, and the stores complete before the arrival is counted.
-            auto store2 = [](float* p, float x, float y) {
-                __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, float2_t{x, y}),
-                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            };
-            if (wave == 0) {
-                float* slot = P::at(a.parts, wg, first);
+            lds_barrier();
+            const int r = tid / (D / VW), d = tid % (D / VW) * VW, row = row0 + r;
+            if (row >= rows_here) continue;         // PASS * D / VW == kThreads
+            float top = ms[0][row];
 #pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    const int r = n * 16 + c;
-                    if (r >= rows_here) continue;
-                    float* dst = slot + r * D + 4 * g;
+            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ms[w][row]);
+            float sum = 0.f;
+            vw_t v = 0.f;
 #pragma unroll
-                    for (int k = 0; k < NT; ++k) {
-                        if (a.counters) {
-                            store2(dst + 16 * k, o[n][k][0], o[n][k][1]);
-                            store2(dst + 16 * k + 2, o[n][k][2], o[n][k][3]);
-                        } else {
-                            *reinterpret_cast<float4_t*>(dst + 16 * k) = o[n][k];
-                        }
-                    }
-                    if (g == 0) {
-                        __hip_atomic_store(slot + ROWS * D + r, m[n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        __hip_atomic_store(slot + ROWS * (D + 1) + r, l[n], __ATOMIC_RELAXED,
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = weight_of(ms[w][row], top);
+                sum = fmaf(ls[w][row], f, sum);
+                v += *reinterpret_cast<const vw_t*>(acc[w] + r * PITCH + d) * f;
+            }
+            if (first == final) {
+                v *= sum == 0.f ? 0.f : 1.f / sum;
+                uint16_t* dst = out_row<D>(a, this_b, h, rb * ROWS + row) + d;
+#pragma unroll
+                for (int i = 0; i < VW; i += 2)
+                    *reinterpret_cast<uint32_t*>(dst + i) = round_out2<BF>(v[i], v[i + 1]);
+            } else {
+                // Where the last workgroup adds the parts, they and the counters
+                // are touched only by agent-scope atomic accesses, which pass the
+                // per-XCD L2, and the stores complete before the arrival is counted.
+                if (a.counters) {
+#pragma unroll
+                    for (int i = 0; i < VW; i += 2)
+                        __hip_atomic_store(reinterpret_cast<uint64_t*>(slot + row * D + d + i),
+                                           __builtin_bit_cast(uint64_t, float2_t{v[i], v[i + 1]}), __ATOMIC_RELAXED,
                                            __HIP_MEMORY_SCOPE_AGENT);
-                    }
+                } else {
+                    *reinterpret_cast<vw_t*>(slot + row * D + d) = v;
                 }
-            }
-            if (a.counters) {
-                if (wave == 0) {
-                    __builtin_amdgcn_s_waitcnt(0);
-                    if (lane == 0)
-                        last = __hip_atomic_fetch_add(&a.counters[first], 1u, __ATOMIC_RELAXED,
-                                                      __HIP_MEMORY_SCOPE_AGENT) == final - first;
+                if (d == 0) {
+                    __hip_atomic_store(slot + ROWS * D + row, top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_store(slot + ROWS * (D + 1) + row, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 }
-                __syncthreads();
-                if (last) {
-                    auto load1 = [](const float* p) {
-                        return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    };
-                    auto load2 = [](const float* p) {
-                        return __builtin_bit_cast(float2_t,
-                                                  __hip_atomic_load(reinterpret_cast<const uint64_t*>(p),
-                                                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-                    };
-                    for (int i = 2 * tid; i < rows_here * D; i += 512) {
-                        const float2_t v = join_parts<D, ROWS>(a.parts, first, final, i / D, i % D, load2, load1);
-                        *reinterpret_cast<uint32_t*>(out_row<D>(a, this_b, h, rb * ROWS + i / D) + i % D) =
-                            round_out2<BF>(v[0], v[1]);
-                    }
-                    if (tid == 0)
-                        __hip_atomic_store(&a.counters[first], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
-                __syncthreads();          // `last` is read before the next item sets it
             }
         }
+        if (first != final && a.counters) {
+            __builtin_amdgcn_s_waitcnt(0);          // this thread's stores have completed
+            __syncthreads();
+            if (tid == 0)
+                last = __hip_atomic_fetch_add(&a.counters[first], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                       final - first;
+            __syncthreads();
+            if (last) {
+                auto load1 = [](const float* p) {
+                    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                };
+                auto load2 = [](const float* p) {
+                    return __builtin_bit_cast(float2_t, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p),
+                                                                          __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+                };
+                for (int i = 2 * tid; i < rows_here * D; i += 2 * kThreads) {
+                    const float2_t v = join_parts<D, ROWS>(a.parts, first, final, i / D, i % D, load2, load1);
+                    *reinterpret_cast<uint32_t*>(out_row<D>(a, this_b, h, rb * ROWS + i / D) + i % D) =
+                        round_out2<BF>(v[0], v[1]);
+                }
+                if (tid == 0)
+                    __hip_atomic_store(&a.counters[first], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+        lds_barrier();                    // the sums in LDS and `last` are read before the next item's
     }
 }
 
 // The parts of items that several workgroups share, added by a launch of its
-// own: workgroup (i, y) takes 128 sums, from 128 y on, of item i, its eight
-// groups of 32 threads every eighth part each.
+// own: workgroup (i, y) takes 128 sums, from 128 y on, of item i, its 16
+// groups of 32 threads every sixteenth part each.
 template <bool BF, int D, int NR>
-__global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a) {
-    constexpr int ROWS = 16 * NR, AHEAD = 4;
+__global__ __launch_bounds__(kThreads) void kv4_join_kernel(AttnArgs a) {
+    constexpr int ROWS = 16 * NR, AHEAD = 4, SLICES = kThreads / 32;
     using P = Parts<D, ROWS>;
-    __shared__ uint32_t scratch[4], before[257];
-    __shared__ float4_t vals[8][32];
-    __shared__ float m8[8][32], l8[8][32];
+    __shared__ uint32_t scratch[kWaves], before[kThreads + 1];
+    __shared__ float4_t vals[SLICES][32];
+    __shared__ float m8[SLICES][32], l8[SLICES][32];
     const Shares sh(a, before, scratch);
     const int tid = threadIdx.x, slice = tid >> 5;
     const int b = blockIdx.x / sh.heads;
@@ -638,14 +614,14 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a) {
     if (blockIdx.y * 128 / D >= q_rows - rb * ROWS) return;   // the group of 128 lies in one row but for D = 64
     float top = -__builtin_inff(), sum = 0.f;
     float4_t v = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t w0 = first + slice; w0 <= final; w0 += 8 * AHEAD) {
+    for (uint32_t w0 = first + slice; w0 <= final; w0 += SLICES * AHEAD) {
         float mw[AHEAD], lw[AHEAD];
         float4_t vw[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const uint32_t w = w0 + 8 * k <= final ? w0 + 8 * k : w0;
+            const uint32_t w = w0 + SLICES * k <= final ? w0 + SLICES * k : w0;
             const float* p = P::at(a.parts, w, first);
-            mw[k] = w0 + 8 * k <= final ? p[ROWS * D + r] : -__builtin_inff();
+            mw[k] = w0 + SLICES * k <= final ? p[ROWS * D + r] : -__builtin_inff();
             lw[k] = p[ROWS * (D + 1) + r];
             vw[k] = *reinterpret_cast<const float4_t*>(p + r * D + d);
         }
@@ -670,11 +646,11 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a) {
     if (slice != 0) return;
     float all = -__builtin_inff();
 #pragma unroll
-    for (int k = 0; k < 8; ++k) all = fmaxf(all, m8[k][tid]);
+    for (int k = 0; k < SLICES; ++k) all = fmaxf(all, m8[k][tid]);
     sum = 0.f;
     v = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < SLICES; ++k) {
         const float e = weight_of(m8[k][tid], all);
         sum = fmaf(l8[k][tid], e, sum);
         v += vals[k][tid] * e;
@@ -687,8 +663,8 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a) {
 
 // Rows per workgroup (16 or 32) and the blocks of them that q_rows need.
 int row_tiles(int q_rows) { return q_rows <= 16 ? 1 : 2; }
-// Workgroups that a compute unit holds: the launch bounds above.
-int wgs_per_cu(int D, int nr) { return D <= 128 ? (nr == 1 ? 4 : 2) : nr == 1 ? 2 : 1; }
+// Workgroups that a compute unit holds on its four SIMDs.
+int wgs_per_cu(int D, int nr) { return waves_per_simd(D, nr) * 4 / kWaves; }
 
 }  // namespace
 
@@ -733,9 +709,9 @@ int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride,
     auto go = [&](auto d, auto n, auto bf) {
         constexpr int D = decltype(d)::value, NR = decltype(n)::value;
         constexpr bool BF = decltype(bf)::value;
-        const int rc = launch(kv4_attn_kernel<BF, D, NR>, grid, dim3(256), 0, s, a);
+        const int rc = launch(kv4_attn_kernel<BF, D, NR>, grid, dim3(kThreads), 0, s, a);
         if (rc || !join) return rc;
-        return launch(kv4_join_kernel<BF, D, NR>, join_grid, dim3(256), 0, s, a);
+        return launch(kv4_join_kernel<BF, D, NR>, join_grid, dim3(kThreads), 0, s, a);
     };
     auto by_rows = [&](auto d, auto bf) {
         return nr == 1 ? go(d, std::integral_constant<int, 1>{}, bf) : go(d, std::integral_constant<int, 2>{}, bf);
