@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kRoundKeys = kKvTile * kWaves;   // keys of one round: a tile for each wave
-constexpr uint32_t kItemCost = 2;        // what beginning and ending an item costs, in rounds
+constexpr uint32_t kItemCost = 3;        // what beginning and ending an item costs, in rounds
 constexpr uint32_t kLeastRounds = 4;     // rounds of an item that one workgroup takes before a second helps
 constexpr int kMostWgs = 1024;           // workgroups of a launch, at most
 
@@ -94,14 +94,34 @@ __device__ __forceinline__ uint32_t code_word(const u32x4* x, int u, int w) {
     if constexpr (D == 64) return x[0][2 * u + w];
     else return x[u * (D / 128) + w / 4][w % 4];
 }
-typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
-__device__ __forceinline__ u32x4 load16(GlobalBytes p) {
-    return *(const __attribute__((address_space(1))) u32x4*)p;
+
+// Reads of N 16-byte pieces, `step` bytes apart, from LDS that direct loads
+// fill, waited for in the same statement.  (As statements of the language the
+// compiler would put a wait for every direct load in flight before them.)
+template <int N, int STEP>
+__device__ __forceinline__ void lds_read(u32x4* x, uint32_t at) {
+    if constexpr (N == 1) {
+        asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0]) : "v"(at) : "memory");
+    } else if constexpr (N == 2) {
+        asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:%3\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(x[0]), "=&v"(x[1]) : "v"(at), "i"(STEP) : "memory");
+    } else {
+        static_assert(N == 4, "one, two or four pieces");
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:%5\n\tds_read_b128 %2, %4 offset:%6\n\t"
+                     "ds_read_b128 %3, %4 offset:%7\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+                     : "v"(at), "i"(STEP), "i"(2 * STEP), "i"(3 * STEP) : "memory");
+    }
 }
-template <int D>
-__device__ __forceinline__ void load_codes(u32x4* x, GlobalBytes codes, uint32_t lane_offset) {
-#pragma unroll
-    for (int p = 0; p < kPieces<D>; ++p) x[p] = load16(codes + p * 1024 + lane_offset);
+typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
+// 16 (or 4) bytes a lane from its p straight to LDS: lane i's at dst + 16 i (4 i).
+typedef const __attribute__((address_space(1))) void* GlobalVoid;
+typedef __attribute__((address_space(3))) void* LdsVoid;
+__device__ __forceinline__ void direct_load16(GlobalBytes p, uint32_t dst) {
+    __builtin_amdgcn_global_load_lds((GlobalVoid)p, (LdsVoid)(uintptr_t)dst, 16, 0, 0);
+}
+__device__ __forceinline__ void direct_load4(GlobalBytes p, uint32_t dst) {
+    __builtin_amdgcn_global_load_lds((GlobalVoid)p, (LdsVoid)(uintptr_t)dst, 4, 0, 0);
 }
 
 // Value i (0..7) of eight packed 16-bit floats.
@@ -110,6 +130,10 @@ __device__ __forceinline__ float meta_f32(const u32x4& m, int i) {
     const uint32_t w = m[i / 2];
     if constexpr (BF) return __builtin_bit_cast(float, i & 1 ? w & 0xFFFF0000u : w << 16);
     else return scale_f32<false>(i & 1 ? w >> 16 : w & 0xFFFFu);
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
 // A pointer to memory that no kernel writes while this one runs, as the scalar
@@ -285,9 +309,15 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
     constexpr int PITCH = D + 4;
     constexpr int64_t TB = kv4_tile_bytes(D);
     using P = Parts<D, ROWS>;
+    // Each wave keeps RING tiles in LDS, fetched by direct loads: what it
+    // multiplies and RING - 1 on the way, without a register.  The same memory
+    // takes the waves' sums once an item's tiles are done.
+    constexpr int RING = D == 64 ? 4 : 2, LOADS = 2 * kPieces<D> + 1;
+    constexpr int kRingBytes = kWaves * RING * (int)TB, kSumBytes = kWaves * PASS * PITCH * 4;
+    __shared__ __align__(1024) uint8_t pool[kRingBytes > kSumBytes ? kRingBytes : kSumBytes];
+    float(*const acc)[PASS * PITCH] = reinterpret_cast<float(*)[PASS * PITCH]>(pool);
     __shared__ uint32_t scratch[kWaves], before[kThreads + 1];
-    __shared__ float ms[kWaves][ROWS], ls[kWaves][ROWS];
-    __shared__ __align__(16) float acc[kWaves][PASS * PITCH];
+    __shared__ float ms[kWaves][ROWS], ls[kWaves][ROWS], fs[kWaves][ROWS], tops[ROWS];
     __shared__ u32x4 qs[NR][NW][64];
     __shared__ int last;
 
@@ -302,8 +332,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
     uint32_t seq_start;                   // units (of all heads) before sequence b
     int b = sh.sequence(at, seq_start);
 
-    // the lane's place in a tile: 32-bit offsets from an address that all lanes share
-    const uint32_t lane_offset = lane * 16, meta_offset = g * 64;
+    const uint32_t ring = lds_address(pool) + wave * RING * (uint32_t)TB;
+    const uint32_t q_at = lds_address(qs) + lane * 16;
     const Magic mk = magics<BF>(0), mv = magics<BF>(0x80000000u);
     // Row 0 of a further operand beside the values' codes takes the values'
     // zero-points, row 1 and 2 the offsets of the low and high dims' codes: one
@@ -336,7 +366,6 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
         // Table entries are read through the scalar cache, an iteration ahead: a
         // vector load would wait in line behind the codes.  A tile without a
         // page is some memory of the cache, and every key of it hidden.
-        bool here = true;
         const uint32_t page_tiles = (uint32_t)a.cache.tiles;
         const auto* row = as_constant(a.cache.table) + this_b * a.cache.table_stride;
         auto entry_of = [&](uint32_t t) { return row[t / page_tiles]; };
@@ -347,20 +376,26 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             asm("" : "+s"(p));            // in scalar registers, the lanes' offsets beside it
             return (GlobalBytes)(uintptr_t)p;
         };
-        u32x4 kc[kPieces<D>], vc[kPieces<D>], meta[4];        // meta: k scale, k zero, v scale, v zero
-        auto load_k = [&](GlobalBytes tile) { load_codes<D>(kc, tile, lane_offset); };
-        auto load_meta = [&](GlobalBytes tile) {
+        auto fetch = [&](GlobalBytes tile, uint32_t slot) {
+            const uint32_t dst = __builtin_amdgcn_readfirstlane(ring + slot * (uint32_t)TB);
+            const uint32_t off = lane * 16;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) meta[i] = load16(tile + 32 * D + i * 16 + meta_offset);
+            for (int p = 0; p < 2 * kPieces<D>; ++p) direct_load16(tile + p * 1024 + off, dst + p * 1024);
+            direct_load4(tile + 32 * D + lane * 4, dst + 32 * D);
         };
-        auto load_v = [&](GlobalBytes tile) { load_codes<D>(vc, tile + 16 * D, lane_offset); };
         uint32_t t = kWaves * r0 + wave;
         const uint32_t t_end = kWaves * r1 < tiles ? kWaves * r1 : tiles;
-        GlobalBytes tile = tile_at(t, t < t_end ? entry_of(t) : -1, here);
-        int32_t entry = t + kWaves < t_end ? entry_of(t + kWaves) : -1;
-        load_k(tile);
-        load_meta(tile);
-        load_v(tile);
+        // Tiles are fetched RING - 1 ahead, and past the end some memory of the
+        // cache, so that the number of loads in flight is always the same.
+        bool found[RING];
+        int32_t entry;
+#pragma unroll
+        for (int i = 0; i < RING; ++i) {
+            const uint32_t ti = t + i * kWaves;
+            entry = ti < t_end ? entry_of(ti) : -1;
+            fetch(tile_at(ti, entry, found[i]), i);
+        }
+        entry = t + RING * kWaves < t_end ? entry_of(t + RING * kWaves) : -1;
 
         // The queries as the matrix cores take them, in LDS (the registers hold
         // sums and codes); wave n brings row tile n.
@@ -387,7 +422,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             sum_q[n] = sa + sb;
             off_q[n] = sa * kOffA<BF> + sb * kOffB<BF>;
         }
-        __syncthreads();
+        lds_barrier();
         float4_t o[NR][NT], osum[NR];     // osum: rows 0..2 of the further operand
         float m[NR], l[NR];               // maximum of scale-free scores; sum of weights
 #pragma unroll
@@ -399,26 +434,35 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             for (int k = 0; k < NT; ++k) o[n][k] = float4_t{0.f, 0.f, 0.f, 0.f};
         }
 
-        for (; t < t_end; t += kWaves) {
-            // each piece of the next tile is fetched as soon as its registers
-            // are free (after the last tile, of that one again)
-            bool next_here = here;
-            if (t + kWaves < t_end) tile = tile_at(t + kWaves, entry, next_here);
-            if (t + 2 * kWaves < t_end) entry = entry_of(t + 2 * kWaves);
+        for (uint32_t slot = 0; t < t_end; t += kWaves, slot = (slot + 1) % RING) {
+            const bool here = found[0];
+            const uint32_t buf = ring + slot * (uint32_t)TB;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"i"((RING - 1) * LOADS) : "memory");     // this tile has landed
             {
                 float4_t s[NR][2];
+                u32x4 kc[kPieces<D>];
+                lds_read<kPieces<D>, 1024>(kc, buf + lane * 16);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int n = 0; n < NR; ++n) s[n][u] = float4_t{-off_q[n], -off_q[n], -off_q[n], -off_q[n]};
+                constexpr int QW = NW < 4 ? NW : 4;         // words of queries at a time
 #pragma unroll
-                    for (int w = 0; w < NW; ++w) {
-                        const u32x4 kf = code_pairs<BF>(code_word<D>(kc, u, w), mk);
+                for (int w0 = 0; w0 < NW; w0 += QW) {
+                    u32x4 qf[NR][QW];
 #pragma unroll
-                        for (int n = 0; n < NR; ++n) s[n][u] = mfma16<BF>(kf, qs[n][w][lane], s[n][u]);
-                    }
+                    for (int n = 0; n < NR; ++n) lds_read<QW, 1024>(qf[n], q_at + (n * NW + w0) * 1024);
+#pragma unroll
+                    for (int w = 0; w < QW; ++w)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const u32x4 kf = code_pairs<BF>(code_word<D>(kc, u, w0 + w), mk);
+#pragma unroll
+                            for (int n = 0; n < NR; ++n) s[n][u] = mfma16<BF>(kf, qf[n][w], s[n][u]);
+                        }
                 }
-                load_k(tile);
+                u32x4 meta[4];            // k scale, k zero, v scale, v zero
+                lds_read<4, 16>(meta, buf + 32 * D + g * 64);
                 // slot i of the lane: key 16 (i / 4) + 4 g + i % 4 of the tile
                 const int key0 = (int)(t * kKvTile) + 4 * g;
                 const bool edge = !here || (int)(t * kKvTile) + kKvTile - 1 > (int)len - a.q_len;
@@ -431,13 +475,13 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
                 }
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
-                    const int seen = (here ? limit[n] : -1) - key0;
                     float x[8], top = m[n];
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         x[i] = fmaf(-meta_f32<BF>(meta[1], i), sum_q[n], s[n][i / 4][i % 4]) *
                                meta_f32<BF>(meta[0], i);
                     if (edge) {
+                        const int seen = (here ? limit[n] : -1) - key0;
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             if (16 * (i / 4) + i % 4 > seen) x[i] = -__builtin_inff();
@@ -462,6 +506,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
                         x[i] = e * meta_f32<BF>(meta[2], i);
                     }
                     if (edge) {           // a hidden value's scale may be anything
+                        const int seen = (here ? limit[n] : -1) - key0;
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             if (16 * (i / 4) + i % 4 > seen) x[i] = 0.f;
@@ -471,7 +516,14 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) zrow[i] = c == 0 ? zrow[i] : off_row;
-                load_meta(tile);
+                u32x4 vc[kPieces<D>];
+                lds_read<kPieces<D>, 1024>(vc, buf + 16 * D + lane * 16);
+                // everything of the tile is in registers: its place takes another
+#pragma unroll
+                for (int i = 0; i + 1 < RING; ++i) found[i] = found[i + 1];
+                fetch(tile_at(t + RING * kWaves, entry, found[RING - 1]), slot);
+                if (t + (RING + 1) * kWaves < t_end) entry = entry_of(t + (RING + 1) * kWaves);
+                else entry = -1;
 #pragma unroll
                 for (int n = 0; n < NR; ++n) osum[n] = mfma16<BF>(zrow, p[n], osum[n]);
 #pragma unroll
@@ -485,10 +537,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
                         o[n][NW + w] = mfma16<BF>(hi, p[n], o[n][NW + w]);
                     }
                 }
-                load_v(tile);
             }
-            here = next_here;
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing lands in the ring any more
 
         // ---- the wave's sums: offsets and zero-points leave
 #pragma unroll
@@ -511,6 +562,16 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
         const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
         const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_end - 1);
         float* const slot = P::at(a.parts, wg, first);
+        lds_barrier();                    // the tiles are read; maxima and sums are there
+        // what each wave's sums weigh under the common maximum
+        if (tid < kWaves * ROWS) {
+            const int w = tid / ROWS, r = tid % ROWS;
+            float top = ms[0][r];
+#pragma unroll
+            for (int i = 1; i < kWaves; ++i) top = fmaxf(top, ms[i][r]);
+            fs[w][r] = weight_of(ms[w][r], top);
+            if (w == 0) tops[r] = top;
+        }
         for (int row0 = 0; row0 < rows_here; row0 += PASS) {
             if (row0 > 0) lds_barrier();            // the rows before are read
 #pragma unroll
@@ -524,14 +585,11 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             lds_barrier();
             const int r = tid / (D / VW), d = tid % (D / VW) * VW, row = row0 + r;
             if (row >= rows_here) continue;         // PASS * D / VW == kThreads
-            float top = ms[0][row];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ms[w][row]);
             float sum = 0.f;
             vw_t v = 0.f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const float f = weight_of(ms[w][row], top);
+                const float f = fs[w][row];
                 sum = fmaf(ls[w][row], f, sum);
                 v += *reinterpret_cast<const vw_t*>(acc[w] + r * PITCH + d) * f;
             }
@@ -555,7 +613,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
                     *reinterpret_cast<vw_t*>(slot + row * D + d) = v;
                 }
                 if (d == 0) {
-                    __hip_atomic_store(slot + ROWS * D + row, top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_store(slot + ROWS * D + row, tops[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                     __hip_atomic_store(slot + ROWS * (D + 1) + row, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 }
             }
