@@ -389,12 +389,18 @@ int tf_kv4_attention(const tf_kv4_cache* cache, const void* Q, int64_t q_stride,
  * zeros.  cu_q and cu_k: int32 [batch + 1].  Q, K, V strided as above, O
  * [tokens_q, q_heads, head_dim] contiguous.  Scores and sums in fp32, softmax
  * weights rounded to dtype for the matrix cores.  Rows of O that no sequence
- * owns are not written.
+ * owns are not written.  workspace: NULL, or at least
+ * tf_prompt_attention_workspace_bytes(...) bytes (may be 0), 16-byte aligned, no
+ * initial value: few queries on many keys are then split over the keys too,
+ * their parts added in a fixed order.  Calls that may run concurrently must not
+ * share one.
  */
+int64_t tf_prompt_attention_workspace_bytes(int64_t batch, int64_t tokens_q, int64_t tokens_k, int q_heads,
+                                            int kv_heads, int head_dim);
 int tf_prompt_attention(int dtype, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
                         int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t tokens_q,
                         int64_t tokens_k, int q_heads, int kv_heads, int head_dim, float scale, int causal, void* O,
-                        void* stream);
+                        void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,8 @@ int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride,
 int launch_prompt_attention(bool bf, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                             int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int64_t batch,
                             int64_t tokens_q, int64_t tokens_k, int q_heads, int kv_heads, int D, float scale,
-                            bool causal, void* out, hipStream_t s);
+                            bool causal, void* out, void* ws, hipStream_t s);
+int64_t prompt_attention_workspace_bytes(int64_t batch, int64_t tokens_q, int64_t tokens_k, int q_heads, int D);
 }  // namespace tf
 
 namespace {
@@ -140,26 +141,35 @@ int tf_kv4_attention(const tf_kv4_cache* cache, const void* Q, int64_t q_stride,
                                     static_cast<hipStream_t>(stream));
 }
 
-int tf_prompt_attention(int dtype, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
-                        int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t tokens_q,
-                        int64_t tokens_k, int q_heads, int kv_heads, int head_dim, float scale, int causal, void* O,
-                        void* stream) {
-    if (!Q || !K || !V || !cu_q || !cu_k || !O) return TF_ERR_NULL;
-    if (bad_dtype(dtype) || bad_scale(scale)) return TF_ERR_ARG;
+int64_t tf_prompt_attention_workspace_bytes(int64_t batch, int64_t tokens_q, int64_t tokens_k, int q_heads,
+                                            int kv_heads, int head_dim) {
     if (bad_head_dim(head_dim) || bad_heads(q_heads) || bad_heads(kv_heads) || q_heads % kv_heads != 0)
         return TF_ERR_SHAPE;
     if (batch < 1 || batch > TF_MAX_BATCH || tokens_q < 1 || tokens_q > TF_MAX_M || tokens_k < 1 ||
         tokens_k > TF_MAX_M)
         return TF_ERR_SHAPE;
+    return tf::prompt_attention_workspace_bytes(batch, tokens_q, tokens_k, q_heads, head_dim);
+}
+
+int tf_prompt_attention(int dtype, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
+                        int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int64_t batch, int64_t tokens_q,
+                        int64_t tokens_k, int q_heads, int kv_heads, int head_dim, float scale, int causal, void* O,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    if (!Q || !K || !V || !cu_q || !cu_k || !O) return TF_ERR_NULL;
+    if (bad_dtype(dtype) || bad_scale(scale)) return TF_ERR_ARG;
+    const int64_t need =
+        tf_prompt_attention_workspace_bytes(batch, tokens_q, tokens_k, q_heads, kv_heads, head_dim);
+    if (need < 0) return (int)need;
     if (bad_stride(q_stride, q_heads, head_dim) || bad_stride(k_stride, kv_heads, head_dim) ||
         bad_stride(v_stride, kv_heads, head_dim))
         return TF_ERR_SHAPE;
     if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(O) || misaligned(cu_q, 4) ||
-        misaligned(cu_k, 4))
+        misaligned(cu_k, 4) || misaligned(workspace))
         return TF_ERR_ALIGN;
+    if (workspace && (int64_t)workspace_bytes < need) return TF_ERR_ARG;
     return tf::launch_prompt_attention(dtype == TF_BF16, Q, q_stride, K, k_stride, V, v_stride, cu_q, cu_k, batch,
                                        tokens_q, tokens_k, q_heads, kv_heads, head_dim, scale, causal != 0, O,
-                                       static_cast<hipStream_t>(stream));
+                                       need > 0 ? workspace : nullptr, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -21,6 +21,7 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 4;
 constexpr int kBM = 32 * kWaves;       // queries of a workgroup
 constexpr int kBN = 64;                // keys of a step
+constexpr int kSizedForCus = 256, kMostSplits = 16;
 
 struct PromptArgs {
     const uint16_t *q, *k, *v;
@@ -31,6 +32,9 @@ struct PromptArgs {
     float scale2;
     int causal;
     uint16_t* out;
+    int splits;                        // parts that each block's keys are split into
+    float* parts;                      // splits > 1: [part][block * q_heads + head][kBM] rows of D sums, maxima, sums
+    int64_t part_stride;               // floats of one part
 };
 
 template <bool BF>
@@ -65,6 +69,74 @@ __device__ __forceinline__ u32x2 lds_read_tr16(const uint16_t* p) {
     return __builtin_bit_cast(u32x2, v);
 }
 
+// Which sequence, block of queries and head a workgroup takes: slot counts
+// (block, head) pairs, heads fastest, so that neighbouring workgroups
+// (neighbouring XCDs) take different key/value heads; the last blocks of the
+// packed sequences, the longest of each, go first.  Offsets that leave the
+// tensors or run backwards make an empty sequence.
+struct Block {
+    int sequence = -1, block = 0, n_q = 0, n_k = 0, hq = 0, hk = 0, steps = 0, splits = 1;
+    int64_t q_start = 0, k_start = 0;
+
+    static __device__ __forceinline__ int span(const int32_t* cu, int b, int64_t tokens, int64_t& start) {
+        start = cu[b];
+        const int64_t n = (int64_t)cu[b + 1] - start;
+        return start < 0 || n < 0 || start + n > tokens ? 0 : (int)n;
+    }
+    static __device__ __forceinline__ uint32_t blocks_of(const PromptArgs& a, int b) {
+        int64_t s;
+        return (uint32_t)((span(a.cu_q, b, a.tokens_q, s) + kBM - 1) / kBM);
+    }
+    // The first of the block's steps that part s takes.
+    __device__ __forceinline__ int first_step(int s) const { return (int)((int64_t)steps * s / splits); }
+
+    // All threads; wave_total: kWaves words of LDS, before: 64 kWaves + 1.
+    __device__ __forceinline__ Block(const PromptArgs& a, uint32_t slot, uint32_t* wave_total, uint32_t* before) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int seg = (a.batch + 64 * kWaves - 1) / (64 * kWaves);
+        uint32_t sum = 0;
+        for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) sum += blocks_of(a, b);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(sum, d);
+            if (lane >= d) sum += o;
+        }
+        if (lane == 63) wave_total[wave] = sum;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) sum += wave_total[w];
+        before[tid + 1] = sum;
+        if (tid == 0) before[0] = 0;
+        __syncthreads();
+        const uint32_t total = before[64 * kWaves], order = slot / (uint32_t)a.q_heads;
+        if (order >= total) return;
+        const int kv_heads = a.q_heads / a.group, hx = (int)(slot % (uint32_t)a.q_heads);
+        hk = hx % kv_heads;
+        hq = hk * a.group + hx / kv_heads;
+        const uint32_t x = total - 1 - order;
+        int s0 = 0, s1 = 64 * kWaves;
+        while (s1 - s0 > 1) {
+            const int mid = (s0 + s1) >> 1;
+            if (before[mid] <= x) s0 = mid;
+            else s1 = mid;
+        }
+        int b = s0 * seg;
+        uint32_t done = before[s0];
+        for (;; ++b) {
+            const uint32_t n = blocks_of(a, b);
+            if (x < done + n) break;
+            done += n;
+        }
+        sequence = __builtin_amdgcn_readfirstlane(b);
+        block = __builtin_amdgcn_readfirstlane((int)(x - done));
+        n_q = span(a.cu_q, sequence, a.tokens_q, q_start);
+        n_k = span(a.cu_k, sequence, a.tokens_k, k_start);
+        const int q_end = (block + 1) * kBM < n_q ? (block + 1) * kBM : n_q;
+        const int keys = a.causal ? (q_end + n_k - n_q < n_k ? q_end + n_k - n_q : n_k) : n_k;
+        steps = keys > 0 ? (keys + kBN - 1) / kBN : 0;
+        splits = a.splits;
+    }
+};
+
 template <bool BF, int D>
 __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_kernel(PromptArgs a) {
     constexpr int CH = D / 8;             // 16-byte chunks of a row
@@ -78,73 +150,19 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-    // ---- which sequence, block of queries and head
-    auto span = [&](const int32_t* cu, int b, int64_t tokens, int64_t& start) {
-        start = cu[b];
-        const int64_t n = (int64_t)cu[b + 1] - start;
-        return start < 0 || n < 0 || start + n > tokens ? 0 : (int)n;
-    };
-    auto blocks_of = [&](int b) {
-        int64_t s;
-        return (uint32_t)((span(a.cu_q, b, a.tokens_q, s) + kBM - 1) / kBM);
-    };
-    const int seg = (a.batch + 64 * kWaves - 1) / (64 * kWaves);
-    {
-        uint32_t sum = 0;
-        for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) sum += blocks_of(b);
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(sum, d);
-            if (lane >= d) sum += o;
-        }
-        if (lane == 63) wave_total[wave] = sum;
-        __syncthreads();
-        uint32_t base = 0;
-        for (int w = 0; w < wave; ++w) base += wave_total[w];
-        before[tid + 1] = base + sum;
-        if (tid == 0) before[0] = 0;
-        __syncthreads();
-    }
-    const uint32_t total = before[64 * kWaves];
-    const uint32_t order = blockIdx.x / (uint32_t)a.q_heads;
-    if (order >= total) return;
-    // neighbouring workgroups (neighbouring XCDs) take different key/value
-    // heads; the last, longest blocks go first
-    const int kv_heads = a.q_heads / a.group;
-    const int hx = (int)(blockIdx.x % (uint32_t)a.q_heads);
-    const int hk = hx % kv_heads, hq = hk * a.group + hx / kv_heads;
-    const uint32_t x = total - 1 - order;
-    int b, block;
-    {
-        int s0 = 0, s1 = 64 * kWaves;
-        while (s1 - s0 > 1) {
-            const int mid = (s0 + s1) >> 1;
-            if (before[mid] <= x) s0 = mid;
-            else s1 = mid;
-        }
-        b = s0 * seg;
-        uint32_t done = before[s0];
-        for (;; ++b) {
-            const uint32_t n = blocks_of(b);
-            if (x < done + n) break;
-            done += n;
-        }
-        b = __builtin_amdgcn_readfirstlane(b);
-        block = __builtin_amdgcn_readfirstlane((int)(x - done));
-    }
-    int64_t q_start, k_start;
-    const int n_q = span(a.cu_q, b, a.tokens_q, q_start);
-    const int n_k = span(a.cu_k, b, a.tokens_k, k_start);
-    const int q0 = block * kBM + wave * 32;               // the wave's first query
+    const uint32_t slot = blockIdx.x / (uint32_t)a.splits, split = blockIdx.x % (uint32_t)a.splits;
+    const Block bl(a, slot, wave_total, before);
+    if (bl.sequence < 0) return;
+    const int n_q = bl.n_q, n_k = bl.n_k, past = n_k - n_q, hq = bl.hq, hk = bl.hk;
+    const int64_t q_start = bl.q_start, k_start = bl.k_start;
+    const int q0 = bl.block * kBM + wave * 32;            // the wave's first query
     const int qi = q0 + col;                              // the lane's query
-    const int past = n_k - n_q;
     const int limit = a.causal ? (qi + past < n_k - 1 ? qi + past : n_k - 1) : n_k - 1;
     const int wave_low = a.causal ? (q0 + past < n_k - 1 ? q0 + past : n_k - 1) : n_k - 1;
-    const int q_last = block * kBM + kBM < n_q ? block * kBM + kBM - 1 : n_q - 1;
     const int wave_q_last = q0 + 31 < n_q ? q0 + 31 : n_q - 1;
-    const int wg_keys = a.causal ? (q_last + past + 1 < n_k ? q_last + past + 1 : n_k) : n_k;
     const int wave_keys = q0 >= n_q ? 0 : a.causal ? (wave_q_last + past + 1 < n_k ? wave_q_last + past + 1 : n_k) : n_k;
-    const int steps = wg_keys > 0 ? (wg_keys + kBN - 1) / kBN : 0;
+    // this part's steps of the block's
+    const int step0 = bl.first_step(split), steps = bl.first_step(split + 1);
 
     u32x4 q[KS];
     {
@@ -180,8 +198,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = -__builtin_inff(), l = 0.f;
 
-    if (steps > 0) fetch(0);
-    for (int step = 0; step < steps; ++step) {
+    if (step0 < steps) fetch(step0);
+    for (int step = step0; step < steps; ++step) {
         __builtin_amdgcn_s_waitcnt(0);                    // this wave's part of the tiles is there
         __syncthreads();                                  // everyone's is, and the other buffer is free
         if (step + 1 < steps) fetch(step + 1);
@@ -249,6 +267,21 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
     }
     l += __shfl_xor(l, 32);
     if (qi >= n_q) return;
+    if (a.splits > 1) {
+        // a row's sums as they are, its maximum and its sum of weights
+        float* part = a.parts + split * a.part_stride + (int64_t)slot * kBM * (D + 2);
+        float* dst = part + (wave * 32 + col) * D + 4 * half;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4_t*>(dst + 32 * t + 2 * i) = float4_t{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+        if (half == 0) {
+            part[kBM * D + wave * 32 + col] = m * a.scale2;
+            part[kBM * (D + 1) + wave * 32 + col] = l;
+        }
+        return;
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint16_t* dst = a.out + ((q_start + qi) * a.q_heads + hq) * (int64_t)D + 4 * half;
 #pragma unroll
@@ -260,23 +293,74 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
                       round_out2<BF>(o[t][i + 2] * inv, o[t][i + 3] * inv)};
 }
 
+// Adds the parts of one block of queries in their order: workgroup (slot, y)
+// takes the block's rows 8 y .. 8 y + 7, a row every 32 threads.
+template <bool BF, int D>
+__global__ __launch_bounds__(64 * kWaves) void prompt_join_kernel(PromptArgs a) {
+    __shared__ uint32_t wave_total[kWaves], before[64 * kWaves + 1];
+    const Block bl(a, blockIdx.x, wave_total, before);
+    if (bl.sequence < 0) return;
+    constexpr int VW = D / 32;            // neighbouring dims of a thread
+    typedef float vec_t __attribute__((ext_vector_type(VW)));
+    const int r = blockIdx.y * 8 + threadIdx.x / 32, d = threadIdx.x % 32 * VW, qi = bl.block * kBM + r;
+    if (qi >= bl.n_q) return;
+    const float* part = a.parts + (int64_t)blockIdx.x * kBM * (D + 2);
+    float top = -__builtin_inff(), sum = 0.f;
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, part[s * a.part_stride + kBM * D + r]);
+    vec_t v = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float* p = part + s * a.part_stride;
+        const float ms = p[kBM * D + r];
+        const float f = ms == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ms - top);
+        sum = fmaf(p[kBM * (D + 1) + r], f, sum);
+        v += *reinterpret_cast<const vec_t*>(p + r * D + d) * f;
+    }
+    v *= sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t* dst = a.out + ((bl.q_start + qi) * a.q_heads + bl.hq) * (int64_t)D + d;
+#pragma unroll
+    for (int i = 0; i < VW; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = round_out2<BF>(v[i], v[i + 1]);
+}
+
+// Blocks of queries times heads, at most: the sum of ceil(n / kBM) over sequences.
+int64_t most_slots(int64_t batch, int64_t tokens_q, int q_heads) {
+    return (tokens_q + (kBM - 1) * (batch < tokens_q ? batch : tokens_q)) / kBM * q_heads;
+}
+// Parts that the keys of a block are split into: where blocks and heads leave
+// most of the chip idle and the keys are many, enough to give each compute unit
+// two workgroups, of at least 8 steps each.
+int splits_for(int64_t slots, int64_t batch, int64_t tokens_k) {
+    const int64_t idle = 2 * kSizedForCus / slots, by_keys = tokens_k / batch / (8 * kBN);
+    const int64_t s = idle < by_keys ? idle : by_keys;
+    return s < 2 ? 1 : s > kMostSplits ? kMostSplits : (int)s;
+}
+
 }  // namespace
+
+int64_t prompt_attention_workspace_bytes(int64_t batch, int64_t tokens_q, int64_t tokens_k, int q_heads, int D) {
+    const int64_t slots = most_slots(batch, tokens_q, q_heads);
+    const int s = splits_for(slots, batch, tokens_k);
+    return s == 1 ? 0 : align256(slots * s * kBM * (D + 2) * 4);
+}
 
 int launch_prompt_attention(bool bf, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                             int64_t v_stride, const int32_t* cu_q, const int32_t* cu_k, int64_t batch,
                             int64_t tokens_q, int64_t tokens_k, int q_heads, int kv_heads, int D, float scale,
-                            bool causal, void* out, hipStream_t s) {
+                            bool causal, void* out, void* ws, hipStream_t s) {
     auto in = [](const void* p) { return static_cast<const uint16_t*>(p); };
-    const PromptArgs a{in(q), in(k), in(v), q_stride, k_stride, v_stride, cu_q, cu_k, (int)batch, q_heads,
-                       q_heads / kv_heads, tokens_q, tokens_k, scale * 1.4426950408889634f, causal ? 1 : 0,
-                       static_cast<uint16_t*>(out)};
-    // sum of ceil(n / kBM) over the sequences, at most
-    const int64_t blocks = (tokens_q + (kBM - 1) * (batch < tokens_q ? batch : tokens_q)) / kBM;
-    const dim3 grid((unsigned)(blocks * q_heads));
+    PromptArgs a{in(q), in(k), in(v), q_stride, k_stride, v_stride, cu_q, cu_k, (int)batch, q_heads,
+                 q_heads / kv_heads, tokens_q, tokens_k, scale * 1.4426950408889634f, causal ? 1 : 0,
+                 static_cast<uint16_t*>(out), 1, static_cast<float*>(ws), 0};
+    const int64_t slots = most_slots(batch, tokens_q, q_heads);
+    if (ws) a.splits = splits_for(slots, batch, tokens_k);
+    a.part_stride = slots * kBM * (D + 2);
+    const dim3 grid((unsigned)(slots * a.splits)), join_grid((unsigned)slots, kBM / 8);
     auto go = [&](auto d) {
         constexpr int D_ = decltype(d)::value;
-        return bf ? launch(prompt_attn_kernel<true, D_>, grid, dim3(64 * kWaves), 0, s, a)
-                  : launch(prompt_attn_kernel<false, D_>, grid, dim3(64 * kWaves), 0, s, a);
+        const int rc = bf ? launch(prompt_attn_kernel<true, D_>, grid, dim3(64 * kWaves), 0, s, a)
+                          : launch(prompt_attn_kernel<false, D_>, grid, dim3(64 * kWaves), 0, s, a);
+        if (rc || a.splits == 1) return rc;
+        return bf ? launch(prompt_join_kernel<true, D_>, join_grid, dim3(64 * kWaves), 0, s, a)
+                  : launch(prompt_join_kernel<false, D_>, join_grid, dim3(64 * kWaves), 0, s, a);
     };
     if (D == 64) return go(std::integral_constant<int, 64>{});
     if (D == 128) return go(std::integral_constant<int, 128>{});

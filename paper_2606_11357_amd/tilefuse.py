@@ -35,7 +35,8 @@ EXPORTS = (
     "tf_w8a16_gemm", "tf_w4a16_gemv", "tf_w8a16_gemv", "tf_w4a16_gemv_noalloc", "tf_w4a16_gemm_bf16", "tf_w8a16_gemm_bf16", "tf_w4a16_gemv_bf16",
     "tf_w8a16_gemv_bf16", "tf_unpack", "tf_dequant", "tf_silu_mul", "tf_silu_mul_bf16",
     "tf_add_rms_norm", "tf_kv4_cache_bytes", "tf_kv4_append", "tf_kv4_read",
-    "tf_kv4_attention_workspace_bytes", "tf_kv4_attention", "tf_prompt_attention",
+    "tf_kv4_attention_workspace_bytes", "tf_kv4_attention", "tf_prompt_attention_workspace_bytes",
+    "tf_prompt_attention",
 )
 
 
@@ -94,7 +95,8 @@ def load() -> ctypes.CDLL:
         "tf_kv4_read": (I, [C, P, P, I64, I64, P, P, P]),
         "tf_kv4_attention_workspace_bytes": (I64, [I64, I, I, I, I]),
         "tf_kv4_attention": (I, [C, P, I64, P, I64, I, I, F, P, P, SZ, P]),
-        "tf_prompt_attention": (I, [I, P, I64, P, I64, P, I64, P, P, I64, I64, I64, I, I, I, F, I, P, P]),
+        "tf_prompt_attention": (I, [I, P, I64, P, I64, P, I64, P, P, I64, I64, I64, I, I, I, F, I, P, P, SZ, P]),
+        "tf_prompt_attention_workspace_bytes": (I64, [I64, I64, I64, I, I, I]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -548,17 +550,17 @@ def kv4_attention_workspace_bytes(batch: int, q_len: int, q_heads: int, kv_heads
     return int(n)
 
 
-_attention_ws = {}
+_attention_ws, _prompt_ws = {}, {}
 
 
-def _attention_workspace(device, nbytes):
-    """A zero-filled workspace for kv4_attention, cached per device; like the
-    matmuls' (default_workspace) it must not be shared by calls that run
-    concurrently on different streams."""
+def _cached_workspace(cache, device, nbytes):
+    """A zero-filled workspace for the attention calls, cached per device (decode
+    and prompt attention have one each); like the matmuls' (default_workspace) it
+    must not be shared by calls that run concurrently on different streams."""
     torch = _torch()
-    buf = _attention_ws.get(device.index)
+    buf = cache.get(device.index)
     if buf is None or buf.numel() < nbytes:
-        buf = _attention_ws[device.index] = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        buf = cache[device.index] = torch.zeros(nbytes, dtype=torch.uint8, device=device)
     return buf
 
 
@@ -592,7 +594,7 @@ def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
     if B == 0:
         return out
     if workspace is None:
-        workspace = _attention_workspace(dev, kv4_attention_workspace_bytes(B, q_len, q_heads, cache.kv_heads, D))
+        workspace = _cached_workspace(_attention_ws, dev, kv4_attention_workspace_bytes(B, q_len, q_heads, cache.kv_heads, D))
     else:
         _need_cuda(workspace)
     _check(load().tf_kv4_attention(st, _ptr(q), stride, _ptr(lens), B, q_len, q_heads, D ** -0.5 if scale is None else scale, _ptr(out),
@@ -601,11 +603,22 @@ def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
     return out
 
 
-def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None):
+def prompt_attention_workspace_bytes(batch: int, tokens_q: int, tokens_k: int, q_heads: int, kv_heads: int,
+                                     head_dim: int) -> int:
+    n = load().tf_prompt_attention_workspace_bytes(batch, tokens_q, tokens_k, q_heads, kv_heads, head_dim)
+    if n < 0:
+        raise TileFuseError(int(n), "tf_prompt_attention_workspace_bytes")
+    return int(n)
+
+
+def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None, workspace=None):
     """Attention over packed prompts: q [tokens, q_heads, head_dim], k and v
     [keys, kv_heads, head_dim] (parts of one packed projection are fine), cu_q and
     cu_k int32 [batch + 1] (cu_k is cu_q unless given).  causal: the queries are
-    the last of their sequence's keys.  Returns [tokens, q_heads, head_dim]."""
+    the last of their sequence's keys.  workspace: None for the cached per-device
+    one, False for none (keys are then never split over workgroups), or bytes
+    (prompt_attention_workspace_bytes) of the caller's for calls on several
+    streams.  Returns [tokens, q_heads, head_dim]."""
     torch = _torch()
     strides = [_heads_of(t, what) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
     code = _dtype_code(q.dtype, "q")
@@ -625,8 +638,17 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None
     if T > 0 and Tk == 0:
         return out.zero_()
     if T > 0:
+        if workspace is None:
+            need = prompt_attention_workspace_bytes(B, T, Tk, q_heads, kv_heads, D)
+            workspace = _cached_workspace(_prompt_ws, q.device, need) if need else False
+        ws_bytes = 0
+        if workspace is False:
+            workspace = None
+        else:
+            _need_cuda(workspace)
+            ws_bytes = workspace.numel() * workspace.element_size()
         _check(load().tf_prompt_attention(code, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v), strides[2],
                                           _ptr(cu_q), _ptr(cu_k), B, T, Tk, q_heads, kv_heads, D,
-                                          D ** -0.5 if scale is None else scale, int(causal), _ptr(out), _stream(q.device)),
-               "tf_prompt_attention")
+                                          D ** -0.5 if scale is None else scale, int(causal), _ptr(out), _ptr(workspace), ws_bytes,
+                                          _stream(q.device)), "tf_prompt_attention")
     return out
