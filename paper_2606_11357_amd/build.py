@@ -97,35 +97,40 @@ def build_probe() -> str:
 
 BINDING_SRC = os.path.join(PKG, "binding", "tf_binding.cpp")
 BINDING = os.path.join(PKG, "_tf_binding.so")
+BINDING_OPS_SRC = os.path.join(PKG, "binding", "tf_binding_ops.cpp")
+BINDING_OPS = os.path.join(PKG, "_tf_binding_ops.so")
 
 
-def build_binding() -> str:
-    """The native half of the Python binding (host code only: a CPython
-    extension over torch's C++ tensors, called from tilefuse.py)."""
+def build_binding(src: str | None = None, out: str | None = None) -> str:
+    """A native part of the Python binding, that of the matmul calls unless given
+    (host code only: a CPython extension over torch's C++ tensors, called from
+    tilefuse.py)."""
+    src, out = src or BINDING_SRC, out or BINDING
     import sysconfig
 
     import torch
     from torch.utils import cpp_extension
-    inc = [f"-I{d}" for d in cpp_extension.include_paths()] + [f"-I{sysconfig.get_paths()['include']}"]
+    inc = [f"-I{d}" for d in cpp_extension.include_paths()] + [f"-I{INCLUDE}", f"-I{sysconfig.get_paths()['include']}"]
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *inc, BINDING_SRC,
-           f"-L{lib}", "-lc10", "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{lib}", "-o", BINDING + ".tmp"]
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *inc, src,
+           f"-L{lib}", "-lc10", "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{lib}", "-o", out + ".tmp"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"g++ failed for tf_binding.cpp:\n{r.stderr}")
-    os.replace(BINDING + ".tmp", BINDING)
-    return BINDING
+        raise RuntimeError(f"g++ failed for {os.path.basename(src)}:\n{r.stderr}")
+    os.replace(out + ".tmp", out)
+    return out
 
 
 def build(verbose: bool = False) -> str:
-    with cf.ThreadPoolExecutor(1) as ex:
-        binding = ex.submit(build_binding)
+    with cf.ThreadPoolExecutor(2) as ex:
+        bindings = [ex.submit(build_binding), ex.submit(build_binding, BINDING_OPS_SRC, BINDING_OPS)]
         _build_into(LIB)
         build_probe()
-        binding.result()
+        for b in bindings:
+            b.result()
     if verbose:
-        print(f"built {LIB}, {BINDING} and {PROBE_LIB}")
+        print(f"built {LIB}, {BINDING}, {BINDING_OPS} and {PROBE_LIB}")
     return LIB
 
 

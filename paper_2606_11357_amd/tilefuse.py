@@ -388,6 +388,43 @@ def _int32(t, shape, device, what):
     _same(t, torch.int32, device, shape, what)
 
 
+_ops = None
+
+
+def _native_ops():
+    """The native module's calls of these operators, bound to the loaded library's
+    functions, or stand-ins that leave every call to the general paths (as for the
+    matmuls, _native)."""
+    global _ops
+    if _ops is None:
+        torch = _torch()
+        lib = load()
+        names = ("norm", "append", "read", "decode", "prompt")
+        try:
+            from . import _tf_binding_ops as native
+        except ImportError as e:
+            _ops = dict.fromkeys(names, lambda *call: NotImplemented)
+            warnings.warn(f"the native binding does not load ({e}): norm, cache and attention calls take some 8 us more "
+                          "on the host; build it with `python -m paper_2606_11357_amd.build`", RuntimeWarning, stacklevel=4)
+            return _ops
+        at = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value  # noqa: E731
+        native.bind(tuple(at(n) for n in ("tf_add_rms_norm", "tf_kv4_append", "tf_kv4_read",
+                                              "tf_kv4_attention_workspace_bytes", "tf_kv4_attention",
+                                              "tf_prompt_attention_workspace_bytes", "tf_prompt_attention")),
+                        torch._C._cuda_getCurrentRawStream, _attention_ws, _prompt_ws, _cached_workspace)
+        _ops = {n: getattr(native, n) for n in names}
+    return _ops
+
+
+def _call(name, where, *args):
+    """One native call: its result, NotImplemented (for the general path), or the
+    library's refusal raised."""
+    got = (_ops or _native_ops())[name](*args)
+    if type(got) is int:
+        _check(got, where)
+    return got
+
+
 def add_rms_norm(x, residual=None, weight=None, *, post_weight=None, gate=None, scale=1.0, offset=0.0, eps=1e-6,
                  out=None, residual_out=None):
     """The residual sum and the norms around it, for fp16 or bf16 [M, N]:
@@ -400,6 +437,9 @@ def add_rms_norm(x, residual=None, weight=None, *, post_weight=None, gate=None, 
     without a weight out is None, and with nothing that changes x (no residual,
     post_weight, gate or scale) r is x.  residual_out may be residual itself and
     out may be x: both are then updated in place."""
+    got = _call("norm", "tf_add_rms_norm", x, residual, weight, post_weight, gate, scale, offset, eps, out, residual_out)
+    if got is not NotImplemented:
+        return got
     torch = _torch()
     _need_cuda(x, residual, weight, post_weight, out, residual_out)
     if x.dim() != 2:
@@ -444,10 +484,12 @@ def kv4_cache_bytes(pages: int, page_size: int, kv_heads: int, head_dim: int) ->
 class KV4Cache:
     """A pool of pages of 4-bit keys and values (made by kv4_cache): `data` in the
     library's layout, and the sizes it was made for."""
-    __slots__ = ("data", "pages", "page_size", "kv_heads", "head_dim", "dtype", "_code")
+    __slots__ = ("data", "pages", "page_size", "kv_heads", "head_dim", "dtype", "_sizes")
 
     def __init__(self, data, pages, page_size, kv_heads, head_dim, dtype):
-        self._code = _dtype_code(dtype, "dtype")
+        self._sizes = (pages, page_size, kv_heads, head_dim, _dtype_code(dtype, "dtype"))
+        if not data.is_cuda or not data.is_contiguous() or data.nbytes < kv4_cache_bytes(*self._sizes[:4]):
+            raise ValueError("data must be contiguous GPU memory of kv4_cache_bytes(...) bytes")
         self.data, self.pages, self.page_size = data, pages, page_size
         self.kv_heads, self.head_dim, self.dtype = kv_heads, head_dim, dtype
 
@@ -460,8 +502,7 @@ class KV4Cache:
         if table.shape[1] > 1 and table.stride(1) != 1:
             raise ValueError("the rows of the page table must be contiguous")
         n = table.shape[1]
-        return _Kv4Struct(self.data.data_ptr(), self.pages, self.page_size, self.kv_heads, self.head_dim, self._code,
-                          table.data_ptr(), table.stride(0) if batch > 1 else n, n)
+        return _Kv4Struct(self.data.data_ptr(), *self._sizes, table.data_ptr(), table.stride(0) if batch > 1 else n, n)
 
 
 def kv4_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=None, device="cuda"):
@@ -484,6 +525,9 @@ def kv4_append(cache, table, cu, starts, k, v, cos=None, sin=None, q=None, keys=
     or None for no rotation.  Returns (q, k) rotated, as new tensors or in q_out
     and k_out; q is None where it is not given, k unless keys is true or k_out
     is given."""
+    got = _call("append", "tf_kv4_append", cache, table, cu, starts, k, v, cos, sin, q, keys, q_out, k_out)
+    if got is not NotImplemented:
+        return got
     torch = _torch()
     dev = cache.data.device
     k_stride, v_stride = _heads_of(k, "k"), _heads_of(v, "v")
@@ -525,6 +569,9 @@ def kv4_append(cache, table, cu, starts, k, v, cos=None, sin=None, q=None, keys=
 def kv4_read(cache, table, cu, starts, tokens: int, k_out=None, v_out=None):
     """The cached keys and values of positions starts[b] .. as [tokens, kv_heads,
     head_dim] each, packed as cu (int32 [batch + 1], cu[-1] == tokens) says."""
+    got = _call("read", "tf_kv4_read", cache, table, cu, starts, tokens, k_out, v_out)
+    if got is not NotImplemented:
+        return got
     torch = _torch()
     dev = cache.data.device
     B = starts.shape[0]
@@ -573,6 +620,9 @@ def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
     given.  workspace: None for the cached per-device one, or zero-filled bytes
     (kv4_attention_workspace_bytes) of the caller's for calls on several
     streams.  Returns a tensor of q's shape."""
+    got = _call("decode", "tf_kv4_attention", q, cache, table, lens, scale, out, workspace)
+    if got is not NotImplemented:
+        return got
     torch = _torch()
     dev = cache.data.device
     if q.dim() not in (3, 4):
@@ -619,6 +669,9 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None
     one, False for none (keys are then never split over workgroups), or bytes
     (prompt_attention_workspace_bytes) of the caller's for calls on several
     streams.  Returns [tokens, q_heads, head_dim]."""
+    got = _call("prompt", "tf_prompt_attention", q, k, v, cu_q, cu_k, scale, causal, out, workspace)
+    if got is not NotImplemented:
+        return got
     torch = _torch()
     strides = [_heads_of(t, what) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
     code = _dtype_code(q.dtype, "q")

@@ -396,6 +396,28 @@ def test_prompt(tf, dt, causal, heads, n_q, n_k):
     check_prompt(dt, down(got), qv, kv, vv, n_q, n_k, causal)
 
 
+SPLITS = [((4, 1, 128), [70], [3000]), ((2, 2, 64), [1], [2049]), ((2, 1, 256), [40, 0, 129], [5000, 7, 1300]),
+          ((3, 3, 64), [200, 33], [190, 4200])]
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+@pytest.mark.parametrize("heads,n_q,n_k", SPLITS, ids=str)
+def test_prompt_split_over_keys(tf, dt, causal, heads, n_q, n_k):
+    """Few queries on many keys: the keys in parts, with and without a workspace."""
+    Hq, Hk, D = heads
+    assert tf.prompt_attention_workspace_bytes(len(n_q), sum(n_q), sum(n_k), Hq, Hk, D) > 0
+    rng = np.random.default_rng(sum(n_q) + D)
+    q, qv = up(rng.standard_normal((sum(n_q), Hq, D)), dt)
+    k, kv = up(rng.standard_normal((sum(n_k), Hk, D)) * np.exp(0.5 * rng.standard_normal((1, Hk, D))), dt)
+    v, vv = up(rng.standard_normal((sum(n_k), Hk, D)) + 0.5, dt)
+    args = (q, k, v, i32(offsets(n_q)), i32(offsets(n_k)))
+    got = tf.prompt_attention(*args, causal=causal)
+    check_prompt(dt, down(got), qv, kv, vv, n_q, n_k, causal)
+    assert torch.equal(got, tf.prompt_attention(*args, causal=causal))
+    check_prompt(dt, down(tf.prompt_attention(*args, causal=causal, workspace=False)), qv, kv, vv, n_q, n_k, causal)
+
+
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
 def test_prompt_strided_scale_and_sharp_softmax(tf, dt):
     """Parts of one projection as they are, a scale of the caller's, scores far apart."""
@@ -482,3 +504,85 @@ def test_another_stream(tf):
         got = tf.kv4_attention(q * 1, cache, table, n, workspace=ws)
     s.synchronize()
     assert torch.equal(got, want)
+
+
+def test_native_and_general_paths_agree(tf, monkeypatch):
+    """The native module's calls and the general paths that stand behind them."""
+    heads, lens = (8, 2, 128), [300, 41]
+    cache, table, *_ = filled(tf, "bf16", heads, lens, 64, 12, width=6)
+    x = torch.randn(2, 12, 128, device="cuda").bfloat16()
+    w = torch.randn(1536, device="cuda").bfloat16()
+    cos, sin = (torch.from_numpy(t).cuda() for t in angles(400, 128))
+    cu, starts, after = i32(range(3)), i32(lens), i32([n + 1 for n in lens])
+    flat = x.view(2, 1536)
+
+    def all_calls():
+        return [*tf.add_rms_norm(flat, flat, w), *tf.add_rms_norm(flat, None, w, gate=flat, scale=2),
+                *tf.kv4_append(cache, table, cu, starts, x[:, 8:10], x[:, 10:], cos, sin, q=x[:, :8], keys=True),
+                *tf.kv4_read(cache, table, cu, starts, 2), tf.kv4_attention(x[:, :8], cache, table, after, scale=0.1),
+                tf.prompt_attention(x[:, :8], x[:, 8:10], x[:, 10:], cu)]
+
+    assert tf._native_ops()["norm"](flat, flat, w, None, None, 1.0, 0.0, 1e-6, None, None) is not NotImplemented
+    native = all_calls()
+    monkeypatch.setattr(tf, "_ops", dict.fromkeys(("norm", "append", "read", "decode", "prompt"),
+                                                  lambda *call: NotImplemented))
+    for a, b in zip(native, all_calls()):
+        assert torch.equal(a, b)
+
+
+def test_refusals(tf):
+    """What the binding and the library refuse, on either path."""
+    x = torch.zeros(4, 64, device="cuda").half()
+    with pytest.raises(ValueError):
+        tf.add_rms_norm(x, x.bfloat16(), x[0])
+    with pytest.raises(ValueError):
+        tf.add_rms_norm(x, x[:2], x[0])
+    with pytest.raises(ValueError):
+        tf.add_rms_norm(x.float())
+    with pytest.raises(tf.TileFuseError) as e:
+        tf.add_rms_norm(x[:, :60].contiguous(), weight=x[0, :60].contiguous())
+    assert e.value.status == tf.TF_ERR_SHAPE
+    cache = tf.kv4_cache(2, 32, 1, 64)
+    table, cu, starts = i32([0, 1]).view(1, 2), i32([0, 4]), i32([0])
+    kv = torch.zeros(4, 1, 64, device="cuda").half()
+    for bad in (dict(k=kv.bfloat16()), dict(k=kv[:3]), dict(cu=i32([0, 2, 4])), dict(starts=starts.long()),
+                dict(table=table.view(2, 1)), dict(cos=torch.zeros(9, 32, device="cuda")), dict(k=kv.cpu()),
+                dict(k=torch.zeros(4, 1, 128, device="cuda").half()[:, :, ::2])):
+        a = dict(table=table, cu=cu, starts=starts, k=kv, v=kv) | bad
+        with pytest.raises(ValueError):
+            tf.kv4_append(cache, **a)
+    with pytest.raises(ValueError):
+        tf.kv4_attention(kv[:, :, :32], cache, table, starts)
+    q = torch.zeros(1, 9, 1, 64, device="cuda").half()
+    with pytest.raises(tf.TileFuseError) as e:
+        tf.kv4_attention(q, cache, table, starts)                  # nine tokens
+    assert e.value.status == tf.TF_ERR_ARG
+    with pytest.raises(tf.TileFuseError) as e:
+        tf.kv4_attention(kv[:1], cache, table, starts, scale=0.0)
+    assert e.value.status == tf.TF_ERR_ARG
+    with pytest.raises(tf.TileFuseError) as e:
+        tf.kv4_attention(kv[:1], cache, table, starts, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == tf.TF_ERR_ARG
+    with pytest.raises(ValueError):
+        tf.prompt_attention(kv, kv, kv.bfloat16(), cu)
+    with pytest.raises(tf.TileFuseError) as e:
+        tf.prompt_attention(kv.expand(4, 3, 64).contiguous(), kv.expand(4, 2, 64).contiguous(),
+                            kv.expand(4, 2, 64).contiguous(), cu)
+    assert e.value.status == tf.TF_ERR_SHAPE
+    with pytest.raises(tf.TileFuseError):
+        tf.kv4_cache(2, 48, 1, 64)
+
+
+def test_nothing_to_do(tf):
+    """Calls without tokens return empty tensors."""
+    e = torch.empty(0, 2, 64, device="cuda").half()
+    cache = tf.kv4_cache(1, 32, 2, 64)
+    table = i32([0]).view(1, 1)
+    y, r = tf.add_rms_norm(torch.empty(0, 64, device="cuda").half(), None, torch.ones(64, device="cuda").half())
+    assert y.shape == (0, 64)
+    q, k = tf.kv4_append(cache, table, i32([0, 0]), i32([0]), e, e, q=e, keys=True)
+    assert q.shape == k.shape == (0, 2, 64)
+    assert tf.kv4_read(cache, table, i32([0, 0]), i32([0]), 0)[0].shape == (0, 2, 64)
+    assert tf.prompt_attention(e, e, e, i32([0, 0])).shape == (0, 2, 64)
+    q = torch.randn(3, 2, 64, device="cuda").half()
+    assert (tf.prompt_attention(q, e, e, i32([0, 3]), i32([0, 0])) == 0).all()
