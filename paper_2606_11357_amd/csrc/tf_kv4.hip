@@ -7,6 +7,11 @@ namespace {
 
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 
+// Values (of keys, and as many of values) from which a read goes tile by tile.
+#ifndef KTT
+#define KTT (1 << 22)
+#endif
+constexpr int64_t kTileValues = KTT;
 constexpr int kStagedBatch = 1024;     // up to this many sequences' offsets are searched in LDS
 
 struct AppendArgs {
@@ -78,74 +83,70 @@ __device__ __forceinline__ uint32_t code_of(float x, const RowQuant& r) {
     return (uint32_t)t;
 }
 
-// One row of D values (a query, key or value of one token and head) on D / 16
-// lanes: lane i holds dims 8 i .. + 7 and their partners D/2 + 8 i .. + 7, so
-// the rotation needs no exchange and both operands come in 16-byte loads.
-// HBM-bound: every input is read once and every output written once.
-template <bool BF, int D>
-__global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
-    constexpr int LPR = D / 16;
-    __shared__ int32_t lds_cu[kStagedBatch + 1];
-    const int32_t* cu = stage_offsets(a.cu, a.batch, lds_cu);
-    const int rows = a.q_heads + 2 * a.cache.kv_heads;
-    // (token, row) pairs: at most TF_MAX_M * 3 TF_MAX_HEADS, below 2^32
-    const uint32_t at = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    const int i = threadIdx.x % LPR;
-    const bool active = at < a.tokens * rows;
-    const int64_t t = active ? at / (uint32_t)rows : 0;
-    const int row = active ? (int)(at % (uint32_t)rows) : 0;
-    const int kind = row < a.q_heads ? 0 : row < a.q_heads + a.cache.kv_heads ? 1 : 2;
-    const int h = row - (kind == 0 ? 0 : kind == 1 ? a.q_heads : a.q_heads + a.cache.kv_heads);
-    const uint16_t* src = (kind == 0   ? a.q + t * a.q_stride
-                           : kind == 1 ? a.k + t * a.k_stride
-                                       : a.v + t * a.v_stride) +
-                          (int64_t)h * D + 8 * i;
-    u16x8 xa{}, xb{};
-    if (active) {
-        xa = *reinterpret_cast<const u16x8*>(src);
-        xb = *reinterpret_cast<const u16x8*>(src + D / 2);
+// A row of D values (a query, key or value of one token and head) on D / 16
+// lanes: lane i holds dims 8 i .. + 7 and their partners D/2 + 8 i .. + 7, so the
+// rotation needs no exchange and both operands come in 16-byte loads.
+struct Row {
+    u16x8 a, b;          // as loaded
+    int kind, h;         // 0 query, 1 key, 2 value; head
+    int64_t t;           // packed token
+    uint32_t pos;        // its position, where known
+    bool active, known;  // a row of the call; one with a position (and angles)
+};
+
+template <int D>
+__device__ __forceinline__ void load_row(const AppendArgs& a, Row& r, int i) {
+    const uint16_t* src = (r.kind == 0   ? a.q + r.t * a.q_stride
+                           : r.kind == 1 ? a.k + r.t * a.k_stride
+                                         : a.v + r.t * a.v_stride) +
+                          (int64_t)r.h * D + 8 * i;
+    r.a = r.b = u16x8{};
+    if (r.active) {
+        r.a = *reinterpret_cast<const u16x8*>(src);
+        r.b = *reinterpret_cast<const u16x8*>(src + D / 2);
     }
-    const int b = owner_of(cu, a.batch, t);
-    const int64_t pos = b < 0 ? -1 : (int64_t)a.starts[b] + (t - cu[b]);
-    bool known = pos >= 0 && pos <= INT32_MAX;
+}
+
+// Rotates, writes the 16-bit outputs, and quantizes a key or value into its
+// tile (null: nowhere).  All lanes of the wave; tile() is asked once per row.
+template <bool BF, int D, typename TileOf>
+__device__ __forceinline__ void append_row(const AppendArgs& a, const Row& r, int i, TileOf tile_of) {
+    constexpr int LPR = D / 16;
     float lo[8], hi[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        lo[j] = scale_f32<BF>(xa[j]);
-        hi[j] = scale_f32<BF>(xb[j]);
+        lo[j] = scale_f32<BF>(r.a[j]);
+        hi[j] = scale_f32<BF>(r.b[j]);
     }
-    if (a.cos) {
-        known = known && pos < a.positions;
-        if (kind < 2 && known) {
+    if (a.cos && r.kind < 2 && r.known) {
 #pragma clang fp contract(off)
-            const float* cp = a.cos + pos * (D / 2) + 8 * i;
-            const float* sp = a.sin + pos * (D / 2) + 8 * i;
-            float c[8], s[8];
+        const float* cp = a.cos + (int64_t)r.pos * (D / 2) + 8 * i;
+        const float* sp = a.sin + (int64_t)r.pos * (D / 2) + 8 * i;
+        float c[8], s[8];
 #pragma unroll
-            for (int j = 0; j < 8; j += 4) {
-                const float4_t cv = *reinterpret_cast<const float4_t*>(cp + j);
-                const float4_t sv = *reinterpret_cast<const float4_t*>(sp + j);
+        for (int j = 0; j < 8; j += 4) {
+            const float4_t cv = *reinterpret_cast<const float4_t*>(cp + j);
+            const float4_t sv = *reinterpret_cast<const float4_t*>(sp + j);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) { c[j + m] = cv[m]; s[j + m] = sv[m]; }
-            }
+            for (int m = 0; m < 4; ++m) { c[j + m] = cv[m]; s[j + m] = sv[m]; }
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float ac = lo[j] * c[j], bs = hi[j] * s[j];
-                const float bc = hi[j] * c[j], as = lo[j] * s[j];
-                lo[j] = ac - bs;
-                hi[j] = bc + as;
-            }
+        for (int j = 0; j < 8; ++j) {
+            const float ac = lo[j] * c[j], bs = hi[j] * s[j];
+            const float bc = hi[j] * c[j], as = lo[j] * s[j];
+            lo[j] = ac - bs;
+            hi[j] = bc + as;
         }
     }
-    uint16_t* out = kind == 0 ? a.q_out : kind == 1 ? a.k_out : nullptr;
-    if (active && out) {
-        uint16_t* o = out + (t * (kind == 0 ? a.q_heads : a.cache.kv_heads) + h) * D + 8 * i;
+    uint16_t* out = r.kind == 0 ? a.q_out : r.kind == 1 ? a.k_out : nullptr;
+    if (r.active && out) {
+        uint16_t* o = out + (r.t * (r.kind == 0 ? a.q_heads : a.cache.kv_heads) + r.h) * D + 8 * i;
         const uint16_t nan16 = BF ? 0x7FC0 : 0x7E00;
         u16x8 oa, ob;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            oa[j] = known ? round_out<BF>(lo[j]) : nan16;
-            ob[j] = known ? round_out<BF>(hi[j]) : nan16;
+            oa[j] = r.known ? round_out<BF>(lo[j]) : nan16;
+            ob[j] = r.known ? round_out<BF>(hi[j]) : nan16;
         }
         *reinterpret_cast<u16x8*>(o) = oa;
         *reinterpret_cast<u16x8*>(o + D / 2) = ob;
@@ -161,9 +162,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
     least = -row_max<LPR>(-least);
     most = row_max<LPR>(most);
     const bool finite = row_max<LPR>(total == 0.f ? 0.f : 1.f) == 0.f;
-    if (!active || kind == 0 || !known) return;
-    constexpr int64_t TB = kv4_tile_bytes(D);
-    uint8_t* tile = kv4_tile(a.cache, b, (uint32_t)pos, h, TB);
+    if (!r.active || r.kind == 0 || !r.known) return;
+    uint8_t* tile = tile_of();
     if (!tile) return;
     const RowQuant rq = row_quant<BF>(least, most, finite);
     uint32_t qa[8], qb[8];
@@ -172,8 +172,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
         qa[j] = code_of(lo[j], rq);
         qb[j] = code_of(hi[j], rq);
     }
-    const int kk = (int)(pos % kKvTile), u = kk >> 4, c = kk & 15, g = c >> 2, jj = c & 3;
-    if (kind == 1) {
+    const int kk = (int)(r.pos % kKvTile), u = kk >> 4, c = kk & 15, g = c >> 2, jj = c & 3;
+    if (r.kind == 1) {
         // two words of 8 codes: dims 8 i (lane group 8 i / (D/4)) and D/2 + 8 i
         uint32_t wa = 0, wb = 0;
 #pragma unroll
@@ -195,11 +195,107 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
         }
     }
     if (i == 0) {
-        uint16_t* meta = reinterpret_cast<uint16_t*>(tile + 32 * D) + g * 32 + (kind == 1 ? 0 : 16) + 4 * u + jj;
+        uint16_t* meta = reinterpret_cast<uint16_t*>(tile + 32 * D) + g * 32 + (r.kind == 1 ? 0 : 16) + 4 * u + jj;
         meta[0] = rq.s16;
         meta[8] = rq.z16;
     }
 }
+
+// The row at place `at` of (token, row of the token) pairs.
+__device__ __forceinline__ void place_row(const AppendArgs& a, const int32_t* cu, uint32_t at, int rows, Row& r,
+                                          int& sequence) {
+    r.active = at < a.tokens * rows;
+    r.t = r.active ? at / (uint32_t)rows : 0;
+    const int row = r.active ? (int)(at % (uint32_t)rows) : 0;
+    r.kind = row < a.q_heads ? 0 : row < a.q_heads + a.cache.kv_heads ? 1 : 2;
+    r.h = row - (r.kind == 0 ? 0 : r.kind == 1 ? a.q_heads : a.q_heads + a.cache.kv_heads);
+    sequence = owner_of(cu, a.batch, r.t);
+    const int64_t pos = sequence < 0 ? -1 : (int64_t)a.starts[sequence] + (r.t - cu[sequence]);
+    r.known = pos >= 0 && pos <= INT32_MAX && (!a.cos || pos < a.positions);
+    r.pos = (uint32_t)pos;
+}
+
+// Every row of every token in order.  HBM-bound where tokens are many, else by a
+// chain of four dependent loads (offsets, start, page, angles).
+template <bool BF, int D>
+__global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
+    constexpr int LPR = D / 16;
+    __shared__ int32_t lds_cu[kStagedBatch + 1];
+    const int32_t* cu = stage_offsets(a.cu, a.batch, lds_cu);
+    // (token, row) pairs: at most TF_MAX_M * 3 TF_MAX_HEADS, below 2^32
+    const int i = threadIdx.x % LPR;
+    Row r;
+    int b;
+    place_row(a, cu, blockIdx.x * (256 / LPR) + threadIdx.x / LPR, a.q_heads + 2 * a.cache.kv_heads, r, b);
+    load_row<D>(a, r, i);
+    append_row<BF, D>(a, r, i, [&] { return kv4_tile(a.cache, b, r.pos, r.h, kv4_tile_bytes(D)); });
+}
+
+// Tiles of the cache that the tokens of a call touch: sequence by sequence,
+// with the tokens that no sequence owns, before cu[0] and from cu[batch] on, as
+// two more.  slot -> its sequence, tile and the packed token of its key 0.
+struct TileSlot {
+    int sequence = -2;               // -1: unowned tokens; -2: no such slot
+    int32_t tile;                    // may be negative (positions below 0)
+    int64_t t0;                      // packed token of the tile's first position
+    int64_t from, to;                // the sequence's packed tokens
+
+    static __device__ __forceinline__ void range(const int32_t* cu, int batch, int64_t tokens, int i, int64_t& from,
+                                                 int64_t& to) {
+        from = i == 0 ? 0 : cu[i - 1];
+        to = i > batch ? tokens : cu[i];
+        from = from < 0 ? 0 : from;
+        to = to > tokens ? tokens : to;
+    }
+    static __device__ __forceinline__ int32_t start_of(const int32_t* starts, int batch, int i) {
+        return i == 0 || i > batch ? 0 : starts[i - 1];
+    }
+    static __device__ __forceinline__ uint32_t tiles_of(int64_t from, int64_t to, int32_t start) {
+        if (to <= from) return 0;
+        return (uint32_t)((((int64_t)start + (to - from) - 1) >> 5) - (start >> 5) + 1);
+    }
+    // All 256 threads; before: 257 words of LDS, scratch: 4.
+    __device__ __forceinline__ TileSlot(const int32_t* cu, const int32_t* starts, int batch, int64_t tokens,
+                                        uint32_t slot, uint32_t* before, uint32_t* scratch) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = batch + 2, seg = (n + 255) / 256;
+        uint32_t sum = 0;
+        for (int i = tid * seg; i < (tid + 1) * seg && i < n; ++i) {
+            range(cu, batch, tokens, i, from, to);
+            sum += tiles_of(from, to, start_of(starts, batch, i));
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(sum, d);
+            if (lane >= d) sum += o;
+        }
+        if (lane == 63) scratch[wave] = sum;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) sum += scratch[w];
+        before[tid + 1] = sum;
+        if (tid == 0) before[0] = 0;
+        __syncthreads();
+        if (slot >= before[256]) return;
+        int s0 = 0, s1 = 256;
+        while (s1 - s0 > 1) {
+            const int mid = (s0 + s1) >> 1;
+            if (before[mid] <= slot) s0 = mid;
+            else s1 = mid;
+        }
+        int i = s0 * seg;
+        uint32_t done = before[s0];
+        int32_t start;
+        for (;; ++i) {
+            range(cu, batch, tokens, i, from, to);
+            start = start_of(starts, batch, i);
+            const uint32_t k = tiles_of(from, to, start);
+            if (slot < done + k) break;
+            done += k;
+        }
+        sequence = i == 0 || i > batch ? -1 : __builtin_amdgcn_readfirstlane(i - 1);
+        tile = (start >> 5) + (int32_t)(slot - done);
+        t0 = from + ((int64_t)tile * kKvTile - start);
+    }
+};
 
 struct ReadArgs {
     Kv4 cache;
@@ -209,7 +305,7 @@ struct ReadArgs {
     uint16_t *k, *v;
 };
 
-// One row on D / 16 lanes, as in the append.
+// Few tokens of a sequence at a time: one row on D / 16 lanes, as in the append.
 template <bool BF, int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
     constexpr int LPR = D / 16;
@@ -269,11 +365,98 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
     *reinterpret_cast<u16x8*>(o + D / 2) = ob;
 }
 
+// Many tokens of a sequence: a wave takes the keys (or values) of one head for
+// one tile, whose lines it reads whole.
+template <bool BF, int D>
+__global__ __launch_bounds__(256) void kv4_read_tiles_kernel(ReadArgs a, uint32_t wgs_per_slot) {
+    __shared__ uint32_t before[257], scratch[4];
+    const TileSlot ts(a.cu, a.starts, a.batch, a.tokens, blockIdx.x / wgs_per_slot, before, scratch);
+    const int item = (int)(blockIdx.x % wgs_per_slot) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (ts.sequence == -2 || item >= 2 * a.cache.kv_heads) return;
+    const bool is_v = item >= a.cache.kv_heads;
+    const int h = item - (is_v ? a.cache.kv_heads : 0);
+    const uint8_t* tile = nullptr;
+    if (ts.sequence >= 0 && ts.tile >= 0 && ts.tile <= INT32_MAX / kKvTile)
+        tile = kv4_tile(a.cache, ts.sequence, (uint32_t)ts.tile * kKvTile, h, kv4_tile_bytes(D));
+    auto out = [&](int kk, int d) {
+        return reinterpret_cast<u16x8*>((is_v ? a.v : a.k) + ((ts.t0 + kk) * a.cache.kv_heads + h) * (int64_t)D + d);
+    };
+    auto inside = [&](int kk) { return ts.t0 + kk >= ts.from && ts.t0 + kk < ts.to; };
+    if (!tile) {
+        u16x8 nan;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) nan[j] = BF ? 0x7FC0 : 0x7E00;
+        for (int x = lane; x < kKvTile * D / 8; x += 64)
+            if (inside(x / (D / 8))) *out(x / (D / 8), x % (D / 8) * 8) = nan;
+        return;
+    }
+    const uint16_t* meta = reinterpret_cast<const uint16_t*>(tile + 32 * D);
+    if (!is_v) {
+        // a word is 8 dims of one key
+        constexpr int WPR = D / 8, ROUNDS = kKvTile * WPR / 64;
+        uint32_t word[ROUNDS];
+        float s[ROUNDS], z[ROUNDS];
+#pragma unroll
+        for (int n = 0; n < ROUNDS; ++n) {
+            const int kk = (n * 64 + lane) / WPR, x = lane % WPR, g = x / (D / 32), w = x % (D / 32);
+            word[n] = *reinterpret_cast<const uint32_t*>(tile + kv4_word<D>(kk >> 4, g * 16 + (kk & 15), w));
+            const uint16_t* m = meta + (kk >> 2 & 3) * 32 + 4 * (kk >> 4) + (kk & 3);
+            s[n] = scale_f32<BF>(m[0]);
+            z[n] = scale_f32<BF>(m[8]);
+        }
+#pragma unroll
+        for (int n = 0; n < ROUNDS; ++n) {
+            const int kk = (n * 64 + lane) / WPR;
+            u16x8 o;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                o[j] = round_out<BF>(((float)(word[n] >> (4 * (j >> 1) + 16 * (j & 1)) & 15) - z[n]) * s[n]);
+            if (inside(kk)) *out(kk, lane % WPR * 8) = o;
+        }
+        return;
+    }
+    // eight words are 8 dims and their partners D/2 on of four keys
+    constexpr int UNITS = kKvTile / 4 * (D / 16);
+#pragma unroll
+    for (int x = lane; x < UNITS; x += 64) {
+        const int dims = x % (D / 16) * 8, ug = x / (D / 16), u = ug >> 2, g = ug & 3;
+        uint32_t word[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            word[j] = *reinterpret_cast<const uint32_t*>(
+                tile + 16 * D + kv4_word<D>(u, g * 16 + (dims & 15) + j, dims >> 4));
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+            const int kk = 16 * u + 4 * g + jj;
+            const uint16_t* m = meta + g * 32 + 16 + 4 * u + jj;
+            const float s = scale_f32<BF>(m[0]), z = scale_f32<BF>(m[8]);
+            u16x8 oa, ob;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t byte = (word[j] >> (8 * kv4_byte(jj)) & 0xFF) ^ (jj & 1 ? 0xFFu : 0u);
+                oa[j] = round_out<BF>(((float)(byte & 15) - z) * s);
+                ob[j] = round_out<BF>(((float)(byte >> 4) - z) * s);
+            }
+            if (inside(kk)) {
+                *out(kk, dims) = oa;
+                *out(kk, dims + D / 2) = ob;
+            }
+        }
+    }
+}
+
 template <typename F>
 int by_head_dim(int D, F&& f) {
     if (D == 64) return f(std::integral_constant<int, 64>{});
     if (D == 128) return f(std::integral_constant<int, 128>{});
     return f(std::integral_constant<int, 256>{});
+}
+
+// Tiles that the tokens of a call touch, at most: n tokens of a sequence (or of
+// the two runs that none owns) touch no more than n / 32 + 2.
+int64_t most_tiles(int64_t batch, int64_t tokens) {
+    const int64_t runs = batch + 2 < tokens ? batch + 2 : tokens;
+    return (tokens + 62 * runs) / kKvTile;
 }
 
 Kv4 device_view(const tf_kv4_cache& c) {
@@ -304,10 +487,10 @@ int launch_kv4_append(const tf_kv4_cache& c, const void* q, int64_t q_stride, co
                        static_cast<uint16_t*>(k_out)};
     return by_head_dim(c.head_dim, [&](auto d) {
         constexpr int D = decltype(d)::value;
-        const int64_t threads = tokens * (q_heads + 2 * c.kv_heads) * (D / 16);
-        const dim3 grid((unsigned)((threads + 255) / 256));
-        if (c.dtype == TF_BF16) return launch(kv4_append_kernel<true, D>, grid, dim3(256), 0, s, a);
-        return launch(kv4_append_kernel<false, D>, grid, dim3(256), 0, s, a);
+        const bool bf = c.dtype == TF_BF16;
+        const dim3 grid((unsigned)((tokens * (q_heads + 2 * c.kv_heads) * (D / 16) + 255) / 256));
+        return bf ? launch(kv4_append_kernel<true, D>, grid, dim3(256), 0, s, a)
+                  : launch(kv4_append_kernel<false, D>, grid, dim3(256), 0, s, a);
     });
 }
 
@@ -317,10 +500,16 @@ int launch_kv4_read(const tf_kv4_cache& c, const int32_t* cu, const int32_t* sta
                      static_cast<uint16_t*>(v)};
     return by_head_dim(c.head_dim, [&](auto d) {
         constexpr int D = decltype(d)::value;
-        const int64_t threads = tokens * 2 * c.kv_heads * (D / 16);
-        const dim3 grid((unsigned)((threads + 255) / 256));
-        if (c.dtype == TF_BF16) return launch(kv4_read_kernel<true, D>, grid, dim3(256), 0, s, a);
-        return launch(kv4_read_kernel<false, D>, grid, dim3(256), 0, s, a);
+        const bool bf = c.dtype == TF_BF16;
+        if (tokens * c.kv_heads * D >= kTileValues) {
+            const uint32_t per_slot = (uint32_t)(2 * c.kv_heads + 3) / 4;
+            const dim3 grid((unsigned)most_tiles(batch, tokens) * per_slot);
+            return bf ? launch(kv4_read_tiles_kernel<true, D>, grid, dim3(256), 0, s, a, per_slot)
+                      : launch(kv4_read_tiles_kernel<false, D>, grid, dim3(256), 0, s, a, per_slot);
+        }
+        const dim3 grid((unsigned)((tokens * 2 * c.kv_heads * (D / 16) + 255) / 256));
+        return bf ? launch(kv4_read_kernel<true, D>, grid, dim3(256), 0, s, a)
+                  : launch(kv4_read_kernel<false, D>, grid, dim3(256), 0, s, a);
     });
 }
 
