@@ -272,7 +272,7 @@ int tf_silu_mul_bf16(const uint16_t* GU_bf16, int64_t M, int64_t N, uint16_t* H_
  * `dtype` is TF_F16 or TF_BF16, the type of every 16-bit tensor of a call.
  * Activations are [tokens, heads, head_dim] with head_dim contiguous, heads
  * head_dim apart and tokens `stride` elements apart (a multiple of 8, at least
- * heads * head_dim), so that the parts of one packed q, k, v projection are
+ * heads * head_dim and at most 2^24), so that the parts of one packed q, k, v projection are
  * operands as they are.  head_dim is 64, 128 or 256; q_heads is a multiple of
  * kv_heads, and query head h reads key/value head h / (q_heads / kv_heads).
  * Sequences are packed one after the other: sequence b has the tokens

@@ -30,7 +30,8 @@ bool bad_dtype(int dtype) { return dtype != TF_F16 && dtype != TF_BF16; }
 bool bad_head_dim(int d) { return d != 64 && d != 128 && d != 256; }
 bool bad_heads(int64_t h) { return h < 1 || h > TF_MAX_HEADS; }
 bool bad_stride(int64_t stride, int heads, int d) {
-    return stride % 8 != 0 || stride < (int64_t)heads * d || stride > (int64_t(1) << 40);
+    // a kernel's 32-bit offsets span 64 tokens
+    return stride % 8 != 0 || stride < (int64_t)heads * d || stride > (int64_t(1) << 24);
 }
 bool bad_scale(float s) { return !(s > 0.f) || s > 1e30f; }
 

@@ -21,6 +21,8 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 4;
 constexpr int kBM = 32 * kWaves;       // queries of a workgroup
 constexpr int kBN = 64;                // keys of a step
+constexpr float kSlack = 8.f;
+template <bool BF> constexpr uint32_t kOnes = BF ? 0x3F803F80u : 0x3C003C00u;
 constexpr int kSizedForCus = 256, kMostSplits = 16;
 
 struct PromptArgs {
@@ -36,6 +38,13 @@ struct PromptArgs {
     float* parts;                      // splits > 1: [part][block * q_heads + head][kBM] rows of D sums, maxima, sums
     int64_t part_stride;               // floats of one part
 };
+
+// v of the lane 32 away
+__device__ __forceinline__ float other_half(float v) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return __builtin_bit_cast(float, threadIdx.x & 32 ? r[0] : r[1]);
+}
 
 template <bool BF>
 __device__ __forceinline__ float16_t mfma32(const u32x4& a, const u32x4& b, const float16_t& c) {
@@ -137,6 +146,12 @@ struct Block {
     }
 };
 
+// 16 bytes a lane from base + off straight to LDS, lane i's at dst + 16 i.
+__device__ __forceinline__ void direct_load16(const uint16_t* base, uint32_t off, uint16_t* dst) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(base, 0x7FFFFFFFu),
+                                             (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
+}
+
 template <bool BF, int D>
 __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_kernel(PromptArgs a) {
     constexpr int CH = D / 8;             // 16-byte chunks of a row
@@ -171,23 +186,37 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u32x4*>(src + 16 * s);
     }
-    // the keys' and values' rows straight into LDS, each lane 16 bytes in
-    // order; the rearrangement is in which chunk of the row a lane fetches
-    auto fetch = [&](int step) {
-        const int buf = step & 1;
-        constexpr int LOADS = kBN * CH / (64 * kWaves);
+    // The keys' (or values') rows of a step straight into LDS, each lane 16 bytes
+    // in order; the rearrangement is in which chunk of the row a lane fetches.
+    // A lane's offsets from the step's first row are the same in every step but
+    // one that ends past the last key: there they stay on the last row (those
+    // scores are hidden, and what is hidden has to be a number).
+    constexpr int LOADS = kBN * CH / (64 * kWaves);
+    const uint32_t k_row = (uint32_t)a.k_stride * 2, v_row = (uint32_t)a.v_stride * 2;
+    const uint16_t* const k_base = a.k + k_start * a.k_stride + (int64_t)hk * D;
+    const uint16_t* const v_base = a.v + k_start * a.v_stride + (int64_t)hk * D;
+    uint32_t k_off[LOADS], v_off[LOADS];
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int at = (wave * LOADS + i) * 64;       // the wave's first chunk
-            const int r = (at + lane) / CH, ch = (at + lane) % CH;
-            int key = step * kBN + r;
-            key = key < n_k ? key : n_k - 1;              // rows past the end: masked scores
-            const uint16_t* kp = a.k + (k_start + key) * a.k_stride + (int64_t)hk * D + 8 * k_chunk<D>(r, ch);
-            const uint16_t* vp = a.v + (k_start + key) * a.v_stride + (int64_t)hk * D + 8 * v_chunk<D>(r, ch);
-            typedef __attribute__((address_space(3))) void lds_void;
-            typedef const __attribute__((address_space(1))) void global_void;
-            __builtin_amdgcn_global_load_lds((global_void*)kp, (lds_void*)&ks[buf][at * 8], 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((global_void*)vp, (lds_void*)&vs[buf][at * 8], 16, 0, 0);
+    for (int i = 0; i < LOADS; ++i) {
+        const int at = (wave * LOADS + i) * 64 + lane, r = at / CH, ch = at % CH;
+        k_off[i] = r * k_row + 16 * k_chunk<D>(r, ch);
+        v_off[i] = r * v_row + 16 * v_chunk<D>(r, ch);
+    }
+    auto fetch = [&](bool V, int step) {
+        uint16_t* const buf = (V ? vs[step & 1] : ks[step & 1]) + wave * LOADS * 512;
+        const int64_t key0 = (int64_t)step * kBN;
+        const uint16_t* const rows = V ? v_base + key0 * a.v_stride : k_base + key0 * a.k_stride;
+        if (key0 + kBN <= n_k) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) direct_load16(rows, V ? v_off[i] : k_off[i], buf + i * 512);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int at = (wave * LOADS + i) * 64 + lane, r = at / CH, ch = at % CH;
+                const uint32_t row = min(r, (int)(n_k - 1 - key0));
+                direct_load16(rows, V ? row * v_row + 16 * v_chunk<D>(r, ch) : row * k_row + 16 * k_chunk<D>(r, ch),
+                              buf + i * 512);
+            }
         }
     };
 
@@ -197,17 +226,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = -__builtin_inff(), l = 0.f;
-
-    if (step0 < steps) fetch(step0);
-    for (int step = step0; step < steps; ++step) {
-        __builtin_amdgcn_s_waitcnt(0);                    // this wave's part of the tiles is there
-        __syncthreads();                                  // everyone's is, and the other buffer is free
-        if (step + 1 < steps) fetch(step + 1);
-        const int key0 = step * kBN;
-        if (key0 >= wave_keys) continue;
+    // S^T of a step's 64 keys
+    auto scores = [&](float16_t (&s)[2], int step) {
         const uint16_t* kb = ks[step & 1];
-        const uint16_t* vb = vs[step & 1];
-        float16_t s[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -219,6 +240,28 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
                 s[t] = mfma32<BF>(kf, q[j], s[t]);
             }
         }
+    };
+
+    // A step's scores are computed while the step before goes through its
+    // softmax: the matrix cores and the vector units then work side by side.
+    // Keys are fetched two steps ahead, values one.
+    float16_t s[2];
+    if (step0 < steps) {
+        fetch(false, step0);
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (step0 + 1 < steps) fetch(false, step0 + 1);
+        fetch(true, step0);
+        scores(s, step0);
+    }
+    for (int step = step0; step < steps; ++step) {
+        __builtin_amdgcn_s_waitcnt(0);                    // this wave's part of the tiles is there
+        __syncthreads();                                  // everyone's is, and the other buffers are free
+        if (step + 2 < steps) fetch(false, step + 2);
+        if (step + 1 < steps) fetch(true, step + 1);
+        const int key0 = step * kBN;
+        if (key0 >= wave_keys) continue;
+        const uint16_t* vb = vs[step & 1];
         if (key0 + kBN - 1 > wave_low) {                  // some key is hidden from some query
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -231,8 +274,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > m)) {
+        top = fmaxf(top, other_half(top));
+        // The sums move to a new maximum only where it outgrows the old one by
+        // 2^kSlack; until then weights above 1 are as exact as those below.
+        if (__any((top - m) * a.scale2 > kSlack || (m == -__builtin_inff() && top > m))) {
             const float f = top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m - top) * a.scale2);
             m = top;
             l *= f;
@@ -242,6 +287,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
                 for (int i = 0; i < 16; ++i) o[t][i] *= f;
         }
         const float base = m == -__builtin_inff() ? 0.f : m * a.scale2;
+        // (after the last step the scores of a step that is there are computed again)
+        float16_t next[2];
+        scores(next, step + 1 < steps ? step + 1 : step);
         u32x4 p[4];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -249,8 +297,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
             for (int i = 0; i < 16; i += 2) {
                 const float e0 = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale2, -base));
                 const float e1 = __builtin_amdgcn_exp2f(fmaf(s[t][i + 1], a.scale2, -base));
-                l += e0 + e1;
-                p[2 * t + i / 8][(i % 8) / 2] = round_out2<BF>(e0, e1);
+                const uint32_t pair = round_out2<BF>(e0, e1);
+                p[2 * t + i / 8][(i % 8) / 2] = pair;
+                l = dot2<BF>(pair, kOnes<BF>, l);         // the weights as the matrix cores see them
             }
         // keys 16 j + 4 half + 0..3 and + 8: the order in which p holds them
         const int l16 = lane & 15, sub = (lane >> 4) & 1;
@@ -264,8 +313,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
                 const u32x2 v1 = lds_read_tr16(vb + r1 * D + 8 * v_chunk<D>(r1, d >> 3) + (d & 7));
                 o[t] = mfma32<BF>(u32x4{v0[0], v0[1], v1[0], v1[1]}, p[j], o[t]);
             }
+        s[0] = next[0];
+        s[1] = next[1];
     }
-    l += __shfl_xor(l, 32);
+    l += other_half(l);
     if (qi >= n_q) return;
     if (a.splits > 1) {
         // a row's sums as they are, its maximum and its sum of weights
