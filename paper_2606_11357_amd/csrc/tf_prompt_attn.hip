@@ -35,7 +35,7 @@ struct PromptArgs {
     int causal;
     uint16_t* out;
     int splits;                        // parts that each block's keys are split into
-    float* parts;                      // splits > 1: [part][block * q_heads + head][kBM] rows of D sums, maxima, sums
+    float* parts;                      // splits > 1: [part][slot] kBM rows of D sums, of a maximum, of a sum
     int64_t part_stride;               // floats of one part
 };
 
@@ -99,12 +99,22 @@ struct Block {
     // The first of the block's steps that part s takes.
     __device__ __forceinline__ int first_step(int s) const { return (int)((int64_t)steps * s / splits); }
 
-    // All threads; wave_total: kWaves words of LDS, before: 64 kWaves + 1.
-    __device__ __forceinline__ Block(const PromptArgs& a, uint32_t slot, uint32_t* wave_total, uint32_t* before) {
+    struct Found { int32_t sequence, block; int64_t q_start, k_start; int32_t n_q, n_k; };
+    // All threads.  Each looks at its own sequences, and the one whose sequence
+    // the block falls into tells the others.
+    __device__ __forceinline__ Block(const PromptArgs& a, uint32_t slot, uint32_t* wave_total, Found* found) {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        const int seg = (a.batch + 64 * kWaves - 1) / (64 * kWaves);
-        uint32_t sum = 0;
-        for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) sum += blocks_of(a, b);
+        const int seg = (a.batch + 64 * kWaves - 1) / (64 * kWaves), first = tid * seg;
+        const int last = first + seg < a.batch ? first + seg : a.batch;
+        Found mine{};
+        uint32_t own = 0;
+        for (int b = first; b < last; ++b) {
+            // (with one sequence a thread all four offsets are loaded at once)
+            mine.n_q = span(a.cu_q, b, a.tokens_q, mine.q_start);
+            mine.n_k = span(a.cu_k, b, a.tokens_k, mine.k_start);
+            own += (uint32_t)((mine.n_q + kBM - 1) / kBM);
+        }
+        uint32_t sum = own;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t o = __shfl_up(sum, d);
@@ -112,33 +122,44 @@ struct Block {
         }
         if (lane == 63) wave_total[wave] = sum;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) sum += wave_total[w];
-        before[tid + 1] = sum;
-        if (tid == 0) before[0] = 0;
-        __syncthreads();
-        const uint32_t total = before[64 * kWaves], order = slot / (uint32_t)a.q_heads;
+        uint32_t total = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) sum += wave_total[w];
+            total += wave_total[w];
+        }
+        const uint32_t order = slot / (uint32_t)a.q_heads;
         if (order >= total) return;
+        uint32_t x = total - 1 - order;
+        if (x < sum && x >= sum - own) {
+            x -= sum - own;
+            mine.sequence = first;
+            if (seg > 1) {
+                for (;; ++mine.sequence) {
+                    const uint32_t n = blocks_of(a, mine.sequence);
+                    if (x < n) break;
+                    x -= n;
+                }
+                mine.n_q = span(a.cu_q, mine.sequence, a.tokens_q, mine.q_start);
+                mine.n_k = span(a.cu_k, mine.sequence, a.tokens_k, mine.k_start);
+            }
+            mine.block = (int)x;
+            *found = mine;
+        }
+        __syncthreads();
         const int kv_heads = a.q_heads / a.group, hx = (int)(slot % (uint32_t)a.q_heads);
         hk = hx % kv_heads;
         hq = hk * a.group + hx / kv_heads;
-        const uint32_t x = total - 1 - order;
-        int s0 = 0, s1 = 64 * kWaves;
-        while (s1 - s0 > 1) {
-            const int mid = (s0 + s1) >> 1;
-            if (before[mid] <= x) s0 = mid;
-            else s1 = mid;
-        }
-        int b = s0 * seg;
-        uint32_t done = before[s0];
-        for (;; ++b) {
-            const uint32_t n = blocks_of(a, b);
-            if (x < done + n) break;
-            done += n;
-        }
-        sequence = __builtin_amdgcn_readfirstlane(b);
-        block = __builtin_amdgcn_readfirstlane((int)(x - done));
-        n_q = span(a.cu_q, sequence, a.tokens_q, q_start);
-        n_k = span(a.cu_k, sequence, a.tokens_k, k_start);
+        auto uniform = [](int64_t v) {
+            return (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+                   (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+        };
+        sequence = __builtin_amdgcn_readfirstlane(found->sequence);
+        block = __builtin_amdgcn_readfirstlane(found->block);
+        n_q = __builtin_amdgcn_readfirstlane(found->n_q);
+        n_k = __builtin_amdgcn_readfirstlane(found->n_k);
+        q_start = uniform(found->q_start);
+        k_start = uniform(found->k_start);
         const int q_end = (block + 1) * kBM < n_q ? (block + 1) * kBM : n_q;
         const int keys = a.causal ? (q_end + n_k - n_q < n_k ? q_end + n_k - n_q : n_k) : n_k;
         steps = keys > 0 ? (keys + kBN - 1) / kBN : 0;
@@ -160,13 +181,13 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
     __shared__ __align__(16) uint16_t ks[2][kBN * D];
     __shared__ __align__(16) uint16_t vs[2][kBN * D];
     __shared__ uint32_t wave_total[kWaves];
-    __shared__ uint32_t before[64 * kWaves + 1];
+    __shared__ Block::Found found;
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     const uint32_t slot = blockIdx.x / (uint32_t)a.splits, split = blockIdx.x % (uint32_t)a.splits;
-    const Block bl(a, slot, wave_total, before);
+    const Block bl(a, slot, wave_total, &found);
     if (bl.sequence < 0) return;
     const int n_q = bl.n_q, n_k = bl.n_k, past = n_k - n_q, hq = bl.hq, hk = bl.hk;
     const int64_t q_start = bl.q_start, k_start = bl.k_start;
@@ -317,22 +338,23 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         s[1] = next[1];
     }
     l += other_half(l);
-    if (qi >= n_q) return;
     if (a.splits > 1) {
-        // a row's sums as they are, its maximum and its sum of weights
+        // the sums as the lanes hold them, whole lines at a time; then the rows'
+        // maxima and sums of weights
         float* part = a.parts + split * a.part_stride + (int64_t)slot * kBM * (D + 2);
-        float* dst = part + (wave * 32 + col) * D + 4 * half;
+        float4_t* dst = reinterpret_cast<float4_t*>(part) + wave * DT * 4 * 64 + lane;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<float4_t*>(dst + 32 * t + 2 * i) = float4_t{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+                dst[(t * 4 + i / 4) * 64] = float4_t{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
         if (half == 0) {
             part[kBM * D + wave * 32 + col] = m * a.scale2;
             part[kBM * (D + 1) + wave * 32 + col] = l;
         }
         return;
     }
+    if (qi >= n_q) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint16_t* dst = a.out + ((q_start + qi) * a.q_heads + hq) * (int64_t)D + 4 * half;
 #pragma unroll
@@ -345,31 +367,49 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
 }
 
 // Adds the parts of one block of queries in their order: workgroup (slot, y)
-// takes the block's rows 8 y .. 8 y + 7, a row every 32 threads.
+// takes 256 of the block's lanes' groups of four sums, one a thread.
 template <bool BF, int D>
 __global__ __launch_bounds__(64 * kWaves) void prompt_join_kernel(PromptArgs a) {
-    __shared__ uint32_t wave_total[kWaves], before[64 * kWaves + 1];
-    const Block bl(a, blockIdx.x, wave_total, before);
+    constexpr int DT = D / 32, AHEAD = 4;
+    __shared__ uint32_t wave_total[kWaves];
+    __shared__ Block::Found found;
+    const Block bl(a, blockIdx.x, wave_total, &found);
     if (bl.sequence < 0) return;
-    constexpr int VW = D / 32;            // neighbouring dims of a thread
-    typedef float vec_t __attribute__((ext_vector_type(VW)));
-    const int r = blockIdx.y * 8 + threadIdx.x / 32, d = threadIdx.x % 32 * VW, qi = bl.block * kBM + r;
+    const int x = blockIdx.y * 64 * kWaves + threadIdx.x, lane = x % 64, t = x / 256 % DT, i = x / 64 % 4;
+    const int r = x / (256 * DT) * 32 + lane % 32, qi = bl.block * kBM + r;
     if (qi >= bl.n_q) return;
     const float* part = a.parts + (int64_t)blockIdx.x * kBM * (D + 2);
     float top = -__builtin_inff(), sum = 0.f;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, part[s * a.part_stride + kBM * D + r]);
-    vec_t v = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float* p = part + s * a.part_stride;
-        const float ms = p[kBM * D + r];
-        const float f = ms == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ms - top);
-        sum = fmaf(p[kBM * (D + 1) + r], f, sum);
-        v += *reinterpret_cast<const vec_t*>(p + r * D + d) * f;
+    float4_t v = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < a.splits; s0 += AHEAD) {
+        float ms[AHEAD], ls[AHEAD];
+        float4_t vs[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const bool real = s0 + k < a.splits;
+            const float* p = part + (real ? s0 + k : s0) * a.part_stride;
+            ms[k] = real ? p[kBM * D + r] : -__builtin_inff();
+            ls[k] = p[kBM * (D + 1) + r];
+            vs[k] = reinterpret_cast<const float4_t*>(p)[x];
+        }
+        float next = top;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) next = fmaxf(next, ms[k]);
+        auto weight_of = [&](float m) { return m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - next); };
+        const float f = weight_of(top);
+        top = next;
+        sum *= f;
+        v *= f;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float e = weight_of(ms[k]);
+            sum = fmaf(ls[k], e, sum);
+            v += vs[k] * e;
+        }
     }
     v *= sum == 0.f ? 0.f : 1.f / sum;
-    uint16_t* dst = a.out + ((bl.q_start + qi) * a.q_heads + bl.hq) * (int64_t)D + d;
-#pragma unroll
-    for (int i = 0; i < VW; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = round_out2<BF>(v[i], v[i + 1]);
+    *reinterpret_cast<u32x2*>(a.out + ((bl.q_start + qi) * a.q_heads + bl.hq) * (int64_t)D + 32 * t + 8 * i +
+                              4 * (lane / 32)) = u32x2{round_out2<BF>(v[0], v[1]), round_out2<BF>(v[2], v[3])};
 }
 
 // Blocks of queries times heads, at most: the sum of ceil(n / kBM) over sequences.
@@ -404,7 +444,7 @@ int launch_prompt_attention(bool bf, const void* q, int64_t q_stride, const void
     const int64_t slots = most_slots(batch, tokens_q, q_heads);
     if (ws) a.splits = splits_for(slots, batch, tokens_k);
     a.part_stride = slots * kBM * (D + 2);
-    const dim3 grid((unsigned)(slots * a.splits)), join_grid((unsigned)slots, kBM / 8);
+    const dim3 grid((unsigned)(slots * a.splits)), join_grid((unsigned)slots, (unsigned)(kBM * D / 4 / (64 * kWaves)));
     auto go = [&](auto d) {
         constexpr int D_ = decltype(d)::value;
         const int rc = bf ? launch(prompt_attn_kernel<true, D_>, grid, dim3(64 * kWaves), 0, s, a)
