@@ -46,6 +46,11 @@ struct AttnArgs {
 template <bool BF> constexpr float kOffA = BF ? 128.f : 1024.f;   // nibbles 0, 2
 template <bool BF> constexpr float kOffB = BF ? 128.f : 64.f;     // nibbles 1, 3
 
+// The sums stay under an old maximum until the new one is 2^kSlack times it;
+// weights above 1 are as exact as those below, as long as a weight times a
+// value's scale (at most 2 * 65504 / 15 in fp16) is in range.
+template <bool BF> constexpr float kSlack = BF ? 8.f : 2.f;
+
 struct Magic { uint32_t a, b; };
 template <bool BF>
 __device__ __forceinline__ Magic magics(uint32_t sign) {
@@ -153,44 +158,51 @@ __device__ __forceinline__ const __attribute__((address_space(4))) int32_t* as_c
 // one length then end where shares do).
 struct Shares {
     const AttnArgs& a;
-    const uint32_t* before;               // LDS: units of one head before each thread's sequences
-    int seg;                              // sequences of a thread in `before`
+    int first_b, last_b;                  // this thread's sequences
+    uint32_t own_len, own, until;         // the last one's length; units of one head of them, and with all before
     uint32_t heads, total, wgs;
 
-    __device__ __forceinline__ static uint32_t length_of(const AttnArgs& a, int b) {
-        const int64_t n = a.lens[b];
+    __device__ __forceinline__ static uint32_t clamped(const AttnArgs& a, int64_t n) {
         return (uint32_t)(n < 0 ? 0 : n > a.capacity ? a.capacity : n);
     }
+    __device__ __forceinline__ static uint32_t length_of(const AttnArgs& a, int b) { return clamped(a, a.lens[b]); }
     // the same for a b that all lanes share
     __device__ __forceinline__ static uint32_t uniform_length(const AttnArgs& a, int b) {
-        const int64_t n = as_constant(a.lens)[b];
-        return (uint32_t)(n < 0 ? 0 : n > a.capacity ? a.capacity : n);
+        return clamped(a, as_constant(a.lens)[b]);
     }
     __device__ __forceinline__ static uint32_t rounds_of(uint32_t n) {
         return n == 0 ? 1u : (n + kRoundKeys - 1) / kRoundKeys;
     }
     __device__ __forceinline__ static uint32_t units_of(uint32_t n) { return kItemCost + rounds_of(n); }
-    // All kThreads threads; before: kThreads + 1 words of LDS, scratch: kWaves.
-    __device__ __forceinline__ Shares(const AttnArgs& args, uint32_t* lds, uint32_t* scratch) : a(args), before(lds) {
+    // All kThreads threads, each with its part of the sequences; scratch: kWaves
+    // words of LDS.
+    __device__ __forceinline__ Shares(const AttnArgs& args, uint32_t* scratch) : a(args), own_len(0), own(0) {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        seg = (a.batch + kThreads - 1) / kThreads;
-        uint32_t sum = 0;
-        for (int b = tid * seg; b < (tid + 1) * seg && b < a.batch; ++b) sum += units_of(length_of(a, b));
+        const int seg = (a.batch + kThreads - 1) / kThreads;
+        first_b = tid * seg;
+        last_b = first_b + seg < a.batch ? first_b + seg : a.batch;
+        for (int b = first_b; b < last_b; ++b) {
+            own_len = length_of(a, b);
+            own += units_of(own_len);
+        }
+        until = own;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(sum, d);
-            if (lane >= d) sum += o;
+            const uint32_t o = __shfl_up(until, d);
+            if (lane >= d) until += o;
         }
-        if (lane == 63) scratch[wave] = sum;
+        if (lane == 63) scratch[wave] = until;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) sum += scratch[w];
-        lds[tid + 1] = sum;
-        if (tid == 0) lds[0] = 0;
-        __syncthreads();
+        uint32_t all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) until += scratch[w];
+            all += scratch[w];
+        }
         heads = (uint32_t)a.cache.kv_heads * a.row_blocks;
-        total = lds[kThreads] * heads;
+        total = all * heads;
         const uint32_t items = heads * a.batch;
-        const uint32_t mean = (lds[kThreads] - kItemCost * a.batch) / a.batch;
+        const uint32_t mean = (all - kItemCost * a.batch) / a.batch;
         const uint32_t pieces = (mean + kLeastRounds - 1) / kLeastRounds;
         wgs = items < a.wgs && items * pieces < a.wgs ? items * (pieces ? pieces : 1) : a.wgs;
     }
@@ -200,23 +212,42 @@ struct Shares {
     __device__ __forceinline__ uint32_t owner(uint32_t x) const {
         return (uint32_t)((((uint64_t)x + 1) * wgs + total - 1) / total) - 1;
     }
-    // the sequence of unit x, and the units before its first
-    __device__ __forceinline__ int sequence(uint32_t x, uint32_t& seq_start) const {
+    struct Found { int32_t b; uint32_t start, len; };
+    // The sequence of unit x, the units (of all heads) before it and its length,
+    // told by the thread that has it.
+    __device__ __forceinline__ Found sequence_of_unit(uint32_t x, Found* lds) const {
         x /= heads;
-        // the last of the kThreads entries that is not above x: eight at a time, then one
-        const int lane = threadIdx.x & 63;
-        static_assert(kThreads == 512, "two steps of 64 and 8");
-        int s0 = 8 * (__popcll(__ballot(before[8 * lane] <= x)) - 1);
-        s0 += __popcll(__ballot(before[s0 + (lane & 7)] <= x) & 0xFF) - 1;
-        int b = __builtin_amdgcn_readfirstlane(s0 * seg);
-        uint32_t done = __builtin_amdgcn_readfirstlane(before[s0]);
-        for (;; ++b) {
-            const uint32_t n = units_of(uniform_length(a, b));
-            if (x < done + n) break;
-            done += n;
+        if (x < until && x >= until - own) {
+            Found f{first_b, until - own, own_len};
+            if (last_b - first_b > 1)
+                for (;; ++f.b) {
+                    f.len = length_of(a, f.b);
+                    const uint32_t n = units_of(f.len);
+                    if (x < f.start + n) break;
+                    f.start += n;
+                }
+            *lds = f;
         }
-        seq_start = done * heads;
-        return b;
+        return told(lds);
+    }
+    // The same for sequence b.
+    __device__ __forceinline__ Found sequence(int b, Found* lds) const {
+        if (b >= first_b && b < last_b) {
+            Found f{b, until - own, own_len};
+            if (last_b - first_b > 1) {
+                for (int i = first_b; i < b; ++i) f.start += units_of(length_of(a, i));
+                f.len = length_of(a, b);
+            }
+            *lds = f;
+        }
+        return told(lds);
+    }
+
+private:
+    __device__ __forceinline__ Found told(const Found* lds) const {
+        __syncthreads();
+        return {__builtin_amdgcn_readfirstlane(lds->b), (uint32_t)__builtin_amdgcn_readfirstlane(lds->start) * heads,
+                (uint32_t)__builtin_amdgcn_readfirstlane(lds->len)};
     }
 };
 
@@ -316,21 +347,24 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
     constexpr int kRingBytes = kWaves * RING * (int)TB, kSumBytes = kWaves * PASS * PITCH * 4;
     __shared__ __align__(1024) uint8_t pool[kRingBytes > kSumBytes ? kRingBytes : kSumBytes];
     float(*const acc)[PASS * PITCH] = reinterpret_cast<float(*)[PASS * PITCH]>(pool);
-    __shared__ uint32_t scratch[kWaves], before[kThreads + 1];
+    __shared__ uint32_t scratch[kWaves];
+    __shared__ Shares::Found found;
     __shared__ float ms[kWaves][ROWS], ls[kWaves][ROWS], fs[kWaves][ROWS], tops[ROWS];
     __shared__ u32x4 qs[NR][NW][64];
     __shared__ int last;
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Shares sh(a, before, scratch);
+    const Shares sh(a, scratch);
     const uint32_t wg = blockIdx.x;
     if (wg >= sh.wgs) return;
     uint32_t at = __builtin_amdgcn_readfirstlane(sh.begin_of(wg));
     const uint32_t end = __builtin_amdgcn_readfirstlane(sh.begin_of(wg + 1));
     if (at >= end) return;
-    uint32_t seq_start;                   // units (of all heads) before sequence b
-    int b = sh.sequence(at, seq_start);
+    const Shares::Found at_first = sh.sequence_of_unit(at, &found);
+    int b = at_first.b;
+    uint32_t seq_start = at_first.start;  // units (of all heads) before sequence b
+    uint32_t b_len = at_first.len;
 
     const uint32_t ring = lds_address(pool) + wave * RING * (uint32_t)TB;
     const uint32_t q_at = lds_address(qs) + lane * 16;
@@ -345,7 +379,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
 
     while (at < end) {
         // ---- the item at `at`
-        const uint32_t len = Shares::uniform_length(a, b);
+        const uint32_t len = b_len;
         const uint32_t n_rounds = Shares::rounds_of(len), n_units = Shares::units_of(len);
         const uint32_t item = (at - seq_start) / n_units;
         const uint32_t item_rounds = seq_start + item * n_units + kItemCost;      // unit of its first round
@@ -358,6 +392,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
         if (item + 1 == sh.heads && at == item_end) {
             seq_start += sh.heads * n_units;
             ++b;
+            if (at < end) b_len = Shares::uniform_length(a, b);
         }
         if (at <= item_rounds) continue;  // the share ends before the item's rounds
 
@@ -489,7 +524,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
 #pragma unroll
                     for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
                     top = max_over_groups(top);
-                    if (__any(top > m[n])) {
+                    // moved to a new maximum only where it outgrows the old one
+                    if (__any((top - m[n]) * a.scale2 > kSlack<BF> || (m[n] == -__builtin_inff() && top > m[n]))) {
                         const float f =
                             top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m[n] - top) * a.scale2);
                         m[n] = top;
@@ -653,17 +689,17 @@ template <bool BF, int D, int NR>
 __global__ __launch_bounds__(kThreads) void kv4_join_kernel(AttnArgs a) {
     constexpr int ROWS = 16 * NR, AHEAD = 4, SLICES = kThreads / 32;
     using P = Parts<D, ROWS>;
-    __shared__ uint32_t scratch[kWaves], before[kThreads + 1];
+    __shared__ uint32_t scratch[kWaves];
+    __shared__ Shares::Found found;
     __shared__ float4_t vals[SLICES][32];
     __shared__ float m8[SLICES][32], l8[SLICES][32];
-    const Shares sh(a, before, scratch);
+    const Shares sh(a, scratch);
     const int tid = threadIdx.x, slice = tid >> 5;
     const int b = blockIdx.x / sh.heads;
     const uint32_t item = blockIdx.x % sh.heads;
-    uint32_t seq_units = before[b / sh.seg];
-    for (int i = b / sh.seg * sh.seg; i < b; ++i) seq_units += Shares::units_of(Shares::uniform_length(a, i));
-    const uint32_t len = Shares::uniform_length(a, b), n_rounds = Shares::rounds_of(len);
-    const uint32_t item_rounds = seq_units * sh.heads + item * Shares::units_of(len) + kItemCost;
+    const Shares::Found seq = sh.sequence(b, &found);
+    const uint32_t n_rounds = Shares::rounds_of(seq.len);
+    const uint32_t item_rounds = seq.start + item * Shares::units_of(seq.len) + kItemCost;
     const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_rounds + n_rounds - 1);
     if (first == final) return;
     const int h = (int)(item / a.row_blocks), rb = (int)(item % a.row_blocks);
