@@ -161,6 +161,7 @@ struct Shares {
     int first_b, last_b;                  // this thread's sequences
     uint32_t own_len, own, until;         // the last one's length; units of one head of them, and with all before
     uint32_t heads, total, wgs;
+    uint32_t share, rest;                 // total / wgs and what that leaves
 
     __device__ __forceinline__ static uint32_t clamped(const AttnArgs& a, int64_t n) {
         return (uint32_t)(n < 0 ? 0 : n > a.capacity ? a.capacity : n);
@@ -205,12 +206,17 @@ struct Shares {
         const uint32_t mean = (all - kItemCost * a.batch) / a.batch;
         const uint32_t pieces = (mean + kLeastRounds - 1) / kLeastRounds;
         wgs = items < a.wgs && items * pieces < a.wgs ? items * (pieces ? pieces : 1) : a.wgs;
+        share = total / wgs;
+        rest = total % wgs;
     }
-    // floor(w total / wgs)
-    __device__ __forceinline__ uint32_t begin_of(uint32_t w) const { return (uint32_t)((uint64_t)w * total / wgs); }
+    // floor(w total / wgs) (w is at most kMostWgs and rest below it: 32 bits do)
+    __device__ __forceinline__ uint32_t begin_of(uint32_t w) const { return w * share + w * rest / wgs; }
     // the workgroup that takes unit x: the last w with begin_of(w) <= x
     __device__ __forceinline__ uint32_t owner(uint32_t x) const {
-        return (uint32_t)((((uint64_t)x + 1) * wgs + total - 1) / total) - 1;
+        uint32_t w = (uint32_t)((float)x * ((float)wgs / (float)total));      // one off at most
+        w = w < wgs ? w : wgs - 1;
+        if (begin_of(w) > x) return w - 1;
+        return w + 1 < wgs && begin_of(w + 1) <= x ? w + 1 : w;
     }
     struct Found { int32_t b; uint32_t start, len; };
     // The sequence of unit x, the units (of all heads) before it and its length,
@@ -337,7 +343,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
     // rows whose sums the waves add at a time, VW neighbouring dims a thread
     constexpr int VW = NR == 2 ? 4 : 2, PASS = VW * kThreads / D;
     typedef float vw_t __attribute__((ext_vector_type(VW)));
-    constexpr int PITCH = D + 4;
+    constexpr int PITCH = D + 16;         // neighbouring rows in other banks than a row's four lane groups
     constexpr int64_t TB = kv4_tile_bytes(D);
     using P = Parts<D, ROWS>;
     // Each wave keeps RING tiles in LDS, fetched by direct loads: what it
@@ -349,7 +355,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
     float(*const acc)[PASS * PITCH] = reinterpret_cast<float(*)[PASS * PITCH]>(pool);
     __shared__ uint32_t scratch[kWaves];
     __shared__ Shares::Found found;
-    __shared__ float ms[kWaves][ROWS], ls[kWaves][ROWS], fs[kWaves][ROWS], tops[ROWS];
+    __shared__ float ms[kWaves][ROWS], ls[kWaves][ROWS], tops[ROWS], sums[ROWS];
+    __shared__ __align__(16) float fs[ROWS][kWaves];
     __shared__ u32x4 qs[NR][NW][64];
     __shared__ int last;
 
@@ -396,6 +403,24 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
         }
         if (at <= item_rounds) continue;  // the share ends before the item's rounds
 
+        // The queries as the matrix cores take them (requested before anything
+        // waits for the page table), by way of LDS: the registers hold sums.
+        u32x4 q[NR][NW];
+        int limit[NR];                    // last visible position of the lane's row
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const int row = rb * ROWS + n * 16 + c;
+            const bool real = row < q_rows;
+            const int tq = real ? row / a.group : 0, hq = h * a.group + (real ? row - tq * a.group : 0);
+            const uint16_t* src = a.q + ((int64_t)this_b * a.q_len + tq) * a.q_stride + (int64_t)hq * D + g * (D / 4);
+            limit[n] = (int)len - a.q_len + tq;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                q[n][w] = *reinterpret_cast<const u32x4*>(src + 8 * w);
+                if (!real) q[n][w] = u32x4{0, 0, 0, 0};
+            }
+        }
+
         // ---- the wave's tiles: 8 r + wave for r0 <= r < r1, those that begin before len
         const uint32_t tiles = (len + kKvTile - 1) / kKvTile;
         // Table entries are read through the scalar cache, an iteration ahead: a
@@ -432,23 +457,14 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
         }
         entry = t + RING * kWaves < t_end ? entry_of(t + RING * kWaves) : -1;
 
-        // The queries as the matrix cores take them, in LDS (the registers hold
-        // sums and codes); wave n brings row tile n.
         float sum_q[NR], off_q[NR];
-        int limit[NR];                    // last visible position of the lane's row
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-            const int row = rb * ROWS + n * 16 + c;
-            const bool real = row < q_rows;
-            const int tq = real ? row / a.group : 0, hq = h * a.group + (real ? row - tq * a.group : 0);
-            const uint16_t* src = a.q + ((int64_t)this_b * a.q_len + tq) * a.q_stride + (int64_t)hq * D + g * (D / 4);
-            limit[n] = (int)len - a.q_len + tq;
             float sa = 0.f, sb = 0.f;
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                u32x4 v = *reinterpret_cast<const u32x4*>(src + 8 * w);
-                if (!real) v = u32x4{0, 0, 0, 0};
-                if (wave == n) qs[n][w][lane] = v;
+                const u32x4& v = q[n][w];
+                if (wave == n) qs[n][w][lane] = v;       // wave n brings row tile n
                 sa += meta_f32<BF>(v, 0) + meta_f32<BF>(v, 1) + meta_f32<BF>(v, 4) + meta_f32<BF>(v, 5);
                 sb += meta_f32<BF>(v, 2) + meta_f32<BF>(v, 3) + meta_f32<BF>(v, 6) + meta_f32<BF>(v, 7);
             }
@@ -595,41 +611,50 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             }
         }
         // ---- the waves' sums under a common maximum, PASS rows at a time
+        // (the thread's places are worked out here: held over the loop they would
+        // be spilled, and a reload waits for the stores before it)
+        int et = tid;
+        asm volatile("" : "+v"(et));
         const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
         const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_end - 1);
         float* const slot = P::at(a.parts, wg, first);
         lds_barrier();                    // the tiles are read; maxima and sums are there
         // what each wave's sums weigh under the common maximum
-        if (tid < kWaves * ROWS) {
-            const int w = tid / ROWS, r = tid % ROWS;
-            float top = ms[0][r];
+        if (et < ROWS) {
+            float top = ms[0][et], sum = 0.f;
 #pragma unroll
-            for (int i = 1; i < kWaves; ++i) top = fmaxf(top, ms[i][r]);
-            fs[w][r] = weight_of(ms[w][r], top);
-            if (w == 0) tops[r] = top;
+            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ms[w][et]);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = weight_of(ms[w][et], top);
+                fs[et][w] = f;
+                sum = fmaf(ls[w][et], f, sum);
+            }
+            tops[et] = top;
+            sums[et] = sum;
         }
         for (int row0 = 0; row0 < rows_here; row0 += PASS) {
             if (row0 > 0) lds_barrier();            // the rows before are read
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
-                const int r = n * 16 + c - row0;
+                const int r = n * 16 + (et & 15) - row0;
                 if (r < 0 || r >= PASS) continue;
-                float* dst = acc[wave] + r * PITCH + 4 * g;
+                float* dst = acc[wave] + r * PITCH + (et >> 4 & 3) * 4;
 #pragma unroll
                 for (int k = 0; k < NT; ++k) *reinterpret_cast<float4_t*>(dst + 16 * k) = o[n][k];
             }
             lds_barrier();
-            const int r = tid / (D / VW), d = tid % (D / VW) * VW, row = row0 + r;
+            const int r = et / (D / VW), d = et % (D / VW) * VW, row = row0 + r;
             if (row >= rows_here) continue;         // PASS * D / VW == kThreads
-            float sum = 0.f;
+            float f[kWaves];
+#pragma unroll
+            for (int w = 0; w < kWaves; w += 4)
+                *reinterpret_cast<float4_t*>(f + w) = *reinterpret_cast<const float4_t*>(&fs[row][w]);
             vw_t v = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float f = fs[w][row];
-                sum = fmaf(ls[w][row], f, sum);
-                v += *reinterpret_cast<const vw_t*>(acc[w] + r * PITCH + d) * f;
-            }
+            for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const vw_t*>(acc[w] + r * PITCH + d) * f[w];
             if (first == final) {
+                const float sum = sums[row];
                 v *= sum == 0.f ? 0.f : 1.f / sum;
                 uint16_t* dst = out_row<D>(a, this_b, h, rb * ROWS + row) + d;
 #pragma unroll
@@ -650,7 +675,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
                 }
                 if (d == 0) {
                     __hip_atomic_store(slot + ROWS * D + row, tops[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    __hip_atomic_store(slot + ROWS * (D + 1) + row, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_store(slot + ROWS * (D + 1) + row, sums[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 }
             }
         }
