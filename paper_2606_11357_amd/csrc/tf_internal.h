@@ -392,6 +392,25 @@ __device__ __forceinline__ void mfma_acc(float4_t& acc, const u32x4& a, const u3
     else
         asm("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
 }
+// v with the 16-lane (32-lane) rows of neighbours in place of its own, by row
+// swaps within the vector registers: swap16 gives lanes of rows 0, 1 both of
+// them, in either order (2, 3 alike), swap32 lanes of either half both halves.
+// (An element of the swap's result is copied before it is read as a float: a bit
+// cast straight from it reads element 0 whichever was named.)
+struct SwapPair { float a, b; };
+__device__ __forceinline__ SwapPair swap16(float v) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t a = r[0], b = r[1];
+    return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+__device__ __forceinline__ SwapPair swap32(float v) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    const uint32_t a = r[0], b = r[1];
+    return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+
 // 32 wait states, more than any matrix-instruction dependency requires.
 __device__ __forceinline__ void mfma_hazard_gap() {
     asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7\n\ts_nop 7");

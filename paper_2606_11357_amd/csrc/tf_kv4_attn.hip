@@ -46,11 +46,6 @@ struct AttnArgs {
 template <bool BF> constexpr float kOffA = BF ? 128.f : 1024.f;   // nibbles 0, 2
 template <bool BF> constexpr float kOffB = BF ? 128.f : 64.f;     // nibbles 1, 3
 
-// The sums stay under an old maximum until the new one is 2^kSlack times it;
-// weights above 1 are as exact as those below, as long as a weight times a
-// value's scale (at most 2 * 65504 / 15 in fp16) is in range.
-template <bool BF> constexpr float kSlack = BF ? 8.f : 2.f;
-
 struct Magic { uint32_t a, b; };
 template <bool BF>
 __device__ __forceinline__ Magic magics(uint32_t sign) {
@@ -77,18 +72,16 @@ __device__ __forceinline__ u32x4 code_pairs(uint32_t w, const Magic& m) {
     return o;
 }
 
-__device__ __forceinline__ float over_groups(float v) {       // sum over the four 16-lane groups
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+// Sum and maximum over the four 16-lane groups, the same in all of them.
+__device__ __forceinline__ float over_groups(float v) {
+    const SwapPair r = swap16(v);
+    const SwapPair h = swap32(r.a + r.b);
+    return h.a + h.b;
 }
-// max over the four 16-lane groups: swaps of 16- and 32-lane rows, no LDS
 __device__ __forceinline__ float max_over_groups(float v) {
-    const uint32_t a = __builtin_bit_cast(uint32_t, v);
-    const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-    v = fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
-    const uint32_t b = __builtin_bit_cast(uint32_t, v);
-    const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-    return fmaxf(__builtin_bit_cast(float, s[0]), __builtin_bit_cast(float, s[1]));
+    const SwapPair r = swap16(v);
+    const SwapPair h = swap32(fmaxf(r.a, r.b));
+    return fmaxf(h.a, h.b);
 }
 
 // 16-byte pieces of a lane's K (or V) codes, and word w of key half u in them
@@ -540,8 +533,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
 #pragma unroll
                     for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
                     top = max_over_groups(top);
-                    // moved to a new maximum only where it outgrows the old one
-                    if (__any((top - m[n]) * a.scale2 > kSlack<BF> || (m[n] == -__builtin_inff() && top > m[n]))) {
+                    if (__any(top > m[n])) {
                         const float f =
                             top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m[n] - top) * a.scale2);
                         m[n] = top;

@@ -39,13 +39,6 @@ struct PromptArgs {
     int64_t part_stride;               // floats of one part
 };
 
-// v of the lane 32 away
-__device__ __forceinline__ float other_half(float v) {
-    const uint32_t x = __builtin_bit_cast(uint32_t, v);
-    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return __builtin_bit_cast(float, threadIdx.x & 32 ? r[0] : r[1]);
-}
-
 template <bool BF>
 __device__ __forceinline__ float16_t mfma32(const u32x4& a, const u32x4& b, const float16_t& c) {
     if constexpr (BF)
@@ -295,7 +288,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-        top = fmaxf(top, other_half(top));
+        const SwapPair halves = swap32(top);
+        top = fmaxf(halves.a, halves.b);
         // The sums move to a new maximum only where it outgrows the old one by
         // 2^kSlack; until then weights above 1 are as exact as those below.
         if (__any((top - m) * a.scale2 > kSlack || (m == -__builtin_inff() && top > m))) {
@@ -337,7 +331,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         s[0] = next[0];
         s[1] = next[1];
     }
-    l += other_half(l);
+    const SwapPair sums = swap32(l);
+    l = sums.a + sums.b;
     if (a.splits > 1) {
         // the sums as the lanes hold them, whole lines at a time; then the rows'
         // maxima and sums of weights

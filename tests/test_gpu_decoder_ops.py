@@ -254,7 +254,7 @@ def check_decode(dt, got, q, k, v, lens, heads, new, scale=None):
             step = (np.ptp(kb, -1).max() / 15, np.ptp(vb, -1).max() / 15) if n else (0, 0)
             e = 2.0 ** -22 * scale * np.abs(q[b, :, h]).sum(-1, keepdims=True) * step[0] * (off + 30)
             tol = U[dt] * np.abs(want) + (2 * U[dt] + 2 * e) * bound + 2.0 ** -21 * off * step[1] + TINY[dt]
-            bad = np.abs(got[b, :, h] - want) > tol
+            bad = ~(np.abs(got[b, :, h] - want) <= tol)      # NaN is bad too
             assert not bad.any(), (b, n, h, np.abs(got[b, :, h] - want).max(), tol.min())
 
 
@@ -371,7 +371,7 @@ def check_prompt(dt, got, q, k, v, n_q, n_k, causal=True, scale=None):
             e = 2.0 ** -21 * scale * (np.abs(qb).sum(-1, keepdims=True) * np.abs(kb).max() if kb.size else 0)
             small = TINY[dt] * n_k[b] * (np.abs(vb).max() if vb.size else 0)
             tol = U[dt] * np.abs(want) + (U[dt] + 2 * e + 2.0 ** -20) * bound + small + TINY[dt]
-            bad = np.abs(got[cq[b]:cq[b + 1], h] - want) > tol
+            bad = ~(np.abs(got[cq[b]:cq[b + 1], h] - want) <= tol)      # NaN is bad too
             assert not bad.any(), (b, h, np.abs(got[cq[b]:cq[b + 1], h] - want).max())
 
 
