@@ -17,11 +17,11 @@ Kv4 kv4_view(const tf_kv4_cache& c);
 
 namespace {
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kRoundKeys = kKvTile * kWaves;   // keys of one round: a tile for each wave
 constexpr uint32_t kItemCost = 3;        // what beginning and ending an item costs, in rounds
-constexpr uint32_t kLeastRounds = 4;     // rounds of an item that one workgroup takes before a second helps
-constexpr int kMostWgs = 1024;           // workgroups of a launch, at most
+constexpr uint32_t kLeastRounds = 3;     // rounds of an item that one workgroup takes before a second helps
+constexpr uint32_t kFewParts = 16;       // parts that cost less to join than a second round of each
+constexpr int kMostWgs = 1024;           // workgroups of a launch, at most (and counters in the workspace)
+constexpr int kJoinThreads = 512;
 
 struct AttnArgs {
     Kv4 cache;
@@ -141,15 +141,18 @@ __device__ __forceinline__ const __attribute__((address_space(4))) int32_t* as_c
 }
 
 // How the rounds of all items are shared out.  An item is one (sequence,
-// key/value head, block of query rows); its rounds are 256 keys each, at least
-// one (which writes the zeros of an empty row), and it counts kItemCost units
-// of its own before them.  Workgroup w of `wgs` takes a contiguous share of all
+// key/value head, block of query rows); its rounds are 32 keys for each of W
+// waves, at least one (which writes the zeros of an empty row), and it counts
+// kItemCost units of its own before them.  Workgroup w of `wgs` takes a contiguous share of all
 // units, in the order of sequence, head and block, and shares differ by at most
 // one unit whatever the lengths are.  Where there are fewer items than
-// workgroups, no more of these work than give an item of average length
-// kLeastRounds rounds each: a few rounds cost less than joining parts (items of
-// one length then end where shares do).
+// workgroups, no more of these work than an item of average length is worth: one
+// where no item has more than kLeastRounds rounds (they cost less than joining
+// parts), else one a round, or one for two rounds past kFewParts (items of one
+// length then end where shares do).
+template <int W, int THREADS>
 struct Shares {
+    static constexpr int WAVES = THREADS / 64, KEYS = kKvTile * W;
     const AttnArgs& a;
     int first_b, last_b;                  // this thread's sequences
     uint32_t own_len, own, until;         // the last one's length; units of one head of them, and with all before
@@ -165,40 +168,46 @@ struct Shares {
         return clamped(a, as_constant(a.lens)[b]);
     }
     __device__ __forceinline__ static uint32_t rounds_of(uint32_t n) {
-        return n == 0 ? 1u : (n + kRoundKeys - 1) / kRoundKeys;
+        return n == 0 ? 1u : (n + KEYS - 1) / KEYS;
     }
     __device__ __forceinline__ static uint32_t units_of(uint32_t n) { return kItemCost + rounds_of(n); }
-    // All kThreads threads, each with its part of the sequences; scratch: kWaves
+    // All THREADS threads, each with its part of the sequences; scratch: WAVES
     // words of LDS.
     __device__ __forceinline__ Shares(const AttnArgs& args, uint32_t* scratch) : a(args), own_len(0), own(0) {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        const int seg = (a.batch + kThreads - 1) / kThreads;
+        const int seg = (a.batch + THREADS - 1) / THREADS;
         first_b = tid * seg;
         last_b = first_b + seg < a.batch ? first_b + seg : a.batch;
+        uint32_t longest = 0;
         for (int b = first_b; b < last_b; ++b) {
             own_len = length_of(a, b);
             own += units_of(own_len);
+            longest = own_len > longest ? own_len : longest;
         }
+        // units of all heads fit 31 bits: the 32nd carries whether an item is long
+        const uint32_t is_long = __any(longest > kLeastRounds * KEYS) ? 1u << 31 : 0;
         until = own;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t o = __shfl_up(until, d);
             if (lane >= d) until += o;
         }
-        if (lane == 63) scratch[wave] = until;
+        if (lane == 63) scratch[wave] = until | is_long;
         __syncthreads();
-        uint32_t all = 0;
+        uint32_t all = 0, any_long = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            if (w < wave) until += scratch[w];
-            all += scratch[w];
+        for (int w = 0; w < WAVES; ++w) {
+            const uint32_t n = scratch[w] & ~(1u << 31);
+            if (w < wave) until += n;
+            all += n;
+            any_long |= scratch[w] >> 31;
         }
         heads = (uint32_t)a.cache.kv_heads * a.row_blocks;
         total = all * heads;
         const uint32_t items = heads * a.batch;
         const uint32_t mean = (all - kItemCost * a.batch) / a.batch;
-        const uint32_t pieces = (mean + kLeastRounds - 1) / kLeastRounds;
-        wgs = items < a.wgs && items * pieces < a.wgs ? items * (pieces ? pieces : 1) : a.wgs;
+        const uint32_t pieces = !any_long ? 1 : mean <= kFewParts ? mean : (mean + 1) / 2;
+        wgs = items < a.wgs && items * pieces < a.wgs ? items * pieces : a.wgs;
         share = total / wgs;
         rest = total % wgs;
     }
@@ -324,17 +333,19 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // Waves that a SIMD holds, as the registers of the sums allow.
 constexpr int waves_per_simd(int D, int nr) { return D <= 128 && nr == 1 ? 4 : 2; }
 
-// One workgroup of eight waves on its share of the rounds (see Shares), a tile
-// for each wave a round.  Items that lie inside one share are written directly;
-// the others' partial sums go through the workspace, and the workgroup that
-// arrives last adds them in order (or kv4_join_kernel does).
-template <bool BF, int D, int NR>
-__global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kernel(AttnArgs a) {
+// One workgroup of W waves on its share of the rounds (see Shares), a tile for
+// each wave a round.  Items that lie inside one share are written directly; the
+// others' partial sums go through the workspace, and the workgroup that arrives
+// last adds them in order (or kv4_join_kernel does).
+template <bool BF, int D, int NR, int W>
+__global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel(AttnArgs a) {
+    constexpr int THREADS = 64 * W;
+    using Shares = tf::Shares<W, THREADS>;
     constexpr int NT = D / 16;            // 16-dim tiles of the output
     constexpr int NW = D / 32;            // words of codes per lane and key half
     constexpr int ROWS = 16 * NR;
     // rows whose sums the waves add at a time, VW neighbouring dims a thread
-    constexpr int VW = NR == 2 ? 4 : 2, PASS = VW * kThreads / D;
+    constexpr int VW = NR == 2 || D == 256 ? 4 : 2, PASS = VW * THREADS / D;
     typedef float vw_t __attribute__((ext_vector_type(VW)));
     constexpr int PITCH = D + 16;         // neighbouring rows in other banks than a row's four lane groups
     constexpr int64_t TB = kv4_tile_bytes(D);
@@ -343,13 +354,13 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
     // multiplies and RING - 1 on the way, without a register.  The same memory
     // takes the waves' sums once an item's tiles are done.
     constexpr int RING = D == 64 ? 4 : 2, LOADS = 2 * kPieces<D> + 1;
-    constexpr int kRingBytes = kWaves * RING * (int)TB, kSumBytes = kWaves * PASS * PITCH * 4;
+    constexpr int kRingBytes = W * RING * (int)TB, kSumBytes = W * PASS * PITCH * 4;
     __shared__ __align__(1024) uint8_t pool[kRingBytes > kSumBytes ? kRingBytes : kSumBytes];
     float(*const acc)[PASS * PITCH] = reinterpret_cast<float(*)[PASS * PITCH]>(pool);
-    __shared__ uint32_t scratch[kWaves];
-    __shared__ Shares::Found found;
-    __shared__ float ms[kWaves][ROWS], ls[kWaves][ROWS], tops[ROWS], sums[ROWS];
-    __shared__ __align__(16) float fs[ROWS][kWaves];
+    __shared__ uint32_t scratch[W];
+    __shared__ typename Shares::Found found;
+    __shared__ float ms[W][ROWS], ls[W][ROWS], tops[ROWS], sums[ROWS];
+    __shared__ __align__(16) float fs[ROWS][W];
     __shared__ u32x4 qs[NR][NW][64];
     __shared__ int last;
 
@@ -361,7 +372,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
     uint32_t at = __builtin_amdgcn_readfirstlane(sh.begin_of(wg));
     const uint32_t end = __builtin_amdgcn_readfirstlane(sh.begin_of(wg + 1));
     if (at >= end) return;
-    const Shares::Found at_first = sh.sequence_of_unit(at, &found);
+    const typename Shares::Found at_first = sh.sequence_of_unit(at, &found);
     int b = at_first.b;
     uint32_t seq_start = at_first.start;  // units (of all heads) before sequence b
     uint32_t b_len = at_first.len;
@@ -414,7 +425,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             }
         }
 
-        // ---- the wave's tiles: 8 r + wave for r0 <= r < r1, those that begin before len
+        // ---- the wave's tiles: W r + wave for r0 <= r < r1, those that begin before len
         const uint32_t tiles = (len + kKvTile - 1) / kKvTile;
         // Table entries are read through the scalar cache, an iteration ahead: a
         // vector load would wait in line behind the codes.  A tile without a
@@ -436,19 +447,19 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             for (int p = 0; p < 2 * kPieces<D>; ++p) direct_load16(tile + p * 1024 + off, dst + p * 1024);
             direct_load4(tile + 32 * D + lane * 4, dst + 32 * D);
         };
-        uint32_t t = kWaves * r0 + wave;
-        const uint32_t t_end = kWaves * r1 < tiles ? kWaves * r1 : tiles;
+        uint32_t t = W * r0 + wave;
+        const uint32_t t_end = W * r1 < tiles ? W * r1 : tiles;
         // Tiles are fetched RING - 1 ahead, and past the end some memory of the
         // cache, so that the number of loads in flight is always the same.
         bool found[RING];
         int32_t entry;
 #pragma unroll
         for (int i = 0; i < RING; ++i) {
-            const uint32_t ti = t + i * kWaves;
+            const uint32_t ti = t + i * W;
             entry = ti < t_end ? entry_of(ti) : -1;
             fetch(tile_at(ti, entry, found[i]), i);
         }
-        entry = t + RING * kWaves < t_end ? entry_of(t + RING * kWaves) : -1;
+        entry = t + RING * W < t_end ? entry_of(t + RING * W) : -1;
 
         float sum_q[NR], off_q[NR];
 #pragma unroll
@@ -457,7 +468,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 const u32x4& v = q[n][w];
-                if (wave == n) qs[n][w][lane] = v;       // wave n brings row tile n
+                if (wave == n % W) qs[n][w][lane] = v;   // wave n brings row tile n
                 sa += meta_f32<BF>(v, 0) + meta_f32<BF>(v, 1) + meta_f32<BF>(v, 4) + meta_f32<BF>(v, 5);
                 sb += meta_f32<BF>(v, 2) + meta_f32<BF>(v, 3) + meta_f32<BF>(v, 6) + meta_f32<BF>(v, 7);
             }
@@ -478,7 +489,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             for (int k = 0; k < NT; ++k) o[n][k] = float4_t{0.f, 0.f, 0.f, 0.f};
         }
 
-        for (uint32_t slot = 0; t < t_end; t += kWaves, slot = (slot + 1) % RING) {
+        for (uint32_t slot = 0; t < t_end; t += W, slot = (slot + 1) % RING) {
             const bool here = found[0];
             const uint32_t buf = ring + slot * (uint32_t)TB;
             asm volatile("s_waitcnt vmcnt(%0)" ::"i"((RING - 1) * LOADS) : "memory");     // this tile has landed
@@ -565,8 +576,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
                 // everything of the tile is in registers: its place takes another
 #pragma unroll
                 for (int i = 0; i + 1 < RING; ++i) found[i] = found[i + 1];
-                fetch(tile_at(t + RING * kWaves, entry, found[RING - 1]), slot);
-                if (t + (RING + 1) * kWaves < t_end) entry = entry_of(t + (RING + 1) * kWaves);
+                fetch(tile_at(t + RING * W, entry, found[RING - 1]), slot);
+                if (t + (RING + 1) * W < t_end) entry = entry_of(t + (RING + 1) * W);
                 else entry = -1;
 #pragma unroll
                 for (int n = 0; n < NR; ++n) osum[n] = mfma16<BF>(zrow, p[n], osum[n]);
@@ -615,9 +626,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
         if (et < ROWS) {
             float top = ms[0][et], sum = 0.f;
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ms[w][et]);
+            for (int w = 1; w < W; ++w) top = fmaxf(top, ms[w][et]);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < W; ++w) {
                 const float f = weight_of(ms[w][et], top);
                 fs[et][w] = f;
                 sum = fmaf(ls[w][et], f, sum);
@@ -637,14 +648,13 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
             }
             lds_barrier();
             const int r = et / (D / VW), d = et % (D / VW) * VW, row = row0 + r;
-            if (row >= rows_here) continue;         // PASS * D / VW == kThreads
-            float f[kWaves];
+            if (row >= rows_here) continue;         // PASS * D / VW == THREADS
+            float f[W];
 #pragma unroll
-            for (int w = 0; w < kWaves; w += 4)
-                *reinterpret_cast<float4_t*>(f + w) = *reinterpret_cast<const float4_t*>(&fs[row][w]);
+            for (int w = 0; w < W; ++w) f[w] = fs[row][w];
             vw_t v = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const vw_t*>(acc[w] + r * PITCH + d) * f[w];
+            for (int w = 0; w < W; ++w) v += *reinterpret_cast<const vw_t*>(acc[w] + r * PITCH + d) * f[w];
             if (first == final) {
                 const float sum = sums[row];
                 v *= sum == 0.f ? 0.f : 1.f / sum;
@@ -686,7 +696,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
                     return __builtin_bit_cast(float2_t, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p),
                                                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
                 };
-                for (int i = 2 * tid; i < rows_here * D; i += 2 * kThreads) {
+                for (int i = 2 * tid; i < rows_here * D; i += 2 * THREADS) {
                     const float2_t v = join_parts<D, ROWS>(a.parts, first, final, i / D, i % D, load2, load1);
                     *reinterpret_cast<uint32_t*>(out_row<D>(a, this_b, h, rb * ROWS + i / D) + i % D) =
                         round_out2<BF>(v[0], v[1]);
@@ -702,19 +712,20 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void kv4_attn_kern
 // The parts of items that several workgroups share, added by a launch of its
 // own: workgroup (i, y) takes 128 sums, from 128 y on, of item i, its 16
 // groups of 32 threads every sixteenth part each.
-template <bool BF, int D, int NR>
-__global__ __launch_bounds__(kThreads) void kv4_join_kernel(AttnArgs a) {
-    constexpr int ROWS = 16 * NR, AHEAD = 4, SLICES = kThreads / 32;
+template <bool BF, int D, int NR, int W>
+__global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(AttnArgs a) {
+    constexpr int ROWS = 16 * NR, AHEAD = 4, SLICES = kJoinThreads / 32;
+    using Shares = tf::Shares<W, kJoinThreads>;
     using P = Parts<D, ROWS>;
-    __shared__ uint32_t scratch[kWaves];
-    __shared__ Shares::Found found;
+    __shared__ uint32_t scratch[kJoinThreads / 64];
+    __shared__ typename Shares::Found found;
     __shared__ float4_t vals[SLICES][32];
     __shared__ float m8[SLICES][32], l8[SLICES][32];
     const Shares sh(a, scratch);
     const int tid = threadIdx.x, slice = tid >> 5;
     const int b = blockIdx.x / sh.heads;
     const uint32_t item = blockIdx.x % sh.heads;
-    const Shares::Found seq = sh.sequence(b, &found);
+    const typename Shares::Found seq = sh.sequence(b, &found);
     const uint32_t n_rounds = Shares::rounds_of(seq.len);
     const uint32_t item_rounds = seq.start + item * Shares::units_of(seq.len) + kItemCost;
     const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_rounds + n_rounds - 1);
@@ -774,15 +785,23 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(AttnArgs a) {
 
 // Rows per workgroup (16 or 32) and the blocks of them that q_rows need.
 int row_tiles(int q_rows) { return q_rows <= 16 ? 1 : 2; }
-// Workgroups that a compute unit holds on its four SIMDs.
-int wgs_per_cu(int D, int nr) { return waves_per_simd(D, nr) * 4 / kWaves; }
+// Workgroups of `waves` waves that a compute unit holds on its four SIMDs.
+int wgs_per_cu(int D, int nr, int waves) { return waves_per_simd(D, nr) * 4 / waves; }
+// Workgroups of a launch, at most: what 256 compute units hold, four waves each.
+int most_wgs(int D, int nr) { return kMostWgs / 4 * waves_per_simd(D, nr); }
+// Waves of a workgroup: eight, whose sums meet in LDS, where items are few; four
+// where there are two items and more a compute unit, so that more items are on
+// their way at once.  Measured (8 heads of 128, up to 300 keys, us, 8 -> 4 waves):
+// 32 sequences 12.0 -> 13.9, 64 16.9 -> 15.1, 128 23.6 -> 18.6; 32 heads, 128
+// sequences of up to 2000: 118 -> 90.
+int waves_for(int64_t items, int cus) { return items >= 2 * cus ? 4 : 8; }
 
 }  // namespace
 
 int64_t kv4_attention_workspace_bytes(int64_t batch, int q_len, int q_heads, int kv_heads, int D) {
     (void)batch;
     const int nr = row_tiles(q_len * (q_heads / kv_heads));
-    return align256(kMostWgs * 4) + align256((int64_t)kMostWgs * 2 * 16 * nr * (D + 2) * 4);
+    return align256(kMostWgs * 4) + align256((int64_t)most_wgs(D, nr) * 2 * 16 * nr * (D + 2) * 4);
 }
 
 int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride, const int32_t* lens, int64_t batch,
@@ -803,10 +822,12 @@ int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride,
     a.counters = static_cast<uint32_t*>(ws);
     a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(kMostWgs * 4));
     // no more workgroups than rounds there can be
-    const int64_t item_rounds = (a.capacity + kRoundKeys - 1) / kRoundKeys;
+    const int cus = device_cus(s);
     const int64_t items = batch * c.kv_heads * a.row_blocks;
-    int64_t wgs = (int64_t)device_cus(s) * wgs_per_cu(c.head_dim, nr);
-    if (wgs > kMostWgs) wgs = kMostWgs;
+    const int waves = waves_for(items, cus);
+    const int64_t item_rounds = (a.capacity + kKvTile * waves - 1) / (kKvTile * waves);
+    int64_t wgs = (int64_t)cus * wgs_per_cu(c.head_dim, nr, waves);
+    if (wgs > most_wgs(c.head_dim, nr)) wgs = most_wgs(c.head_dim, nr);
     if (wgs > items * item_rounds) wgs = items * item_rounds;
     a.wgs = (uint32_t)wgs;
     // Parts of one item, at most: as many as one long sequence among empty ones
@@ -817,12 +838,16 @@ int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride,
     const bool join = most * part_rows * c.head_dim * 4 > 256 * 1024 && items <= wgs;
     if (join) a.counters = nullptr;
     const dim3 grid((unsigned)wgs), join_grid((unsigned)items, (unsigned)((part_rows * c.head_dim + 127) / 128));
-    auto go = [&](auto d, auto n, auto bf) {
-        constexpr int D = decltype(d)::value, NR = decltype(n)::value;
+    auto go_waves = [&](auto d, auto n, auto bf, auto w) {
+        constexpr int D = decltype(d)::value, NR = decltype(n)::value, W = decltype(w)::value;
         constexpr bool BF = decltype(bf)::value;
-        const int rc = launch(kv4_attn_kernel<BF, D, NR>, grid, dim3(kThreads), 0, s, a);
+        const int rc = launch(kv4_attn_kernel<BF, D, NR, W>, grid, dim3(64 * W), 0, s, a);
         if (rc || !join) return rc;
-        return launch(kv4_join_kernel<BF, D, NR>, join_grid, dim3(kThreads), 0, s, a);
+        return launch(kv4_join_kernel<BF, D, NR, W>, join_grid, dim3(kJoinThreads), 0, s, a);
+    };
+    auto go = [&](auto d, auto n, auto bf) {
+        return waves == 8 ? go_waves(d, n, bf, std::integral_constant<int, 8>{})
+                          : go_waves(d, n, bf, std::integral_constant<int, 4>{});
     };
     auto by_rows = [&](auto d, auto bf) {
         return nr == 1 ? go(d, std::integral_constant<int, 1>{}, bf) : go(d, std::integral_constant<int, 2>{}, bf);
