@@ -53,14 +53,14 @@ struct RowQuant {
 // Every step is a rounded fp32 operation of its own (no contraction), so the
 // codes are those of the formula wherever it is computed in fp32.
 template <bool BF>
-__device__ __forceinline__ RowQuant row_quant(float lo, float hi, bool finite) {
+__device__ __forceinline__ RowQuant row_quant(float lo, float hi) {
 #pragma clang fp contract(off)
     RowQuant r;
     const float fifteenth = 1.0f / 15.0f;
     const float a = hi * fifteenth, b = lo * fifteenth;
     r.s16 = round_out<BF>(a - b);
     float s = scale_f32<BF>(r.s16);
-    if (!finite || !(s < __builtin_inff())) {
+    if (!(s < __builtin_inff())) {                    // a value that is not finite (hi = inf), or too large a range
         r.s16 = BF ? 0x7FC0 : 0x7E00;                 // NaN
         r.z16 = 0;
         r.inv = r.z = 0.f;
@@ -151,6 +151,7 @@ __device__ __forceinline__ void append_row(const AppendArgs& a, const Row& r, in
         *reinterpret_cast<u16x8*>(o) = oa;
         *reinterpret_cast<u16x8*>(o + D / 2) = ob;
     }
+    if (!__any(r.active && r.kind != 0 && r.known)) return;       // queries only
     // the row's range over its lanes
     float least = lo[0], most = lo[0], total = 0.f;
 #pragma unroll
@@ -159,13 +160,13 @@ __device__ __forceinline__ void append_row(const AppendArgs& a, const Row& r, in
         most = fmaxf(most, fmaxf(lo[j], hi[j]));
         total += (lo[j] - lo[j]) + (hi[j] - hi[j]);    // 0, or NaN where one is not finite
     }
+    if (!(total == 0.f)) most = __builtin_inff();
     least = -row_max<LPR>(-least);
     most = row_max<LPR>(most);
-    const bool finite = row_max<LPR>(total == 0.f ? 0.f : 1.f) == 0.f;
     if (!r.active || r.kind == 0 || !r.known) return;
     uint8_t* tile = tile_of();
     if (!tile) return;
-    const RowQuant rq = row_quant<BF>(least, most, finite);
+    const RowQuant rq = row_quant<BF>(least, most);
     uint32_t qa[8], qb[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
