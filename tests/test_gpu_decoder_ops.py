@@ -220,6 +220,56 @@ def test_append_out_of_place(tf):
         assert torch.equal(torch.isnan(t).all(-1).all(-1).cpu(), nowhere)
 
 
+@pytest.mark.parametrize("heads", [(8, 64), (5, 128), (2, 256)], ids=str)
+def test_reads_of_many_tokens_are_those_of_few(tf, heads):
+    """4 M values and more are read tile by tile, fewer row by row: the same
+    bits, from sequences that begin anywhere in a tile, empty ones, missing
+    pages, positions below 0 and tokens that no sequence owns."""
+    Hk, D = heads
+    rng = np.random.default_rng(D)
+    lens, starts = [4000, 0, 1, 37, 2500, 64, 90], [13, 5, 31, 32, 95, 0, -40]
+    lens[0] += max(0, -(-(1 << 22) // (Hk * D)) - sum(lens))
+    first, T = 3, sum(lens) + 3 + 45                    # unowned: 3 before the first, 45 behind the last
+    table, pages = table_for([max(0, s + n) for s, n in zip(starts, lens)], 64, rng)
+    table[0, 7], table[4, 1] = -1, pages                # missing; outside the pool
+    cache = tf.kv4_cache(pages, 64, Hk, D)
+    cu = i32(first + offsets(lens))
+    k, v = (torch.randn(T, Hk, D, device="cuda").half() for _ in range(2))
+    tf.kv4_append(cache, table, cu, i32(starts), k, v)
+    assert T * Hk * D >= 1 << 22
+    many = tf.kv4_read(cache, table, cu, i32(starts), T)
+    few = [torch.full_like(t, float("nan")) for t in many]
+    at = first
+    for b, n in enumerate(lens):
+        for i in range(0, n, 900):
+            m = min(900, n - i)
+            part = tf.kv4_read(cache, table[b:b + 1].contiguous(), i32([0, m]), i32([starts[b] + i]), m)
+            for whole, piece in zip(few, part):
+                whole[at + i:at + i + m] = piece
+        at += n
+    for a, b in zip(many, few):
+        assert torch.equal(torch.isnan(a), torch.isnan(b))
+        assert torch.equal(a.nan_to_num(), b.nan_to_num())
+    # unowned; page 7 of sequence 0; the 33 positions from 95 on page 1 of sequence 4; below 0
+    assert torch.isnan(many[0]).all(-1).all(-1).sum().item() == 3 + 45 + 64 + 33 + 40
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_append_and_read_of_many_sequences(tf, dt):
+    """More sequences than a workgroup keeps the offsets of (1100)."""
+    Hk, D = 2, 64
+    rng = np.random.default_rng(11)
+    lens, starts = rng.integers(0, 4, 1100).tolist(), rng.integers(0, 40, 1100).tolist()
+    T, cu = sum(lens), offsets(lens)
+    k, kv = up(rng.standard_normal((T, Hk, D)), dt)
+    v, vv = up(rng.standard_normal((T, Hk, D)), dt)
+    table, pages = table_for([s + n for s, n in zip(starts, lens)], 32, rng)
+    cache = tf.kv4_cache(pages, 32, Hk, D, dtype=DT[dt])
+    tf.kv4_append(cache, table, i32(cu), i32(starts), k, v)
+    for got, x in zip(tf.kv4_read(cache, table, i32(cu), i32(starts), T), (kv, vv)):
+        np.testing.assert_array_equal(down(got), oracle.round16(oracle.cached_rows(x.astype(np.float32), dt), dt))
+
+
 # ---------------------------------------------------------------------------
 # attention over the cache
 # ---------------------------------------------------------------------------
@@ -273,6 +323,39 @@ def test_decode(tf, dt, heads, lens, page, new):
     got = tf.kv4_attention(q, cache, table, i32(lens))
     check_decode(dt, down(got), qv, k, v, lens, heads, new)
     # the same from run to run, on the workspace that the first call left
+    assert torch.equal(got, tf.kv4_attention(q, cache, table, i32(lens)))
+
+
+# many items (512 and more: workgroups of four waves), of many sequences
+MANY = [((6, 6, 64), 90, 1), ((8, 4, 128), 130, 1), ((16, 2, 128), 260, 4), ((8, 1, 256), 520, 1),
+        ((8, 1, 256), 515, 4), ((16, 1, 64), 600, 2), ((5, 1, 128), 300, 8)]
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,batch,new", MANY, ids=str)
+def test_decode_of_many_sequences(tf, dt, heads, batch, new):
+    lens = np.random.default_rng(batch).integers(0, 120, batch).tolist()
+    lens[1], lens[batch // 2], lens[-1] = 0, 1300, 200
+    cache, table, k, v, rng = filled(tf, dt, heads, lens, 32, batch)
+    q, qv = up(rng.standard_normal((batch, new, heads[0], heads[2])), dt)
+    got = tf.kv4_attention(q, cache, table, i32(lens))
+    check_decode(dt, down(got), qv, k, v, lens, heads, new)
+    assert torch.equal(got, tf.kv4_attention(q, cache, table, i32(lens)))
+
+
+# long sequences whose parts are added by a launch of their own
+JOINED = [((8, 1, 256), [9000, 5], 4), ((16, 1, 64), [20000, 100], 2), ((16, 1, 128), [0, 9000, 40], 1),
+          ((32, 2, 128), [300, 9000], 1), ((5, 1, 256), [12, 4000, 9000], 8),
+          ((16, 1, 128), [40] * 300 + [6000] + [3] * 300, 1)]
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,lens,new", JOINED, ids=["256x4", "64x2", "128", "two heads", "40 rows", "many"])
+def test_decode_of_long_sequences(tf, dt, heads, lens, new):
+    cache, table, k, v, rng = filled(tf, dt, heads, lens, 64, len(lens) + new)
+    q, qv = up(rng.standard_normal((len(lens), new, heads[0], heads[2])), dt)
+    got = tf.kv4_attention(q, cache, table, i32(lens))
+    check_decode(dt, down(got), qv, k, v, lens, heads, new)
     assert torch.equal(got, tf.kv4_attention(q, cache, table, i32(lens)))
 
 
@@ -394,6 +477,21 @@ def test_prompt(tf, dt, causal, heads, n_q, n_k):
     v, vv = up(rng.standard_normal((sum(n_k), Hk, D)) + 0.5, dt)
     got = tf.prompt_attention(q, k, v, i32(offsets(n_q)), i32(offsets(n_k)), causal=causal)
     check_prompt(dt, down(got), qv, kv, vv, n_q, n_k, causal)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_prompt_of_many_sequences(tf, dt):
+    """More sequences than a workgroup has threads."""
+    heads = Hq, Hk, D = (2, 1, 64)
+    rng = np.random.default_rng(6)
+    n_q = rng.integers(0, 9, 700).tolist()
+    n_q[350] = 200
+    n_k = [n + int(p) for n, p in zip(n_q, rng.integers(0, 20, 700))]
+    q, qv = up(rng.standard_normal((sum(n_q), Hq, D)), dt)
+    k, kv = up(rng.standard_normal((sum(n_k), Hk, D)), dt)
+    v, vv = up(rng.standard_normal((sum(n_k), Hk, D)) + 0.5, dt)
+    got = tf.prompt_attention(q, k, v, i32(offsets(n_q)), i32(offsets(n_k)))
+    check_prompt(dt, down(got), qv, kv, vv, n_q, n_k)
 
 
 SPLITS = [((4, 1, 128), [70], [3000]), ((2, 2, 64), [1], [2049]), ((2, 1, 256), [40, 0, 129], [5000, 7, 1300]),
