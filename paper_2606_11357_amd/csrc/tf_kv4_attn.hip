@@ -23,17 +23,31 @@ constexpr uint32_t kFewParts = 16;       // parts that cost less to join than a 
 constexpr int kMostWgs = 1024;           // workgroups of a launch, at most (and counters in the workspace)
 constexpr int kJoinThreads = 512;
 
+// Division by a number that the host knows, of numbers below 2^31: with
+// 2^(s-1) < d <= 2^s and m = floor(2^(31+s) / d) + 1, n / d = n m >> 31 + s.
+struct Divisor {
+    uint32_t d = 1, m = 0, s = 0;
+    Divisor() = default;
+    explicit Divisor(uint32_t by) : d(by) {
+        while (d > 1u << s) ++s;
+        m = (uint32_t)(((uint64_t)1 << (31 + s)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (uint32_t)((uint64_t)n * m >> (31 + s)); }
+};
+
 struct AttnArgs {
     Kv4 cache;
     const uint16_t* q;
     int64_t q_stride;
     const int32_t* lens;
     int batch, q_len, group, row_blocks;  // group: query heads per key/value head
+    Divisor by_batch, by_group, by_row_blocks, by_heads, by_tiles;        // heads: of keys, times row_blocks; tiles: of a page
     uint32_t wgs;                         // workgroups that share the rounds
-    int64_t capacity;                     // positions a table row can hold
+    int32_t capacity;                     // positions a table row can hold
     float scale2;                         // softmax scale * log2(e)
     uint16_t* out;
-    uint32_t* counters;                   // null: kv4_join_kernel adds the parts
+    uint32_t* counters;                   // null: kv4_join_kernel adds the parts, as `spans` names them
+    uint32_t* spans;                      // first and last workgroup of each item, by the first one
     float* parts;
 };
 
@@ -83,6 +97,9 @@ __device__ __forceinline__ float max_over_groups(float v) {
     const SwapPair h = swap32(fmaxf(r.a, r.b));
     return fmaxf(h.a, h.b);
 }
+
+// What lane % 16 of the first group holds.
+__device__ __forceinline__ float of_group0(float v) { return swap32(swap16(v).a).a; }
 
 // 16-byte pieces of a lane's K (or V) codes, and word w of key half u in them
 // as kv4_word places it.
@@ -158,8 +175,9 @@ struct Shares {
     uint32_t own_len, own, until;         // the last one's length; units of one head of them, and with all before
     uint32_t heads, total, wgs;
     uint32_t share, rest;                 // total / wgs and what that leaves
+    float inv_wgs, wgs_per_unit;
 
-    __device__ __forceinline__ static uint32_t clamped(const AttnArgs& a, int64_t n) {
+    __device__ __forceinline__ static uint32_t clamped(const AttnArgs& a, int32_t n) {
         return (uint32_t)(n < 0 ? 0 : n > a.capacity ? a.capacity : n);
     }
     __device__ __forceinline__ static uint32_t length_of(const AttnArgs& a, int b) { return clamped(a, a.lens[b]); }
@@ -202,20 +220,34 @@ struct Shares {
             all += n;
             any_long |= scratch[w] >> 31;
         }
-        heads = (uint32_t)a.cache.kv_heads * a.row_blocks;
+        all = __builtin_amdgcn_readfirstlane(all);
+        heads = a.by_heads.d;
         total = all * heads;
         const uint32_t items = heads * a.batch;
-        const uint32_t mean = (all - kItemCost * a.batch) / a.batch;
-        const uint32_t pieces = !any_long ? 1 : mean <= kFewParts ? mean : (mean + 1) / 2;
+        uint32_t pieces = 1;
+        if (__builtin_amdgcn_readfirstlane(any_long)) {
+            const uint32_t mean = a.by_batch.of(all - kItemCost * a.batch);
+            pieces = mean <= kFewParts ? mean : (mean + 1) / 2;
+        }
         wgs = items < a.wgs && items * pieces < a.wgs ? items * pieces : a.wgs;
         share = total / wgs;
-        rest = total % wgs;
+        rest = total - share * wgs;
+        inv_wgs = __builtin_amdgcn_rcpf((float)wgs);
+        wgs_per_unit = (float)wgs * __builtin_amdgcn_rcpf((float)total);
     }
-    // floor(w total / wgs) (w is at most kMostWgs and rest below it: 32 bits do)
-    __device__ __forceinline__ uint32_t begin_of(uint32_t w) const { return w * share + w * rest / wgs; }
+    // n / d for quotients below 2^20, of which the approximation is one off at most
+    __device__ __forceinline__ static uint32_t small_quotient(uint32_t n, uint32_t d, float inv) {
+        const uint32_t q = (uint32_t)((float)n * inv);
+        const int32_t r = (int32_t)(n - q * d);
+        return r < 0 ? q - 1 : r >= (int32_t)d ? q + 1 : q;
+    }
+    // floor(w total / wgs) (w is at most kMostWgs and rest below it)
+    __device__ __forceinline__ uint32_t begin_of(uint32_t w) const {
+        return w * share + small_quotient(w * rest, wgs, inv_wgs);
+    }
     // the workgroup that takes unit x: the last w with begin_of(w) <= x
     __device__ __forceinline__ uint32_t owner(uint32_t x) const {
-        uint32_t w = (uint32_t)((float)x * ((float)wgs / (float)total));      // one off at most
+        uint32_t w = (uint32_t)((float)x * wgs_per_unit);                     // one off at most
         w = w < wgs ? w : wgs - 1;
         if (begin_of(w) > x) return w - 1;
         return w + 1 < wgs && begin_of(w + 1) <= x ? w + 1 : w;
@@ -224,7 +256,7 @@ struct Shares {
     // The sequence of unit x, the units (of all heads) before it and its length,
     // told by the thread that has it.
     __device__ __forceinline__ Found sequence_of_unit(uint32_t x, Found* lds) const {
-        x /= heads;
+        x = a.by_heads.of(x);
         if (x < until && x >= until - own) {
             Found f{first_b, until - own, own_len};
             if (last_b - first_b > 1)
@@ -234,18 +266,6 @@ struct Shares {
                     if (x < f.start + n) break;
                     f.start += n;
                 }
-            *lds = f;
-        }
-        return told(lds);
-    }
-    // The same for sequence b.
-    __device__ __forceinline__ Found sequence(int b, Found* lds) const {
-        if (b >= first_b && b < last_b) {
-            Found f{b, until - own, own_len};
-            if (last_b - first_b > 1) {
-                for (int i = first_b; i < b; ++i) f.start += units_of(length_of(a, i));
-                f.len = length_of(a, b);
-            }
             *lds = f;
         }
         return told(lds);
@@ -276,52 +296,61 @@ __device__ __forceinline__ float weight_of(float m, float to) {
     return m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - to);
 }
 
-// Adds the parts of workgroups first..final at two neighbouring sums of row r,
-// in their order, and returns the two outputs.  load2: two floats at an even
-// address.
-template <int D, int ROWS, typename Load2, typename Load1>
-__device__ __forceinline__ float2_t join_parts(float* parts, uint32_t first, uint32_t final, int r, int d, Load2 load2,
-                                               Load1 load1) {
+// Adds the parts of workgroups first..final, in their order, at U pairs of
+// neighbouring sums (d[u] of row r[u]), AHEAD parts at a time; v[u] are the
+// outputs.  load2: two floats at an even address.
+template <int D, int ROWS, int AHEAD, int U, typename Load2, typename Load1>
+__device__ __forceinline__ void join_parts(float* parts, uint32_t first, uint32_t final, const int (&r)[U],
+                                           const int (&d)[U], float2_t (&v)[U], Load2 load2, Load1 load1) {
     using P = Parts<D, ROWS>;
-    constexpr int AHEAD = 8;              // parts in flight
-    float top = -__builtin_inff(), sum = 0.f;
-    float2_t v = {0.f, 0.f};
+    float top[U], sum[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        top[u] = -__builtin_inff();
+        sum[u] = 0.f;
+        v[u] = float2_t{0.f, 0.f};
+    }
     for (uint32_t w0 = first; w0 <= final; w0 += AHEAD) {
-        float mw[AHEAD], lw[AHEAD];
-        float2_t vw[AHEAD];
+        float mw[U][AHEAD], lw[U][AHEAD];
+        float2_t vw[U][AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const uint32_t w = w0 + i <= final ? w0 + i : final;
-            const float* p = P::at(parts, w, first);
-            mw[i] = load1(p + ROWS * D + r);
-            lw[i] = load1(p + ROWS * (D + 1) + r);
-            vw[i] = load2(p + r * D + d);
-        }
-        float next = top;
+            const float* p = P::at(parts, w0 + i <= final ? w0 + i : final, first);
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (w0 + i <= final) next = fmaxf(next, mw[i]);
-        const float f = weight_of(top, next);
-        top = next;
-        sum *= f;
-        v *= f;
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (w0 + i <= final) {
-                const float e = weight_of(mw[i], top);
-                sum = fmaf(lw[i], e, sum);
-                v[0] = fmaf(vw[i][0], e, v[0]);
-                v[1] = fmaf(vw[i][1], e, v[1]);
+            for (int u = 0; u < U; ++u) {
+                mw[u][i] = load1(p + ROWS * D + r[u]);
+                lw[u][i] = load1(p + ROWS * (D + 1) + r[u]);
+                vw[u][i] = load2(p + r[u] * D + d[u]);
             }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float next = top[u];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (w0 + i <= final) next = fmaxf(next, mw[u][i]);
+            const float f = weight_of(top[u], next);
+            top[u] = next;
+            sum[u] *= f;
+            v[u] *= f;
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (w0 + i <= final) {
+                    const float e = weight_of(mw[u][i], next);
+                    sum[u] = fmaf(lw[u][i], e, sum[u]);
+                    v[u][0] = fmaf(vw[u][i][0], e, v[u][0]);
+                    v[u][1] = fmaf(vw[u][i][1], e, v[u][1]);
+                }
+        }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    return float2_t{v[0] * inv, v[1] * inv};
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] *= sum[u] == 0.f ? 0.f : 1.f / sum[u];
 }
 
 // Output row `row` (of the q_len * group that read one head) of an item.
 template <int D>
 __device__ __forceinline__ uint16_t* out_row(const AttnArgs& a, int b, int h, int row) {
-    const int tq = row / a.group;
+    const int tq = (int)a.by_group.of(row);
     return a.out + ((int64_t)b * a.q_len + tq) * ((int64_t)a.cache.kv_heads * a.group * D) +
            (int64_t)(h * a.group + row - tq * a.group) * D;
 }
@@ -329,6 +358,21 @@ __device__ __forceinline__ uint16_t* out_row(const AttnArgs& a, int b, int h, in
 // A barrier for what the workgroup shares in LDS: unlike __syncthreads it does
 // not wait for stores to memory.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Half of 2 N groups of four sums goes to the wave that keeps that half, and this
+// wave adds what that one holds of its own half.
+template <int N>
+__device__ __forceinline__ void exchange(float4_t* v, bool upper, float4_t* out, const float4_t* in) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float4_t lo = v[i], hi = v[N + i];
+        out[i * 64] = upper ? lo : hi;
+        v[i] = upper ? hi : lo;
+    }
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += in[i * 64];
+}
 
 // Waves that a SIMD holds, as the registers of the sums allow.
 constexpr int waves_per_simd(int D, int nr) { return D <= 128 && nr == 1 ? 4 : 2; }
@@ -344,23 +388,21 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
     constexpr int NT = D / 16;            // 16-dim tiles of the output
     constexpr int NW = D / 32;            // words of codes per lane and key half
     constexpr int ROWS = 16 * NR;
-    // rows whose sums the waves add at a time, VW neighbouring dims a thread
-    constexpr int VW = NR == 2 || D == 256 ? 4 : 2, PASS = VW * THREADS / D;
-    typedef float vw_t __attribute__((ext_vector_type(VW)));
-    constexpr int PITCH = D + 16;         // neighbouring rows in other banks than a row's four lane groups
+    constexpr int SUMS = NR * NT;         // groups of four sums of a lane, and what a wave keeps of them
+    constexpr int KEEP = SUMS >= W ? SUMS / W : 1;
     constexpr int64_t TB = kv4_tile_bytes(D);
     using P = Parts<D, ROWS>;
     // Each wave keeps RING tiles in LDS, fetched by direct loads: what it
     // multiplies and RING - 1 on the way, without a register.  The same memory
     // takes the waves' sums once an item's tiles are done.
     constexpr int RING = D == 64 ? 4 : 2, LOADS = 2 * kPieces<D> + 1;
-    constexpr int kRingBytes = W * RING * (int)TB, kSumBytes = W * PASS * PITCH * 4;
-    __shared__ __align__(1024) uint8_t pool[kRingBytes > kSumBytes ? kRingBytes : kSumBytes];
-    float(*const acc)[PASS * PITCH] = reinterpret_cast<float(*)[PASS * PITCH]>(pool);
+    constexpr int kRingBytes = W * RING * (int)TB, kSumBytes = SUMS / 2 * 1024;
+    static_assert(W * kSumBytes <= kRingBytes, "the waves' sums fit the ring");
+    __shared__ __align__(1024) uint8_t pool[kRingBytes];
     __shared__ uint32_t scratch[W];
     __shared__ typename Shares::Found found;
-    __shared__ float ms[W][ROWS], ls[W][ROWS], tops[ROWS], sums[ROWS];
-    __shared__ __align__(16) float fs[ROWS][W];
+    __shared__ __align__(16) float ms[ROWS][W], ls[ROWS][W];
+    __shared__ __align__(16) float2_t q_sums[NR][16][NW];
     __shared__ u32x4 qs[NR][NW][64];
     __shared__ int last;
 
@@ -392,9 +434,9 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
         // ---- the item at `at`
         const uint32_t len = b_len;
         const uint32_t n_rounds = Shares::rounds_of(len), n_units = Shares::units_of(len);
-        const uint32_t item = (at - seq_start) / n_units;
+        const uint32_t item = Shares::small_quotient(at - seq_start, n_units, __builtin_amdgcn_rcpf((float)n_units));
         const uint32_t item_rounds = seq_start + item * n_units + kItemCost;      // unit of its first round
-        const int h = (int)(item / a.row_blocks), rb = (int)(item % a.row_blocks);
+        const int h = (int)a.by_row_blocks.of(item), rb = (int)item - h * a.row_blocks;
         const uint32_t r0 = at > item_rounds ? at - item_rounds : 0;
         const uint32_t item_end = item_rounds + n_rounds;
         const uint32_t r1 = (end < item_end ? end : item_end) - item_rounds;
@@ -407,22 +449,28 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
         }
         if (at <= item_rounds) continue;  // the share ends before the item's rounds
 
-        // The queries as the matrix cores take them (requested before anything
-        // waits for the page table), by way of LDS: the registers hold sums.
-        u32x4 q[NR][NW];
+        // The queries as the matrix cores take them, by way of LDS, each wave some of
+        // their words: a word of 16 rows lies in 64 lines, and all waves asking for
+        // all words cost 4 us of 30 (32 rows of 256).  Requested before anything
+        // waits for the page table.
         int limit[NR];                    // last visible position of the lane's row
+        const uint16_t* q_src[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             const int row = rb * ROWS + n * 16 + c;
             const bool real = row < q_rows;
-            const int tq = real ? row / a.group : 0, hq = h * a.group + (real ? row - tq * a.group : 0);
-            const uint16_t* src = a.q + ((int64_t)this_b * a.q_len + tq) * a.q_stride + (int64_t)hq * D + g * (D / 4);
+            const int tq = real ? (int)a.by_group.of(row) : 0, hq = h * a.group + (real ? row - tq * a.group : 0);
+            q_src[n] = a.q + ((int64_t)this_b * a.q_len + tq) * a.q_stride + (int64_t)hq * D + g * (D / 4);
             limit[n] = (int)len - a.q_len + tq;
+        }
+        constexpr int WORDS = NR * NW, OWN = (WORDS + W - 1) / W;
+        u32x4 q[OWN];
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                q[n][w] = *reinterpret_cast<const u32x4*>(src + 8 * w);
-                if (!real) q[n][w] = u32x4{0, 0, 0, 0};
-            }
+        for (int i = 0; i < OWN; ++i) {
+            const int x = wave + i * W, n = x / NW;
+            q[i] = u32x4{0, 0, 0, 0};
+            if (x < WORDS && rb * ROWS + n * 16 + c < q_rows)
+                q[i] = *reinterpret_cast<const u32x4*>((NR == 2 && n ? q_src[NR - 1] : q_src[0]) + 8 * (x % NW));
         }
 
         // ---- the wave's tiles: W r + wave for r0 <= r < r1, those that begin before len
@@ -430,13 +478,13 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
         // Table entries are read through the scalar cache, an iteration ahead: a
         // vector load would wait in line behind the codes.  A tile without a
         // page is some memory of the cache, and every key of it hidden.
-        const uint32_t page_tiles = (uint32_t)a.cache.tiles;
         const auto* row = as_constant(a.cache.table) + this_b * a.cache.table_stride;
-        auto entry_of = [&](uint32_t t) { return row[t / page_tiles]; };
+        auto entry_of = [&](uint32_t t) { return row[a.by_tiles.of(t)]; };
         auto tile_at = [&](uint32_t t, int32_t page, bool& found) {
             found = page >= 0 && page < a.cache.pages;
+            const uint32_t in_page = t - a.by_tiles.of(t) * a.by_tiles.d;
             const uint8_t* p = a.cache.data + (found ? (int64_t)page * a.cache.page_bytes +
-                                                           ((int64_t)h * page_tiles + t % page_tiles) * TB : 0);
+                                                           ((int64_t)h * a.by_tiles.d + in_page) * TB : 0);
             asm("" : "+s"(p));            // in scalar registers, the lanes' offsets beside it
             return (GlobalBytes)(uintptr_t)p;
         };
@@ -461,24 +509,36 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
         }
         entry = t + RING * W < t_end ? entry_of(t + RING * W) : -1;
 
+        const uint32_t first = __builtin_amdgcn_readfirstlane(sh.owner(item_rounds));
+        const uint32_t final = __builtin_amdgcn_readfirstlane(sh.owner(item_end - 1));
+
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            const int x = wave + i * W, n = x / NW, w = x % NW;
+            if (x >= WORDS) continue;
+            const u32x4& v = q[i];
+            qs[n][w][lane] = v;
+            const float sa = meta_f32<BF>(v, 0) + meta_f32<BF>(v, 1) + meta_f32<BF>(v, 4) + meta_f32<BF>(v, 5);
+            const float sb = meta_f32<BF>(v, 2) + meta_f32<BF>(v, 3) + meta_f32<BF>(v, 6) + meta_f32<BF>(v, 7);
+            const float2_t both = {over_groups(sa), over_groups(sb)};
+            if (g == 0) q_sums[n][c][w] = both;
+        }
+        lds_barrier();
         float sum_q[NR], off_q[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
+            u32x4 x[NW / 2];
+            lds_read<NW / 2, 16>(x, lds_address(q_sums[n][c]));
             float sa = 0.f, sb = 0.f;
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const u32x4& v = q[n][w];
-                if (wave == n % W) qs[n][w][lane] = v;   // wave n brings row tile n
-                sa += meta_f32<BF>(v, 0) + meta_f32<BF>(v, 1) + meta_f32<BF>(v, 4) + meta_f32<BF>(v, 5);
-                sb += meta_f32<BF>(v, 2) + meta_f32<BF>(v, 3) + meta_f32<BF>(v, 6) + meta_f32<BF>(v, 7);
+                sa += __builtin_bit_cast(float, (uint32_t)x[w / 2][2 * (w % 2)]);
+                sb += __builtin_bit_cast(float, (uint32_t)x[w / 2][2 * (w % 2) + 1]);
             }
-            sa = over_groups(sa);
-            sb = over_groups(sb);
             sum_q[n] = sa + sb;
             off_q[n] = sa * kOffA<BF> + sb * kOffB<BF>;
         }
-        lds_barrier();
-        float4_t o[NR][NT], osum[NR];     // osum: rows 0..2 of the further operand
+        float4_t o[SUMS], osum[NR];       // osum: rows 0..2 of the further operand
         float m[NR], l[NR];               // maximum of scale-free scores; sum of weights
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -486,7 +546,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
             l[n] = 0.f;
             osum[n] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < NT; ++k) o[n][k] = float4_t{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < NT; ++k) o[n * NT + k] = float4_t{0.f, 0.f, 0.f, 0.f};
         }
 
         for (uint32_t slot = 0; t < t_end; t += W, slot = (slot + 1) % RING) {
@@ -551,7 +611,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
                         l[n] *= f;
                         osum[n] *= f;
 #pragma unroll
-                        for (int k = 0; k < NT; ++k) o[n][k] *= f;
+                        for (int k = 0; k < NT; ++k) o[n * NT + k] *= f;
                     }
                     const float base = m[n] == -__builtin_inff() ? 0.f : m[n] * a.scale2;
 #pragma unroll
@@ -588,8 +648,8 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
                     const u32x4 lo{a0[0], a0[2], a1[0], a1[2]}, hi{a0[1], a0[3], a1[1], a1[3]};
 #pragma unroll
                     for (int n = 0; n < NR; ++n) {
-                        o[n][w] = mfma16<BF>(lo, p[n], o[n][w]);
-                        o[n][NW + w] = mfma16<BF>(hi, p[n], o[n][NW + w]);
+                        o[n * NT + w] = mfma16<BF>(lo, p[n], o[n * NT + w]);
+                        o[n * NT + NW + w] = mfma16<BF>(hi, p[n], o[n * NT + NW + w]);
                     }
                 }
             }
@@ -601,85 +661,108 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
         for (int n = 0; n < NR; ++n) {
             l[n] = over_groups(l[n]);
             // the three sums of column c are in lane c (group 0)
-            const float z = __shfl(osum[n][0], c);
-            const float ca = z + __shfl(osum[n][1], c), cb = z + __shfl(osum[n][2], c);
+            const float z = of_group0(osum[n][0]);
+            const float ca = z + of_group0(osum[n][1]), cb = z + of_group0(osum[n][2]);
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                o[n][w] -= ca;
-                o[n][NW + w] -= cb;
+                o[n * NT + w] -= ca;
+                o[n * NT + NW + w] -= cb;
             }
             if (g == 0) {
-                ms[wave][n * 16 + c] = m[n] * a.scale2;
-                ls[wave][n * 16 + c] = l[n];
+                ms[n * 16 + c][wave] = m[n] * a.scale2;
+                ls[n * 16 + c][wave] = l[n];
             }
         }
-        // ---- the waves' sums under a common maximum, PASS rows at a time
-        // (the thread's places are worked out here: held over the loop they would
-        // be spilled, and a reload waits for the stores before it)
-        int et = tid;
-        asm volatile("" : "+v"(et));
-        const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
-        const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_end - 1);
-        float* const slot = P::at(a.parts, wg, first);
+        // ---- the waves' sums under a common maximum: each wave keeps its W-th of
+        // them, halving what it holds with one wave after another
         lds_barrier();                    // the tiles are read; maxima and sums are there
-        // what each wave's sums weigh under the common maximum
-        if (et < ROWS) {
-            float top = ms[0][et], sum = 0.f;
+        float tops[NR], sums[NR];
 #pragma unroll
-            for (int w = 1; w < W; ++w) top = fmaxf(top, ms[w][et]);
+        for (int n = 0; n < NR; ++n) {
+            const float *mr = ms[n * 16 + c], *lr = ls[n * 16 + c];
+            float mw[W], lw[W];
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                const float f = weight_of(ms[w][et], top);
-                fs[et][w] = f;
-                sum = fmaf(ls[w][et], f, sum);
+                mw[w] = mr[w];
+                lw[w] = lr[w];
             }
-            tops[et] = top;
-            sums[et] = sum;
+            tops[n] = mw[0];
+#pragma unroll
+            for (int w = 1; w < W; ++w) tops[n] = fmaxf(tops[n], mw[w]);
+            sums[n] = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) sums[n] = fmaf(lw[w], weight_of(mw[w], tops[n]), sums[n]);
+            const float f = weight_of(m[n] * a.scale2, tops[n]);
+#pragma unroll
+            for (int k = 0; k < NT; ++k) o[n * NT + k] *= f;
         }
-        for (int row0 = 0; row0 < rows_here; row0 += PASS) {
-            if (row0 > 0) lds_barrier();            // the rows before are read
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                const int r = n * 16 + (et & 15) - row0;
-                if (r < 0 || r >= PASS) continue;
-                float* dst = acc[wave] + r * PITCH + (et >> 4 & 3) * 4;
-#pragma unroll
-                for (int k = 0; k < NT; ++k) *reinterpret_cast<float4_t*>(dst + 16 * k) = o[n][k];
+        // What wave w writes only the wave it exchanges with reads, which writes
+        // its next half in the same place: one barrier an exchange.
+        auto sums_of = [&](int w) { return reinterpret_cast<float4_t*>(pool + w * kSumBytes) + lane; };
+        exchange<SUMS / 2>(o, wave & W / 2, sums_of(wave), sums_of(wave ^ W / 2));
+        if constexpr (W == 8) {
+            exchange<SUMS / 4>(o, wave & 2, sums_of(wave ^ 4), sums_of(wave ^ 6));
+            if constexpr (SUMS >= 8) {
+                exchange<SUMS / 8>(o, wave & 1, sums_of(wave ^ 6), sums_of(wave ^ 7));
+            } else {                      // half of the four sums that are left
+                const float4_t v = o[0];
+                float2_t* mine = reinterpret_cast<float2_t*>(sums_of(wave ^ 6));
+                *mine = wave & 1 ? float2_t{v[0], v[1]} : float2_t{v[2], v[3]};
+                lds_barrier();
+                const float2_t other = *reinterpret_cast<const float2_t*>(sums_of(wave ^ 7));
+                o[0][0] = (wave & 1 ? v[2] : v[0]) + other[0];
+                o[0][1] = (wave & 1 ? v[3] : v[1]) + other[1];
             }
-            lds_barrier();
-            const int r = et / (D / VW), d = et % (D / VW) * VW, row = row0 + r;
-            if (row >= rows_here) continue;         // PASS * D / VW == THREADS
-            float f[W];
+        } else {
+            exchange<SUMS / 4>(o, wave & 1, sums_of(wave ^ 2), sums_of(wave ^ 3));
+        }
+        // the wave's sums: KEEP groups of four (or half of one) of one row a lane
+        constexpr int VALUES = 4 * SUMS / W < 4 ? 2 : 4;
+        const int kept_at = wave * (4 * SUMS / W), kept_n = kept_at / (4 * NT);
+        const int r = kept_n * 16 + c, d0 = kept_at % (4 * NT) / 4 * 16 + 4 * g + kept_at % 4;
+        const int rows_here = q_rows - rb * ROWS < ROWS ? q_rows - rb * ROWS : ROWS;
+        float* const slot = P::at(a.parts, wg, first);
+        if (r < rows_here && first == final) {
+            const float sum = NR == 2 && kept_n ? sums[NR - 1] : sums[0], inv = sum == 0.f ? 0.f : 1.f / sum;
+            uint16_t* dst = out_row<D>(a, this_b, h, rb * ROWS + r) + d0;
 #pragma unroll
-            for (int w = 0; w < W; ++w) f[w] = fs[row][w];
-            vw_t v = 0.f;
+            for (int i = 0; i < KEEP; ++i) {
+                const float4_t v = o[i] * inv;
+                if constexpr (VALUES == 4)
+                    *reinterpret_cast<u32x2*>(dst + 16 * i) =
+                        u32x2{round_out2<BF>(v[0], v[1]), round_out2<BF>(v[2], v[3])};
+                else
+                    *reinterpret_cast<uint32_t*>(dst) = round_out2<BF>(v[0], v[1]);
+            }
+        } else if (r < rows_here) {
+            // Where the last workgroup adds the parts, they and the counters are
+            // touched only by agent-scope atomic accesses, which pass the per-XCD L2,
+            // and the stores complete before the arrival is counted.
+            float* dst = slot + r * D + d0;
 #pragma unroll
-            for (int w = 0; w < W; ++w) v += *reinterpret_cast<const vw_t*>(acc[w] + r * PITCH + d) * f[w];
-            if (first == final) {
-                const float sum = sums[row];
-                v *= sum == 0.f ? 0.f : 1.f / sum;
-                uint16_t* dst = out_row<D>(a, this_b, h, rb * ROWS + row) + d;
+            for (int i = 0; i < KEEP; ++i) {
+                if (a.counters || VALUES == 2) {
 #pragma unroll
-                for (int i = 0; i < VW; i += 2)
-                    *reinterpret_cast<uint32_t*>(dst + i) = round_out2<BF>(v[i], v[i + 1]);
-            } else {
-                // Where the last workgroup adds the parts, they and the counters
-                // are touched only by agent-scope atomic accesses, which pass the
-                // per-XCD L2, and the stores complete before the arrival is counted.
-                if (a.counters) {
-#pragma unroll
-                    for (int i = 0; i < VW; i += 2)
-                        __hip_atomic_store(reinterpret_cast<uint64_t*>(slot + row * D + d + i),
-                                           __builtin_bit_cast(uint64_t, float2_t{v[i], v[i + 1]}), __ATOMIC_RELAXED,
-                                           __HIP_MEMORY_SCOPE_AGENT);
+                    for (int j = 0; j < VALUES; j += 2)
+                        __hip_atomic_store(reinterpret_cast<uint64_t*>(dst + 16 * i + j),
+                                           __builtin_bit_cast(uint64_t, float2_t{o[i][j], o[i][j + 1]}),
+                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 } else {
-                    *reinterpret_cast<vw_t*>(slot + row * D + d) = v;
-                }
-                if (d == 0) {
-                    __hip_atomic_store(slot + ROWS * D + row, tops[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    __hip_atomic_store(slot + ROWS * (D + 1) + row, sums[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    *reinterpret_cast<float4_t*>(dst + 16 * i) = o[i];
                 }
             }
+        }
+        if (!a.counters && wg == first && tid == 0)
+            *reinterpret_cast<u32x2*>(a.spans + 2 * (this_b * sh.heads + item)) = u32x2{first, final};
+        if (first != final && wave == 0 && g == 0) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+                if (n * 16 + c < rows_here) {
+                    __hip_atomic_store(slot + ROWS * D + n * 16 + c, tops[n], __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_store(slot + ROWS * (D + 1) + n * 16 + c, sums[n], __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+                }
         }
         if (first != final && a.counters) {
             __builtin_amdgcn_s_waitcnt(0);          // this thread's stores have completed
@@ -696,11 +779,31 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
                     return __builtin_bit_cast(float2_t, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p),
                                                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
                 };
-                for (int i = 2 * tid; i < rows_here * D; i += 2 * THREADS) {
-                    const float2_t v = join_parts<D, ROWS>(a.parts, first, final, i / D, i % D, load2, load1);
-                    *reinterpret_cast<uint32_t*>(out_row<D>(a, this_b, h, rb * ROWS + i / D) + i % D) =
-                        round_out2<BF>(v[0], v[1]);
-                }
+                auto join = [&](auto ahead, auto u_) {
+                    constexpr int U = decltype(u_)::value;
+                    const int pairs = rows_here * D / 2;
+                    for (int i0 = tid; i0 < pairs; i0 += U * THREADS) {
+                        int jr[U], jd[U];
+                        float2_t v[U];
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            const int i = i0 + u * THREADS < pairs ? i0 + u * THREADS : i0;
+                            jr[u] = i / (D / 2);
+                            jd[u] = i % (D / 2) * 2;
+                        }
+                        join_parts<D, ROWS, decltype(ahead)::value>(a.parts, first, final, jr, jd, v, load2, load1);
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+                            *reinterpret_cast<uint32_t*>(out_row<D>(a, this_b, h, rb * ROWS + jr[u]) + jd[u]) =
+                                round_out2<BF>(v[u][0], v[u][1]);
+                    }
+                };
+                if constexpr (NR == 2)
+                    join(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
+                else if (rows_here * D / 2 > THREADS)
+                    join(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+                else
+                    join(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
                 if (tid == 0)
                     __hip_atomic_store(&a.counters[first], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
@@ -712,25 +815,18 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
 // The parts of items that several workgroups share, added by a launch of its
 // own: workgroup (i, y) takes 128 sums, from 128 y on, of item i, its 16
 // groups of 32 threads every sixteenth part each.
-template <bool BF, int D, int NR, int W>
+template <bool BF, int D, int NR>
 __global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(AttnArgs a) {
     constexpr int ROWS = 16 * NR, AHEAD = 4, SLICES = kJoinThreads / 32;
-    using Shares = tf::Shares<W, kJoinThreads>;
     using P = Parts<D, ROWS>;
-    __shared__ uint32_t scratch[kJoinThreads / 64];
-    __shared__ typename Shares::Found found;
     __shared__ float4_t vals[SLICES][32];
     __shared__ float m8[SLICES][32], l8[SLICES][32];
-    const Shares sh(a, scratch);
-    const int tid = threadIdx.x, slice = tid >> 5;
-    const int b = blockIdx.x / sh.heads;
-    const uint32_t item = blockIdx.x % sh.heads;
-    const typename Shares::Found seq = sh.sequence(b, &found);
-    const uint32_t n_rounds = Shares::rounds_of(seq.len);
-    const uint32_t item_rounds = seq.start + item * Shares::units_of(seq.len) + kItemCost;
-    const uint32_t first = sh.owner(item_rounds), final = sh.owner(item_rounds + n_rounds - 1);
+    const uint32_t first = a.spans[2 * blockIdx.x], final = a.spans[2 * blockIdx.x + 1];
     if (first == final) return;
-    const int h = (int)(item / a.row_blocks), rb = (int)(item % a.row_blocks);
+    const int tid = threadIdx.x, slice = tid >> 5;
+    const int b = (int)a.by_heads.of(blockIdx.x);
+    const uint32_t item = blockIdx.x - b * a.by_heads.d;
+    const int h = (int)a.by_row_blocks.of(item), rb = (int)item - h * a.row_blocks;
     const int q_rows = a.q_len * a.group;
     const int i = blockIdx.y * 128 + 4 * (tid & 31), r = i / D, d = i % D;
     if (blockIdx.y * 128 / D >= q_rows - rb * ROWS) return;   // the group of 128 lies in one row but for D = 64
@@ -794,14 +890,17 @@ int most_wgs(int D, int nr) { return kMostWgs / 4 * waves_per_simd(D, nr); }
 // their way at once.  Measured (8 heads of 128, up to 300 keys, us, 8 -> 4 waves):
 // 32 sequences 12.0 -> 13.9, 64 16.9 -> 15.1, 128 23.6 -> 18.6; 32 heads, 128
 // sequences of up to 2000: 118 -> 90.
-int waves_for(int64_t items, int cus) { return items >= 2 * cus ? 4 : 8; }
+// 32 rows of 256 keep eight: their queries and rings let a compute unit hold one
+// workgroup, of either size.
+constexpr bool four_waves_fit(int D, int nr) { return D < 256 || nr == 1; }
+int waves_for(int64_t items, int cus, int D, int nr) { return items >= 2 * cus && four_waves_fit(D, nr) ? 4 : 8; }
 
 }  // namespace
 
 int64_t kv4_attention_workspace_bytes(int64_t batch, int q_len, int q_heads, int kv_heads, int D) {
     (void)batch;
     const int nr = row_tiles(q_len * (q_heads / kv_heads));
-    return align256(kMostWgs * 4) + align256((int64_t)most_wgs(D, nr) * 2 * 16 * nr * (D + 2) * 4);
+    return align256(kMostWgs * 12) + align256((int64_t)most_wgs(D, nr) * 2 * 16 * nr * (D + 2) * 4);
 }
 
 int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride, const int32_t* lens, int64_t batch,
@@ -816,16 +915,22 @@ int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride,
     a.q_len = q_len;
     a.group = group;
     a.row_blocks = (q_rows + 16 * nr - 1) / (16 * nr);
-    a.capacity = c.max_pages * c.page_size;
+    a.capacity = (int32_t)(c.max_pages * c.page_size);
+    a.by_batch = Divisor((uint32_t)batch);
+    a.by_group = Divisor((uint32_t)group);
+    a.by_row_blocks = Divisor((uint32_t)a.row_blocks);
+    a.by_heads = Divisor((uint32_t)(c.kv_heads * a.row_blocks));
+    a.by_tiles = Divisor((uint32_t)(c.page_size / kKvTile));
     a.scale2 = scale * 1.4426950408889634f;
     a.out = static_cast<uint16_t*>(out);
     a.counters = static_cast<uint32_t*>(ws);
-    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(kMostWgs * 4));
+    a.spans = a.counters + kMostWgs;
+    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align256(kMostWgs * 12));
     // no more workgroups than rounds there can be
     const int cus = device_cus(s);
     const int64_t items = batch * c.kv_heads * a.row_blocks;
-    const int waves = waves_for(items, cus);
-    const int64_t item_rounds = (a.capacity + kKvTile * waves - 1) / (kKvTile * waves);
+    const int waves = waves_for(items, cus, c.head_dim, nr);
+    const int64_t item_rounds = ((int64_t)a.capacity + kKvTile * waves - 1) / (kKvTile * waves);
     int64_t wgs = (int64_t)cus * wgs_per_cu(c.head_dim, nr, waves);
     if (wgs > most_wgs(c.head_dim, nr)) wgs = most_wgs(c.head_dim, nr);
     if (wgs > items * item_rounds) wgs = items * item_rounds;
@@ -843,11 +948,12 @@ int launch_kv4_attention(const tf_kv4_cache& c, const void* q, int64_t q_stride,
         constexpr bool BF = decltype(bf)::value;
         const int rc = launch(kv4_attn_kernel<BF, D, NR, W>, grid, dim3(64 * W), 0, s, a);
         if (rc || !join) return rc;
-        return launch(kv4_join_kernel<BF, D, NR, W>, join_grid, dim3(kJoinThreads), 0, s, a);
+        return launch(kv4_join_kernel<BF, D, NR>, join_grid, dim3(kJoinThreads), 0, s, a);
     };
     auto go = [&](auto d, auto n, auto bf) {
-        return waves == 8 ? go_waves(d, n, bf, std::integral_constant<int, 8>{})
-                          : go_waves(d, n, bf, std::integral_constant<int, 4>{});
+        if constexpr (four_waves_fit(decltype(d)::value, decltype(n)::value))
+            if (waves == 4) return go_waves(d, n, bf, std::integral_constant<int, 4>{});
+        return go_waves(d, n, bf, std::integral_constant<int, 8>{});
     };
     auto by_rows = [&](auto d, auto bf) {
         return nr == 1 ? go(d, std::integral_constant<int, 1>{}, bf) : go(d, std::integral_constant<int, 2>{}, bf);
