@@ -450,9 +450,8 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
         if (at <= item_rounds) continue;  // the share ends before the item's rounds
 
         // The queries as the matrix cores take them, by way of LDS, each wave some of
-        // their words: a word of 16 rows lies in 64 lines, and all waves asking for
-        // all words cost 4 us of 30 (32 rows of 256).  Requested before anything
-        // waits for the page table.
+        // their 32-dim pieces (all waves asking for all of them cost 4 us of 30 for 32
+        // rows of 256).  Requested before anything waits for the page table.
         int limit[NR];                    // last visible position of the lane's row
         const uint16_t* q_src[NR];
 #pragma unroll
@@ -460,7 +459,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
             const int row = rb * ROWS + n * 16 + c;
             const bool real = row < q_rows;
             const int tq = real ? (int)a.by_group.of(row) : 0, hq = h * a.group + (real ? row - tq * a.group : 0);
-            q_src[n] = a.q + ((int64_t)this_b * a.q_len + tq) * a.q_stride + (int64_t)hq * D + g * (D / 4);
+            q_src[n] = a.q + ((int64_t)this_b * a.q_len + tq) * a.q_stride + (int64_t)hq * D + 8 * g;
             limit[n] = (int)len - a.q_len + tq;
         }
         constexpr int WORDS = NR * NW, OWN = (WORDS + W - 1) / W;
@@ -470,7 +469,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
             const int x = wave + i * W, n = x / NW;
             q[i] = u32x4{0, 0, 0, 0};
             if (x < WORDS && rb * ROWS + n * 16 + c < q_rows)
-                q[i] = *reinterpret_cast<const u32x4*>((NR == 2 && n ? q_src[NR - 1] : q_src[0]) + 8 * (x % NW));
+                q[i] = *reinterpret_cast<const u32x4*>((NR == 2 && n ? q_src[NR - 1] : q_src[0]) + 32 * (x % NW));
         }
 
         // ---- the wave's tiles: W r + wave for r0 <= r < r1, those that begin before len
@@ -517,7 +516,8 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
             const int x = wave + i * W, n = x / NW, w = x % NW;
             if (x >= WORDS) continue;
             const u32x4& v = q[i];
-            qs[n][w][lane] = v;
+            const int ch = 4 * w + g;     // the lane's 8 dims: word ch % NW of lane group ch / NW
+            qs[n][ch % NW][ch / NW * 16 + c] = v;
             const float sa = meta_f32<BF>(v, 0) + meta_f32<BF>(v, 1) + meta_f32<BF>(v, 4) + meta_f32<BF>(v, 5);
             const float sb = meta_f32<BF>(v, 2) + meta_f32<BF>(v, 3) + meta_f32<BF>(v, 6) + meta_f32<BF>(v, 7);
             const float2_t both = {over_groups(sa), over_groups(sb)};
@@ -607,11 +607,14 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
                     if (__any(top > m[n])) {
                         const float f =
                             top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m[n] - top) * a.scale2);
+                        const bool sums_yet = __any(m[n] != -__builtin_inff());
                         m[n] = top;
-                        l[n] *= f;
-                        osum[n] *= f;
+                        if (sums_yet) {
+                            l[n] *= f;
+                            osum[n] *= f;
 #pragma unroll
-                        for (int k = 0; k < NT; ++k) o[n * NT + k] *= f;
+                            for (int k = 0; k < NT; ++k) o[n * NT + k] *= f;
+                        }
                     }
                     const float base = m[n] == -__builtin_inff() ? 0.f : m[n] * a.scale2;
 #pragma unroll
