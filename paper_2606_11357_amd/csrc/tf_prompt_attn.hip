@@ -64,11 +64,16 @@ __device__ __forceinline__ int v_chunk(int r, int ch) {
     return D == 64 ? ch ^ (((r >> 1) & 1) << 2) : ch ^ ((r & 3) << 2);
 }
 
-__device__ __forceinline__ u32x2 lds_read_tr16(const uint16_t* p) {
+typedef __attribute__((address_space(3))) uint16_t Lds;
+
+__device__ __forceinline__ u32x2 lds_read_tr16(const Lds* p) {
     typedef __attribute__((address_space(3))) short4_t lds_short4;
-    const short4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (lds_short4*)(uintptr_t)(const __attribute__((address_space(3))) uint16_t*)p);
+    const short4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)p);
     return __builtin_bit_cast(u32x2, v);
+}
+__device__ __forceinline__ u32x4 lds_read16(const Lds* p) {
+    typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+    return *(lds_u32x4*)p;
 }
 
 // Which sequence, block of queries and head a workgroup takes: slot counts
@@ -161,7 +166,7 @@ struct Block {
 };
 
 // 16 bytes a lane from base + off straight to LDS, lane i's at dst + 16 i.
-__device__ __forceinline__ void direct_load16(const uint16_t* base, uint32_t off, uint16_t* dst) {
+__device__ __forceinline__ void direct_load16(const uint16_t* base, uint32_t off, Lds* dst) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(base, 0x7FFFFFFFu),
                                              (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
 }
@@ -216,10 +221,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         k_off[i] = r * k_row + 16 * k_chunk<D>(r, ch);
         v_off[i] = r * v_row + 16 * v_chunk<D>(r, ch);
     }
-    auto fetch = [&](bool V, int step) {
-        uint16_t* const buf = (V ? vs[step & 1] : ks[step & 1]) + wave * LOADS * 512;
+    auto fetch = [&](bool V, int step, const uint16_t* base, Lds* to) __attribute__((always_inline)) {
+        Lds* const buf = to + wave * LOADS * 512;
         const int64_t key0 = (int64_t)step * kBN;
-        const uint16_t* const rows = V ? v_base + key0 * a.v_stride : k_base + key0 * a.k_stride;
+        const uint16_t* const rows = base + key0 * (V ? a.v_stride : a.k_stride);
         if (key0 + kBN <= n_k) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) direct_load16(rows, V ? v_off[i] : k_off[i], buf + i * 512);
@@ -241,8 +246,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = -__builtin_inff(), l = 0.f;
     // S^T of a step's 64 keys
-    auto scores = [&](float16_t (&s)[2], int step) {
-        const uint16_t* kb = ks[step & 1];
+    auto scores = [&](float16_t (&s)[2], const Lds* kb) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -250,7 +254,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
 #pragma unroll
             for (int j = 0; j < KS; ++j) {
                 const int r = t * 32 + col;
-                const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + r * D + 8 * k_chunk<D>(r, 2 * j + half));
+                const u32x4 kf = lds_read16(kb + r * D + 8 * k_chunk<D>(r, 2 * j + half));
                 s[t] = mfma32<BF>(kf, q[j], s[t]);
             }
         }
@@ -260,22 +264,27 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
     // softmax: the matrix cores and the vector units then work side by side.
     // Keys are fetched two steps ahead, values one.
     float16_t s[2];
+    auto k_tile = [&](int step) { return (Lds*)ks[0] + (step & 1) * kBN * D; };
+    auto v_tile = [&](int step) { return (Lds*)vs[0] + (step & 1) * kBN * D; };
     if (step0 < steps) {
-        fetch(false, step0);
+        fetch(false, step0, k_base, k_tile(step0));
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        if (step0 + 1 < steps) fetch(false, step0 + 1);
-        fetch(true, step0);
-        scores(s, step0);
+        if (step0 + 1 < steps) fetch(false, step0 + 1, k_base, k_tile(step0 + 1));
+        fetch(true, step0, v_base, v_tile(step0));
+        scores(s, k_tile(step0));
     }
-    for (int step = step0; step < steps; ++step) {
-        __builtin_amdgcn_s_waitcnt(0);                    // this wave's part of the tiles is there
-        __syncthreads();                                  // everyone's is, and the other buffers are free
-        if (step + 2 < steps) fetch(false, step + 2);
-        if (step + 1 < steps) fetch(true, step + 1);
+    // One step.  The tiles that it fills and those that it reads are apart, and
+    // said to be: reads would wait for the loads on their way otherwise (one
+    // prompt of 8192, 8 heads of 256: 338 -> 321 us; 2048, 32 heads of 128: 55 ->
+    // 52.5).
+    auto one_step = [&](int step, Lds* __restrict k_to, Lds* __restrict v_to, const Lds* __restrict kb,
+                        const Lds* __restrict vb, const uint16_t* __restrict k_from,
+                        const uint16_t* __restrict v_from) __attribute__((always_inline)) {
+        if (step + 2 < steps) fetch(false, step + 2, k_from, k_to);
+        if (step + 1 < steps) fetch(true, step + 1, v_from, v_to);
         const int key0 = step * kBN;
-        if (key0 >= wave_keys) continue;
-        const uint16_t* vb = vs[step & 1];
+        if (key0 >= wave_keys) return;
         if (key0 + kBN - 1 > wave_low) {                  // some key is hidden from some query
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -302,34 +311,78 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
                 for (int i = 0; i < 16; ++i) o[t][i] *= f;
         }
         const float base = m == -__builtin_inff() ? 0.f : m * a.scale2;
-        // (after the last step the scores of a step that is there are computed again)
-        float16_t next[2];
-        scores(next, step + 1 < steps ? step + 1 : step);
         u32x4 p[4];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale2, -base));
-                const float e1 = __builtin_amdgcn_exp2f(fmaf(s[t][i + 1], a.scale2, -base));
-                const uint32_t pair = round_out2<BF>(e0, e1);
-                p[2 * t + i / 8][(i % 8) / 2] = pair;
-                l = dot2<BF>(pair, kOnes<BF>, l);         // the weights as the matrix cores see them
-            }
+        float16_t next[2];
+        // (after the last step the scores of what the other tile holds are computed)
+        auto weights = [&](int at) {                      // of scores at, at + 1 of 32
+            const int t = at / 16, i = at % 16;
+            const float e0 = __builtin_amdgcn_exp2f(fmaf(s[t][i], a.scale2, -base));
+            const float e1 = __builtin_amdgcn_exp2f(fmaf(s[t][i + 1], a.scale2, -base));
+            const uint32_t pair = round_out2<BF>(e0, e1);
+            p[2 * t + i / 8][(i % 8) / 2] = pair;
+            l = dot2<BF>(pair, kOnes<BF>, l);             // the weights as the matrix cores see them
+        };
         // keys 16 j + 4 half + 0..3 and + 8: the order in which p holds them
-        const int l16 = lane & 15, sub = (lane >> 4) & 1;
+        auto values = [&](int t, int j) {
+            const int l16 = lane & 15, d = 32 * t + 16 * ((lane >> 4) & 1) + 4 * (l16 & 3);
+            const int r0 = 16 * j + 4 * half + (l16 >> 2), r1 = r0 + 8;
+            const u32x2 v0 = lds_read_tr16(vb + r0 * D + 8 * v_chunk<D>(r0, d >> 3) + (d & 7));
+            const u32x2 v1 = lds_read_tr16(vb + r1 * D + 8 * v_chunk<D>(r1, d >> 3) + (d & 7));
+            return u32x4{v0[0], v0[1], v1[0], v1[1]};
+        };
+        if constexpr (D == 256) {
+            // One wave a SIMD: nothing but its own vector work hides a wait for LDS.
+            // The operands come four at a time, a batch ahead of their instructions,
+            // and the softmax is spread over the scores' batches (one prompt of 8192,
+            // 8 heads: 462 -> 338 us; heads of 128 and 64, which have other waves to
+            // run meanwhile, 525 -> 535 and 167 -> 176).
+            auto keys = [&](int x) {                      // operand x of 2 KS: 16 dims of 32 keys
+                const int r = (x & 1) * 32 + col;
+                return lds_read16(kb + r * D + 8 * k_chunk<D>(r, (x & ~1) + half));
+            };
+            constexpr int B = 4, KB = 2 * KS / B;
+            u32x4 f[2][B];
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int d = 32 * t + 16 * sub + 4 * (l16 & 3);
-                const int r0 = 16 * j + 4 * half + (l16 >> 2), r1 = r0 + 8;
-                const u32x2 v0 = lds_read_tr16(vb + r0 * D + 8 * v_chunk<D>(r0, d >> 3) + (d & 7));
-                const u32x2 v1 = lds_read_tr16(vb + r1 * D + 8 * v_chunk<D>(r1, d >> 3) + (d & 7));
-                o[t] = mfma32<BF>(u32x4{v0[0], v0[1], v1[0], v1[1]}, p[j], o[t]);
+                for (int i = 0; i < 16; ++i) next[t][i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < B; ++i) f[0][i] = keys(i);
+#pragma unroll
+            for (int b = 0; b < KB; ++b) {
+#pragma unroll
+                for (int i = 0; i < B; ++i) f[(b + 1) & 1][i] = b + 1 < KB ? keys((b + 1) * B + i) : values(0, i);
+#pragma unroll
+                for (int i = 0; i < B; ++i) next[i & 1] = mfma32<BF>(f[b & 1][i], q[(b * B + i) / 2], next[i & 1]);
+#pragma unroll
+                for (int at = b * 32 / KB; at < (b + 1) * 32 / KB; at += 2) weights(at);
+                __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                if (t + 1 < DT)
+#pragma unroll
+                    for (int i = 0; i < B; ++i) f[(KB + t + 1) & 1][i] = values(t + 1, i);
+#pragma unroll
+                for (int i = 0; i < B; ++i) o[t] = mfma32<BF>(f[(KB + t) & 1][i], p[i], o[t]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            scores(next, kb);
+#pragma unroll
+            for (int at = 0; at < 32; at += 2) weights(at);
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[t] = mfma32<BF>(values(t, j), p[j], o[t]);
+        }
         s[0] = next[0];
         s[1] = next[1];
+    };
+    for (int step = step0; step < steps; ++step) {
+        __builtin_amdgcn_s_waitcnt(0);                    // this wave's part of the tiles is there
+        __syncthreads();                                  // everyone's is, and the other buffers are free
+        one_step(step, k_tile(step), v_tile(step + 1), k_tile(step + 1), v_tile(step), k_base, v_base);
     }
     const SwapPair sums = swap32(l);
     l = sums.a + sums.b;
@@ -411,11 +464,21 @@ __global__ __launch_bounds__(64 * kWaves) void prompt_join_kernel(PromptArgs a) 
 int64_t most_slots(int64_t batch, int64_t tokens_q, int q_heads) {
     return (tokens_q + (kBM - 1) * (batch < tokens_q ? batch : tokens_q)) / kBM * q_heads;
 }
-// Parts that the keys of a block are split into: where blocks and heads leave
-// most of the chip idle and the keys are many, enough to give each compute unit
-// two workgroups, of at least 8 steps each.
-int splits_for(int64_t slots, int64_t batch, int64_t tokens_k) {
-    const int64_t idle = 2 * kSizedForCus / slots, by_keys = tokens_k / batch / (8 * kBN);
+// Parts that the keys of a block are split into, for sequences taken to be of one
+// length: as many as fill the chip (two workgroups a compute unit, one with heads
+// of 256), of at least 8 steps of a block's mean, or 2.5 of the longer ones of
+// heads of 256.  These also pay for parts where causal blocks are many enough but
+// of lengths so different that the longest alone fill the end.  Measured (us,
+// parts 1 / 2 / 4; the rule's in brackets): 16 heads of 128, 1 x 1024 [25.9] / 28.5
+// / 25.4, 1 x 2048 45.9 / [43.1] / 49.2, 4096 [94.5] / 100.8 / 115; 500 after 3000
+// 71.5 / 46.1 / 34.5 / [6: 32.7]; 8 heads of 256, 1 x 1024 46.3 / 36.1 / 30.1 [3:
+// 32.4], 4096 151 / [113] / 135, 4 x 1000 [47.5] / 65.8 / 81.3.
+int splits_for(int64_t slots, int64_t batch, int64_t tokens_q, int64_t tokens_k, int D, bool causal) {
+    const int64_t n_k = tokens_k / batch, n_q = tokens_q / batch < n_k ? tokens_q / batch : n_k;
+    const int64_t mean = causal ? n_k - n_q / 2 : n_k;
+    int64_t wgs = D == 256 ? kSizedForCus : 2 * kSizedForCus;
+    if (D == 256 && mean >= 16 * kBN) wgs = wgs * n_k / mean;
+    const int64_t idle = wgs / slots, by_keys = mean / (D == 256 ? 5 * kBN / 2 : 8 * kBN);
     const int64_t s = idle < by_keys ? idle : by_keys;
     return s < 2 ? 1 : s > kMostSplits ? kMostSplits : (int)s;
 }
@@ -424,7 +487,8 @@ int splits_for(int64_t slots, int64_t batch, int64_t tokens_k) {
 
 int64_t prompt_attention_workspace_bytes(int64_t batch, int64_t tokens_q, int64_t tokens_k, int q_heads, int D) {
     const int64_t slots = most_slots(batch, tokens_q, q_heads);
-    const int s = splits_for(slots, batch, tokens_k);
+    const int full = splits_for(slots, batch, tokens_q, tokens_k, D, false);
+    const int causal = splits_for(slots, batch, tokens_q, tokens_k, D, true), s = full > causal ? full : causal;
     return s == 1 ? 0 : align256(slots * s * kBM * (D + 2) * 4);
 }
 
@@ -437,7 +501,7 @@ int launch_prompt_attention(bool bf, const void* q, int64_t q_stride, const void
                  q_heads / kv_heads, tokens_q, tokens_k, scale * 1.4426950408889634f, causal ? 1 : 0,
                  static_cast<uint16_t*>(out), 1, static_cast<float*>(ws), 0};
     const int64_t slots = most_slots(batch, tokens_q, q_heads);
-    if (ws) a.splits = splits_for(slots, batch, tokens_k);
+    if (ws) a.splits = splits_for(slots, batch, tokens_q, tokens_k, D, causal);
     a.part_stride = slots * kBM * (D + 2);
     const dim3 grid((unsigned)(slots * a.splits)), join_grid((unsigned)slots, (unsigned)(kBM * D / 4 / (64 * kWaves)));
     auto go = [&](auto d) {
