@@ -8,7 +8,13 @@
 // is a 16-bit float off + q (one and-or for two codes), and off and z leave as
 // products with sum(Q) and with sums of P in fp32.
 //
-// HBM-bound: D + 8 bytes of cache a token and head, of which each is read once.
+// The cache, D + 8 bytes a token and head, is read once, at the rate of a large
+// copy where there is enough of it: 16 sequences of 8192, 32 heads on 32 of 128,
+// 110 us, 5.2 TB/s.  Shared heads come near to the vector unit's bound first
+// (codes and softmax of 16 columns a tile, of which q_len * group are real): 64
+// sequences of up to 8192, 32 heads on 8 of 128, 51 us, 3.8 TB/s with it 78% busy.
+// Few tokens cost the chain lengths - table - tiles - sums: one sequence of 513
+// keys 9.3 us.
 #include "tf_kv4.h"
 
 namespace tf {
@@ -160,13 +166,13 @@ __device__ __forceinline__ const __attribute__((address_space(4))) int32_t* as_c
 // How the rounds of all items are shared out.  An item is one (sequence,
 // key/value head, block of query rows); its rounds are 32 keys for each of W
 // waves, at least one (which writes the zeros of an empty row), and it counts
-// kItemCost units of its own before them.  Workgroup w of `wgs` takes a contiguous share of all
-// units, in the order of sequence, head and block, and shares differ by at most
-// one unit whatever the lengths are.  Where there are fewer items than
-// workgroups, no more of these work than an item of average length is worth: one
-// where no item has more than kLeastRounds rounds (they cost less than joining
-// parts), else one a round, or one for two rounds past kFewParts (items of one
-// length then end where shares do).
+// kItemCost units of its own before them.  Workgroup w of `wgs` takes a
+// contiguous share of all units, in the order of sequence, head and block, and
+// shares differ by at most one unit whatever the lengths are.  Where there are
+// fewer items than workgroups, no more of these work than an item of average
+// length is worth: one where no item has more than kLeastRounds rounds (they cost
+// less than joining parts), else one a round, or one for two rounds past kFewParts
+// (items of one length then end where shares do).
 template <int W, int THREADS>
 struct Shares {
     static constexpr int WAVES = THREADS / 64, KEYS = kKvTile * W;
@@ -677,7 +683,8 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
             }
         }
         // ---- the waves' sums under a common maximum: each wave keeps its W-th of
-        // them, halving what it holds with one wave after another
+        // them, halving what it holds with one wave after another (32 rows of 256:
+        // 3 us; some rows of all waves at a time, four times, took 7)
         lds_barrier();                    // the tiles are read; maxima and sums are there
         float tops[NR], sums[NR];
 #pragma unroll
@@ -817,7 +824,8 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
 
 // The parts of items that several workgroups share, added by a launch of its
 // own: workgroup (i, y) takes 128 sums, from 128 y on, of item i, its 16
-// groups of 32 threads every sixteenth part each.
+// groups of 32 threads every sixteenth part each.  Latency-bound: 2 items of 128
+// parts, 32 rows of 256 (8.4 MB), 4.7 us.
 template <bool BF, int D, int NR>
 __global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(AttnArgs a) {
     constexpr int ROWS = 16 * NR, AHEAD = 4, SLICES = kJoinThreads / 32;

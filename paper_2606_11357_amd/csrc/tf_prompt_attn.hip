@@ -10,6 +10,12 @@
 // query's scores (its maximum and sum are the lane's own, joined with one other
 // lane), and the scores it holds are, rounded, the very operand that the second
 // product takes from it.
+//
+// Four waves of 32 queries share each step's 64 keys and values in LDS: with 128
+// dims a wave reads 32 KB of them a step for 1024 cycles of matrix instructions.  Measured (bf16, one causal prompt of 8192): 32 heads on 8 of 128
+// 527 us, 1044 TFLOP/s, matrix cores busy 57% of the time and vector units 49%, at
+// the clock that the card's power leaves; 16 heads of 64 167 us, 823; 8 of 256 321
+// us, 856.
 #include "tf_internal.h"
 
 namespace tf {
@@ -21,6 +27,9 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 4;
 constexpr int kBM = 32 * kWaves;       // queries of a workgroup
 constexpr int kBN = 64;                // keys of a step
+// A weight may pass 1 by 2^kSlack before the sums move to a new maximum (0: 545 us
+// instead of 527 for 32 heads of 128 on 8192; error against 64 bits 1.75e-3 and
+// 1.93e-3, of which 1.65e-3 is the output's rounding).
 constexpr float kSlack = 8.f;
 template <bool BF> constexpr uint32_t kOnes = BF ? 0x3F803F80u : 0x3C003C00u;
 constexpr int kSizedForCus = 256, kMostSplits = 16;
@@ -415,7 +424,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
 }
 
 // Adds the parts of one block of queries in their order: workgroup (slot, y)
-// takes 256 of the block's lanes' groups of four sums, one a thread.
+// takes 256 of the block's lanes' groups of four sums, one a thread.  Bound by
+// reading the parts: 64 blocks of 8 parts, heads of 128 (34 MB), 7.8 us.
 template <bool BF, int D>
 __global__ __launch_bounds__(64 * kWaves) void prompt_join_kernel(PromptArgs a) {
     constexpr int DT = D / 32, AHEAD = 4;
