@@ -124,7 +124,10 @@ def test_workspace_queries(lib):
     n = lib.tf_kv4_attention_workspace_bytes(1, 1, 32, 8, 128)
     assert n > 0 and n % 256 == 0
     assert lib.tf_kv4_attention_workspace_bytes(64, 1, 32, 8, 128) == n
-    assert lib.tf_kv4_attention_workspace_bytes(1, 8, 32, 8, 128) > n
+    # 32 rows a workgroup: twice the parts' rows, of as many workgroups (heads of
+    # 256) or of half as many (128, where the rows' sums halve what a unit holds)
+    assert lib.tf_kv4_attention_workspace_bytes(1, 8, 32, 8, 128) == n
+    assert lib.tf_kv4_attention_workspace_bytes(1, 4, 8, 1, 256) > lib.tf_kv4_attention_workspace_bytes(1, 1, 8, 1, 256)
     assert lib.tf_kv4_attention_workspace_bytes(1, 9, 32, 8, 128) == tfb.TF_ERR_ARG
     assert lib.tf_kv4_attention_workspace_bytes(1, 1, 30, 8, 128) == tfb.TF_ERR_SHAPE
     assert lib.tf_prompt_attention_workspace_bytes(1, 8192, 8192, 32, 8, 128) == 0
