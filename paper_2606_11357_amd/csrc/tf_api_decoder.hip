@@ -33,6 +33,8 @@ bool bad_stride(int64_t stride, int heads, int d) {
     // a kernel's 32-bit offsets span 64 tokens
     return stride % 8 != 0 || stride < (int64_t)heads * d || stride > (int64_t(1) << 24);
 }
+// A launch has fewer than 2^32 threads.
+bool too_many(int64_t threads) { return threads > (int64_t)UINT32_MAX; }
 bool bad_scale(float s) { return !(s > 0.f) || s > 1e30f; }
 
 int check_cache_shape(int64_t pages, int page_size, int kv_heads, int head_dim) {
@@ -98,6 +100,7 @@ int tf_kv4_append(const tf_kv4_cache* cache, const void* Q, int64_t q_stride, co
         bad_stride(v_stride, cache->kv_heads, cache->head_dim))
         return TF_ERR_SHAPE;
     if (cos && positions < 1) return TF_ERR_SHAPE;
+    if (too_many(tokens * (q_heads + 2 * cache->kv_heads) * (cache->head_dim / 16))) return TF_ERR_SHAPE;
     for (const void* p : {Q, K, V, (const void*)cos, (const void*)sin, (const void*)Q_out, (const void*)K_out})
         if (misaligned(p)) return TF_ERR_ALIGN;
     if (misaligned(cu, 4) || misaligned(starts, 4)) return TF_ERR_ALIGN;
@@ -111,6 +114,7 @@ int tf_kv4_read(const tf_kv4_cache* cache, const int32_t* cu, const int32_t* sta
     if (rc) return rc;
     if (!cu || !starts || !K_out || !V_out) return TF_ERR_NULL;
     if (tokens < 1 || tokens > TF_MAX_M) return TF_ERR_SHAPE;
+    if (too_many(tokens * 2 * cache->kv_heads * (cache->head_dim / 16))) return TF_ERR_SHAPE;
     if (misaligned(K_out) || misaligned(V_out) || misaligned(cu, 4) || misaligned(starts, 4)) return TF_ERR_ALIGN;
     return tf::launch_kv4_read(*cache, cu, starts, batch, tokens, K_out, V_out, static_cast<hipStream_t>(stream));
 }
@@ -149,6 +153,8 @@ int64_t tf_prompt_attention_workspace_bytes(int64_t batch, int64_t tokens_q, int
     if (batch < 1 || batch > TF_MAX_BATCH || tokens_q < 1 || tokens_q > TF_MAX_M || tokens_k < 1 ||
         tokens_k > TF_MAX_M)
         return TF_ERR_SHAPE;
+    // 256 threads for each head of 128 queries, the last of each sequence perhaps fewer
+    if (too_many((tokens_q + 127 * (batch < tokens_q ? batch : tokens_q)) * 2 * q_heads)) return TF_ERR_SHAPE;
     return tf::prompt_attention_workspace_bytes(batch, tokens_q, tokens_k, q_heads, head_dim);
 }
 

@@ -118,6 +118,18 @@ def test_prompt_rejects(lib, kw, want):
     assert lib.tf_prompt_attention(*(PROMPT | kw).values(), NULL) == want
 
 
+def test_calls_of_more_threads_than_a_launch_has(lib):
+    """Sizes that each pass their own limit and together ask for 2^32 threads."""
+    big = dict(tokens=1 << 20)
+    c = cache(kv_heads=1024, head_dim=256)
+    wide = dict(q_stride=1024 * 256, k_stride=1024 * 256, v_stride=1024 * 256, q_heads=1024)
+    assert lib.tf_kv4_append(c, *(APPEND | wide | big).values(), NULL) == tfb.TF_ERR_SHAPE
+    assert lib.tf_kv4_read(c, *(READ | big).values(), NULL) == tfb.TF_ERR_SHAPE
+    assert lib.tf_prompt_attention(*(PROMPT | wide | dict(tokens_q=1 << 20, batch=65536, kv_heads=1024, head_dim=256)).values(),
+                                   NULL) == tfb.TF_ERR_SHAPE
+    assert lib.tf_prompt_attention_workspace_bytes(1, 1 << 20, 1 << 20, 1024, 1, 128) == 0      # 2^31: fits
+
+
 def test_workspace_queries(lib):
     """Decode: at least what one call's parts and counters take, the same region
     of counters for every shape.  Prompts: none where blocks fill the chip."""
