@@ -10,11 +10,12 @@
 //
 // The cache, D + 8 bytes a token and head, is read once, at the rate of a large
 // copy where there is enough of it: 16 sequences of 8192, 32 heads on 32 of 128,
-// 110 us, 5.2 TB/s.  Shared heads come near to the vector unit's bound first
-// (codes and softmax of 16 columns a tile, of which q_len * group are real): 64
-// sequences of up to 8192, 32 heads on 8 of 128, 51 us, 3.8 TB/s with it 78% busy.
-// Few tokens cost the chain lengths - table - tiles - sums: one sequence of 513
-// keys 9.3 us.
+// 110 us, 5.2 TB/s; 64 of up to 8192, 32 heads on 8 of 128, 51 us, 3.9 TB/s, of
+// which beginning and end take 8 us.  There the vector unit is 78% busy with codes
+// and the softmax of 16 columns, of which q_len * group are real, but is not what
+// is waited for: a copy with half the softmax ran 2% faster, one with shares that
+// let all workgroups of a compute unit end together 1%.  Few tokens cost the chain
+// lengths - table - tiles - sums: one sequence of 513 keys 9.3 us.
 #include "tf_kv4.h"
 
 namespace tf {
