@@ -112,6 +112,23 @@ inline int launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t shmem,
     return e == hipSuccess ? TF_OK : TF_ERR_HIP;
 }
 
+// A store past the L2: it keeps no line there, and the kernel's end has none to
+// write back.
+template <typename T>
+__device__ __forceinline__ void store_past(T* p, const T& v) { __builtin_nontemporal_store(v, p); }
+// The same where `past` says so.  (The empty statements keep the compiler from
+// making one plain store of both.)
+template <typename T>
+__device__ __forceinline__ void store_past_if(bool past, T* p, const T& v) {
+    if (past) {
+        store_past(p, v);
+    } else {
+        asm volatile("" ::: "memory");
+        *p = v;
+        asm volatile("" ::: "memory");
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Device primitives.
 // ---------------------------------------------------------------------------

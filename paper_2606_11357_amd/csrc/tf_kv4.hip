@@ -8,9 +8,8 @@ namespace {
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 
 // Values (of keys, and as many of values) from which a read goes tile by tile.
-// Measured, 8 heads of 128, us row by row and tile by tile: 1000 tokens (1.0 M
-// values) 4.5 / 6.4, 2000 6.3 / 7.0, 4000 9.35 / 9.17, 8000 14.6 / 12.0, 16000
-// 23.8 / 19.1.
+// Measured, 8 heads of 128, us row by row and tile by tile: 2000 tokens (2 M
+// values) 5.4 / 6.3, 4097 8.5 / 7.7, 8192 13.2 / 10.9.
 constexpr int64_t kTileValues = 1 << 22;
 constexpr int kStagedBatch = 1024;     // up to this many sequences' offsets are searched in LDS
 
@@ -148,8 +147,8 @@ __device__ __forceinline__ void append_row(const AppendArgs& a, const Row& r, in
             oa[j] = r.known ? round_out<BF>(lo[j]) : nan16;
             ob[j] = r.known ? round_out<BF>(hi[j]) : nan16;
         }
-        *reinterpret_cast<u16x8*>(o) = oa;
-        *reinterpret_cast<u16x8*>(o + D / 2) = ob;
+        store_past(reinterpret_cast<u16x8*>(o), oa);
+        store_past(reinterpret_cast<u16x8*>(o + D / 2), ob);
     }
     if (!__any(r.active && r.kind != 0 && r.known)) return;       // queries only
     // the row's range over its lanes
@@ -221,7 +220,8 @@ __device__ __forceinline__ void place_row(const AppendArgs& a, const int32_t* cu
 // tokens are many it is bound by these and by the vector unit that makes the
 // codes (64% busy), else by a chain of four dependent loads (offsets, start,
 // page, angles).  Two and four rows a lane group were no faster.  Measured (bf16,
-// 32/8 heads of 128): 5 x 4097 tokens 116 us, one token each of 64 sequences 5.0.
+// 32/8 heads of 128): 4 x 4096 tokens 89 us (94 with the rotated rows through the
+// L2), one token each of 64 sequences 5.0.
 template <bool BF, int D>
 __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
     constexpr int LPR = D / 16;
@@ -367,14 +367,14 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
             ob[j] = round_out<BF>(((float)qb[j] - z) * s);
         }
     }
-    *reinterpret_cast<u16x8*>(o) = oa;
-    *reinterpret_cast<u16x8*>(o + D / 2) = ob;
+    store_past(reinterpret_cast<u16x8*>(o), oa);
+    store_past(reinterpret_cast<u16x8*>(o + D / 2), ob);
 }
 
 // Many tokens of a sequence: a wave takes the keys (or values) of one head for
 // one tile, whose lines it reads whole.  HBM-bound, by the 4 D bytes that it
 // writes a token and head against D + 8 read: 4 sequences of up to 16384 tokens,
-// 8 heads of 128, 46 us, 4.0 TB/s.
+// 8 heads of 128, 32 us, 5.8 TB/s (46 with the outputs through the L2).
 template <bool BF, int D>
 __global__ __launch_bounds__(256) void kv4_read_tiles_kernel(ReadArgs a, uint32_t wgs_per_slot) {
     __shared__ uint32_t before[257], scratch[4];
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(256) void kv4_read_tiles_kernel(ReadArgs a, uint32_
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 o[j] = round_out<BF>(((float)(word[n] >> (4 * (j >> 1) + 16 * (j & 1)) & 15) - z[n]) * s[n]);
-            if (inside(kk)) *out(kk, lane % WPR * 8) = o;
+            if (inside(kk)) store_past(out(kk, lane % WPR * 8), o);
         }
         return;
     }
@@ -446,8 +446,8 @@ __global__ __launch_bounds__(256) void kv4_read_tiles_kernel(ReadArgs a, uint32_
                 ob[j] = round_out<BF>(((float)(byte >> 4) - z) * s);
             }
             if (inside(kk)) {
-                *out(kk, dims) = oa;
-                *out(kk, dims + D / 2) = ob;
+                store_past(out(kk, dims), oa);
+                store_past(out(kk, dims + D / 2), ob);
             }
         }
     }

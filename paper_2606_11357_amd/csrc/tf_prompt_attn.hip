@@ -32,6 +32,11 @@ constexpr int kBN = 64;                // keys of a step
 // 1.93e-3, of which 1.65e-3 is the output's rounding).
 constexpr float kSlack = 8.f;
 template <bool BF> constexpr uint32_t kOnes = BF ? 0x3F803F80u : 0x3C003C00u;
+// Bytes of all parts up to which they are stored past the L2.  Measured, us through
+// and past it: 13 MB (500 after 3000, 16 heads of 64) 25.1 / 22.9, 17 MB (2048, 16
+// of 64) 32.3 / 29.1, 34 MB (500 after 3000, 32 of 128) 45.2 / 46.1, 67 MB (2048, 8
+// of 256) 54.7 / 58.8.
+constexpr int64_t kMostPast = 24 << 20;
 constexpr int kSizedForCus = 256, kMostSplits = 16;
 
 struct PromptArgs {
@@ -46,6 +51,7 @@ struct PromptArgs {
     int splits;                        // parts that each block's keys are split into
     float* parts;                      // splits > 1: [part][slot] kBM rows of D sums, of a maximum, of a sum
     int64_t part_stride;               // floats of one part
+    bool past;                         // parts past the L2
 };
 
 template <bool BF>
@@ -403,8 +409,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                dst[(t * 4 + i / 4) * 64] = float4_t{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+            for (int i = 0; i < 16; i += 4) {
+                const float4_t v = {o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+                store_past_if(a.past, &dst[(t * 4 + i / 4) * 64], v);
+            }
         if (half == 0) {
             part[kBM * D + wave * 32 + col] = m * a.scale2;
             part[kBM * (D + 1) + wave * 32 + col] = l;
@@ -509,10 +517,11 @@ int launch_prompt_attention(bool bf, const void* q, int64_t q_stride, const void
     auto in = [](const void* p) { return static_cast<const uint16_t*>(p); };
     PromptArgs a{in(q), in(k), in(v), q_stride, k_stride, v_stride, cu_q, cu_k, (int)batch, q_heads,
                  q_heads / kv_heads, tokens_q, tokens_k, scale * 1.4426950408889634f, causal ? 1 : 0,
-                 static_cast<uint16_t*>(out), 1, static_cast<float*>(ws), 0};
+                 static_cast<uint16_t*>(out), 1, static_cast<float*>(ws), 0, false};
     const int64_t slots = most_slots(batch, tokens_q, q_heads);
     if (ws) a.splits = splits_for(slots, batch, tokens_q, tokens_k, D, causal);
     a.part_stride = slots * kBM * (D + 2);
+    a.past = a.splits * a.part_stride * 4 <= kMostPast;
     const dim3 grid((unsigned)(slots * a.splits)), join_grid((unsigned)slots, (unsigned)(kBM * D / 4 / (64 * kWaves)));
     auto go = [&](auto d) {
         constexpr int D_ = decltype(d)::value;

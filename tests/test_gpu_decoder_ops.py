@@ -87,6 +87,16 @@ def test_norm(tf, dt, form, M, N):
         assert (np.abs(down(r) - want_r) <= U[dt] * np.abs(want_r) + 2.0 ** -20 * terms + TINY[dt]).all()
 
 
+def test_norm_of_many_rows_is_that_of_few(tf):
+    """More than 2^24 elements: the same bits as in calls of fewer."""
+    x, res = (torch.randn(4100, 4104, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn(4104, device="cuda").bfloat16()
+    y, r = tf.add_rms_norm(x, res, w)
+    for i in range(0, 4100, 1025):
+        y_part, r_part = tf.add_rms_norm(x[i:i + 1025], res[i:i + 1025], w)
+        assert torch.equal(y[i:i + 1025], y_part) and torch.equal(r[i:i + 1025], r_part)
+
+
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
 def test_norm_in_place_and_parts(tf, dt):
     """residual_out may be residual and out may be x; either output alone."""
@@ -495,7 +505,7 @@ def test_prompt_of_many_sequences(tf, dt):
 
 
 SPLITS = [((4, 1, 128), [70], [3000]), ((2, 2, 64), [1], [2049]), ((2, 1, 256), [40, 0, 129], [5000, 7, 1300]),
-          ((3, 3, 64), [200, 33], [190, 4200])]
+          ((3, 3, 64), [200, 33], [190, 4200]), ((8, 1, 256), [500], [3500])]
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
