@@ -45,6 +45,18 @@ __host__ __device__ constexpr int kv4_word(int u, int L, int w) {
 // Byte of key jj inside a V word.
 __host__ __device__ constexpr int kv4_byte(int jj) { return jj == 1 ? 2 : jj == 2 ? 1 : jj; }
 
+// Division by a number that the host knows, of numbers below 2^31: with
+// 2^(s-1) < d <= 2^s and m = floor(2^(31+s) / d) + 1, n / d = n m >> 31 + s.
+struct Divisor {
+    uint32_t d = 1, m = 0, s = 0;
+    Divisor() = default;
+    explicit Divisor(uint32_t by) : d(by) {
+        while (d > 1u << s) ++s;
+        m = (uint32_t)(((uint64_t)1 << (31 + s)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (uint32_t)((uint64_t)n * m >> (31 + s)); }
+};
+
 // A paged cache as the kernels take it.
 struct Kv4 {
     uint8_t* data;

@@ -23,6 +23,7 @@ struct AppendArgs {
     int batch, q_heads;
     int64_t tokens;
     uint16_t *q_out, *k_out;
+    Divisor by_rows;                  // q_heads + 2 kv_heads
 };
 
 // Offsets of up to kStagedBatch sequences in LDS (a search of log2(batch)
@@ -157,7 +158,7 @@ __device__ __forceinline__ void append_row(const AppendArgs& a, const Row& r, in
     for (int j = 0; j < 8; ++j) {
         least = fminf(least, fminf(lo[j], hi[j]));
         most = fmaxf(most, fmaxf(lo[j], hi[j]));
-        total += (lo[j] - lo[j]) + (hi[j] - hi[j]);    // 0, or NaN where one is not finite
+        total = fmaf(hi[j], 0.f, fmaf(lo[j], 0.f, total));    // 0, or NaN where one is not finite
     }
     if (!(total == 0.f)) most = __builtin_inff();
     least = -row_max<LPR>(-least);
@@ -202,11 +203,11 @@ __device__ __forceinline__ void append_row(const AppendArgs& a, const Row& r, in
 }
 
 // The row at place `at` of (token, row of the token) pairs.
-__device__ __forceinline__ void place_row(const AppendArgs& a, const int32_t* cu, uint32_t at, int rows, Row& r,
-                                          int& sequence) {
-    r.active = at < a.tokens * rows;
-    r.t = r.active ? at / (uint32_t)rows : 0;
-    const int row = r.active ? (int)(at % (uint32_t)rows) : 0;
+__device__ __forceinline__ void place_row(const AppendArgs& a, const int32_t* cu, uint32_t at, Row& r, int& sequence) {
+    const uint32_t t = a.by_rows.of(at);      // (at is below 2^30: at least four lanes a row)
+    r.active = t < a.tokens;
+    r.t = r.active ? t : 0;
+    const int row = r.active ? (int)(at - t * a.by_rows.d) : 0;
     r.kind = row < a.q_heads ? 0 : row < a.q_heads + a.cache.kv_heads ? 1 : 2;
     r.h = row - (r.kind == 0 ? 0 : r.kind == 1 ? a.q_heads : a.q_heads + a.cache.kv_heads);
     sequence = owner_of(cu, a.batch, r.t);
@@ -227,11 +228,10 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
     constexpr int LPR = D / 16;
     __shared__ int32_t lds_cu[kStagedBatch + 1];
     const int32_t* cu = stage_offsets(a.cu, a.batch, lds_cu);
-    // (token, row) pairs: at most TF_MAX_M * 3 TF_MAX_HEADS, below 2^32
     const int i = threadIdx.x % LPR;
     Row r;
     int b;
-    place_row(a, cu, blockIdx.x * (256 / LPR) + threadIdx.x / LPR, a.q_heads + 2 * a.cache.kv_heads, r, b);
+    place_row(a, cu, blockIdx.x * (256 / LPR) + threadIdx.x / LPR, r, b);
     load_row<D>(a, r, i);
     append_row<BF, D>(a, r, i, [&] { return kv4_tile(a.cache, b, r.pos, r.h, kv4_tile_bytes(D)); });
 }
@@ -492,7 +492,7 @@ int launch_kv4_append(const tf_kv4_cache& c, const void* q, int64_t q_stride, co
     auto in = [](const void* p) { return static_cast<const uint16_t*>(p); };
     const AppendArgs a{device_view(c), in(q), in(k), in(v), q_stride, k_stride, v_stride, cos, sin, positions, cu,
                        starts, (int)batch, q_heads, tokens, static_cast<uint16_t*>(q_out),
-                       static_cast<uint16_t*>(k_out)};
+                       static_cast<uint16_t*>(k_out), Divisor((uint32_t)(q_heads + 2 * c.kv_heads))};
     return by_head_dim(c.head_dim, [&](auto d) {
         constexpr int D = decltype(d)::value;
         const bool bf = c.dtype == TF_BF16;

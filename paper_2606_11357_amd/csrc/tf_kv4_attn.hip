@@ -30,18 +30,6 @@ constexpr uint32_t kFewParts = 16;       // parts that cost less to join than a 
 constexpr int kMostWgs = 1024;           // workgroups of a launch, at most (and counters in the workspace)
 constexpr int kJoinThreads = 512;
 
-// Division by a number that the host knows, of numbers below 2^31: with
-// 2^(s-1) < d <= 2^s and m = floor(2^(31+s) / d) + 1, n / d = n m >> 31 + s.
-struct Divisor {
-    uint32_t d = 1, m = 0, s = 0;
-    Divisor() = default;
-    explicit Divisor(uint32_t by) : d(by) {
-        while (d > 1u << s) ++s;
-        m = (uint32_t)(((uint64_t)1 << (31 + s)) / d + 1);
-    }
-    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (uint32_t)((uint64_t)n * m >> (31 + s)); }
-};
-
 struct AttnArgs {
     Kv4 cache;
     const uint16_t* q;
