@@ -218,10 +218,10 @@ __device__ __forceinline__ void place_row(const AppendArgs& a, const int32_t* cu
 
 // Every row of every token in order, one row on D / 16 lanes.  Moves 2 bytes a
 // value in, 2 out for rotated rows and D + 8 bytes a cached key and value; where
-// tokens are many it is bound by these and by the vector unit that makes the
-// codes (64% busy), else by a chain of four dependent loads (offsets, start,
+// tokens are many it is bound by the vector unit (91% busy: rotation, ranges,
+// codes) and by these, else by a chain of four dependent loads (offsets, start,
 // page, angles).  Two and four rows a lane group were no faster.  Measured (bf16,
-// 32/8 heads of 128): 4 x 4096 tokens 89 us (94 with the rotated rows through the
+// 32/8 heads of 128): 4 x 4096 tokens 88 us (93 with the rotated rows through the
 // L2), one token each of 64 sequences 5.0.
 template <bool BF, int D>
 __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
