@@ -386,7 +386,8 @@ int tf_kv4_attention(const tf_kv4_cache* cache, const void* Q, int64_t q_stride,
  *   O[i, h] = sum_j softmax_j(scale * Q[i, h] . K[j]) V[j]
  * for query i of sequence b over its keys j; with causal, only j <= i + n_k - n_q
  * (the queries are the last n_q of n_k tokens).  A query that sees no key gives
- * zeros.  cu_q and cu_k: int32 [batch + 1].  Q, K, V strided as above, O
+ * zeros; keys and values that it does not see do not act on it, NaN and infinite
+ * ones neither.  cu_q and cu_k: int32 [batch + 1].  Q, K, V strided as above, O
  * [tokens_q, q_heads, head_dim] contiguous.  Scores and sums in fp32, softmax
  * weights rounded to dtype for the matrix cores.  Rows of O that no sequence
  * owns are not written.  workspace: NULL, or at least

@@ -195,10 +195,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
     __shared__ __align__(16) uint16_t vs[2][kBN * D];
     __shared__ uint32_t wave_total[kWaves];
     __shared__ Block::Found found;
+    __shared__ int not_finite;
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
+    if (tid == 0) not_finite = 0;
     const uint32_t slot = blockIdx.x / (uint32_t)a.splits, split = blockIdx.x % (uint32_t)a.splits;
     const Block bl(a, slot, wave_total, &found);
     if (bl.sequence < 0) return;
@@ -394,10 +396,66 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         s[0] = next[0];
         s[1] = next[1];
     };
+    // A hidden value's weight is 0, which a value that is not finite would make NaN.
+    // Where some query of the block does not see all of a step's rows (the last row
+    // repeats past the end) such values leave the tile, and those of them that a
+    // query does see are added to its sums afterwards, from memory.  Whether the
+    // tile (or one before it) has any:
+    auto leave_out = [&](Lds* tile) __attribute__((always_inline)) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+        constexpr uint16_t INF = BF ? 0x7F80 : 0x7C00;
+        lds_u32x4* const mine = (lds_u32x4*)tile + tid;
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const u32x4 v = mine[i * 64 * kWaves];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[j] & 0x7FFF7FFFu));
+        }
+        if (most[0] >= INF || most[1] >= INF) {
+#pragma unroll 1
+            for (int i = 0; i < LOADS; ++i) {
+                u32x4 v = mine[i * 64 * kWaves];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if ((v[j] & 0x7FFFu) >= INF) v[j] &= 0xFFFF0000u;
+                    if ((v[j] >> 16 & 0x7FFFu) >= INF) v[j] &= 0xFFFFu;
+                }
+                mine[i * 64 * kWaves] = v;
+            }
+            not_finite = 1;
+        }
+        __syncthreads();
+        return not_finite != 0;
+    };
+    auto add_left_out = [&](int step) __attribute__((always_inline)) {
+        const int key0 = step * kBN, keys = wave_keys - key0 < kBN ? wave_keys - key0 : kBN;
+        const uint16_t* row = v_base + (int64_t)key0 * a.v_stride + 4 * half;
+#pragma unroll 1
+        for (int j = 0; j < keys; ++j, row += a.v_stride) {
+            const bool seen = key0 + j <= limit;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const u32x2 v = *reinterpret_cast<const u32x2*>(row + 32 * t + 2 * i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x = scale_f32<BF>((uint16_t)(v[e / 2] >> (16 * (e % 2))));
+                        if (seen && !(fabsf(x) < __builtin_inff())) o[t][i + e] += x;
+                    }
+                }
+        }
+    };
+    const int block_low = a.causal ? bl.block * kBM + past : n_k - 1;     // last key that all its queries see
     for (int step = step0; step < steps; ++step) {
         __builtin_amdgcn_s_waitcnt(0);                    // this wave's part of the tiles is there
         __syncthreads();                                  // everyone's is, and the other buffers are free
+        const bool left_out = step * kBN + kBN - 1 > block_low && leave_out(v_tile(step));
         one_step(step, k_tile(step), v_tile(step + 1), k_tile(step + 1), v_tile(step), k_base, v_base);
+        if (left_out) add_left_out(step);
     }
     const SwapPair sums = swap32(l);
     l = sums.a + sums.b;

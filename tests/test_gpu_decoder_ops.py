@@ -548,6 +548,51 @@ def test_prompt_hidden_keys_do_not_act(tf):
     assert not torch.isfinite(got[148:]).all()
 
 
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,n_q,n_k", [((4, 2, 64), [97, 150], [97, 190]), ((4, 4, 128), [150], [150]),
+                                           ((4, 1, 128), [70, 9], [3000, 300]), ((2, 1, 256), [200, 3], [140, 3])],
+                         ids=["64", "128", "128 after earlier keys", "256, more queries than keys"])
+def test_prompt_values_that_are_not_finite_act_where_seen(tf, dt, heads, n_q, n_k):
+    """A value that is not finite changes its dim of the queries that see it and
+    nothing else, wherever its tile is shared with queries that do not; a key
+    of NaN changes the queries that see it alone (the others' sums may move to a
+    new maximum at another step: two results, each within u |o| + u sum p |v| and
+    a fifth of that of fp32 error, so 5 u max |v| apart at most)."""
+    Hq, Hk, D = heads
+    q, k, v = (torch.randn(sum(n), h, D, device="cuda").to(DT[dt])
+               for n, h in ((n_q, Hq), (n_k, Hk), (n_k, Hk)))
+    cq, ck = offsets(n_q), offsets(n_k)
+    for causal in (True, False):
+        args = (i32(cq), i32(ck))
+        want = tf.prompt_attention(q, k, v, *args, causal=causal)
+        assert torch.isfinite(want).all()
+        for b in range(len(n_q)):
+            for back, bad in ((1, float("inf")), (2, float("-inf")), (33, float("nan")), (66, float("nan")),
+                              (90, float("inf"))):
+                j = n_k[b] - back
+                if j < 0:
+                    continue
+                sees = torch.zeros(sum(n_q), dtype=torch.bool, device="cuda")
+                i0 = max(0, j - (n_k[b] - n_q[b])) if causal else 0
+                sees[cq[b] + i0:cq[b + 1]] = True
+                w, h, d = v.clone(), back % Hk, (7 * back) % D
+                w[ck[b] + j, h, d] = bad
+                heads_of = slice(h * Hq // Hk, (h + 1) * Hq // Hk)
+                got = tf.prompt_attention(q, k, w, *args, causal=causal)
+                hit = got[sees][:, heads_of, d]
+                assert (torch.isnan(hit) if bad != bad else hit == bad).all(), (b, back, causal)
+                got[cq[b] + i0:cq[b + 1], heads_of, d] = want[cq[b] + i0:cq[b + 1], heads_of, d]
+                # a tile's other values are those it had, to the bit
+                assert torch.equal(got, want), (b, back, causal)
+                w = k.clone()
+                w[ck[b] + j, h, d] = float("nan")
+                got = tf.prompt_attention(q, w, v, *args, causal=causal)
+                assert torch.isnan(got[sees][:, heads_of]).all()
+                got[cq[b] + i0:cq[b + 1], heads_of] = want[cq[b] + i0:cq[b + 1], heads_of]
+                apart = (got.double() - want.double()).abs().max()
+                assert apart <= 5 * U[dt] * v.abs().max().double(), (b, back, causal)
+
+
 def test_prompt_offsets_that_do_not_fit(tf):
     """Sequences whose offsets leave the tensors or run backwards are left out."""
     q, k, v = (torch.randn(64, 2, 64, device="cuda").half() for _ in range(3))
