@@ -13,9 +13,9 @@
 //
 // Four waves of 32 queries share each step's 64 keys and values in LDS: with 128
 // dims a wave reads 32 KB of them a step for 1024 cycles of matrix instructions.  Measured (bf16, one causal prompt of 8192): 32 heads on 8 of 128
-// 527 us, 1044 TFLOP/s, matrix cores busy 57% of the time and vector units 49%, at
-// the clock that the card's power leaves; 16 heads of 64 167 us, 823; 8 of 256 321
-// us, 856.
+// 527 to 540 us, 1.02 to 1.04 PFLOP/s, matrix cores busy 57% of the time and vector units 49%, at
+// the clock that the card's power leaves; 16 heads of 64 165 us, 833 TFLOP/s; 8 of
+// 256 326 us, 843.
 #include "tf_internal.h"
 
 namespace tf {
@@ -400,7 +400,11 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
     // Where some query of the block does not see all of a step's rows (the last row
     // repeats past the end) such values leave the tile, and those of them that a
     // query does see are added to its sums afterwards, from memory.  Whether the
-    // tile (or one before it) has any:
+    // tile (or one before it) has any.  Measured, us without and with it (bf16): one
+    // prompt of 8192, 32 heads of 128, 529 / 529, 8 of 256 319 / 326; 2048, 16 of 64
+    // 28.4 / 29.7; seven of up to 333, 16 of 64, 9.7 / 10.3.  Blocks computed again
+    // with care only where their sums are not finite cost registers in every step:
+    // 8192, 32 heads of 128, 529 / 539, 8 heads on 8 of 256 341 / 362.
     auto leave_out = [&](Lds* tile) __attribute__((always_inline)) {
         typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
         typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
@@ -414,7 +418,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
             for (int j = 0; j < 4; ++j)
                 most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[j] & 0x7FFF7FFFu));
         }
-        if (most[0] >= INF || most[1] >= INF) {
+        if (__builtin_expect(most[0] >= INF || most[1] >= INF, false)) {
 #pragma unroll 1
             for (int i = 0; i < LOADS; ++i) {
                 u32x4 v = mine[i * 64 * kWaves];
@@ -431,6 +435,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         return not_finite != 0;
     };
     auto add_left_out = [&](int step) __attribute__((always_inline)) {
+        asm volatile("" : "+s"(step));                      // (its addresses are nothing to keep ready)
         const int key0 = step * kBN, keys = wave_keys - key0 < kBN ? wave_keys - key0 : kBN;
         const uint16_t* row = v_base + (int64_t)key0 * a.v_stride + 4 * half;
 #pragma unroll 1
@@ -455,7 +460,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void prompt_attn_ker
         __syncthreads();                                  // everyone's is, and the other buffers are free
         const bool left_out = step * kBN + kBN - 1 > block_low && leave_out(v_tile(step));
         one_step(step, k_tile(step), v_tile(step + 1), k_tile(step + 1), v_tile(step), k_base, v_base);
-        if (left_out) add_left_out(step);
+        if (__builtin_expect(left_out, false)) add_left_out(step);
     }
     const SwapPair sums = swap32(l);
     l = sums.a + sums.b;
