@@ -13,17 +13,14 @@
 #include <cmath>
 #include <cstdint>
 
+#include "tf_workspace.h"
 #include "tilefuse.h"
 
 namespace {
 
-PyObject* not_here() { return Py_NewRef(Py_NotImplemented); }
+using tf_binding::Held;
 
-// A reference held until the end of the scope.
-struct Held {
-    PyObject* o = nullptr;
-    ~Held() { Py_XDECREF(o); }
-};
+PyObject* not_here() { return Py_NewRef(Py_NotImplemented); }
 
 // A plain tensor (no subclass) on the GPU, with strides.
 const at::Tensor* on_gpu(PyObject* o) {
@@ -45,6 +42,7 @@ struct Ops {
     decltype(&tf_kv4_attention) decode;
     decltype(&tf_prompt_attention_workspace_bytes) prompt_bytes;
     decltype(&tf_prompt_attention) prompt;
+    tf_binding::CaptureFn capture;
 } g_ops;
 PyObject *g_ops_stream, *g_decode_ws, *g_prompt_ws, *g_make_ws;
 PyObject *g_name_data, *g_name_sizes, *g_name_device;
@@ -56,19 +54,20 @@ PyObject* bind(PyObject*, PyObject* args) {
     if (!PyArg_ParseTuple(args, "O!OO!O!O", &PyTuple_Type, &fns, &stream, &PyDict_Type, &decode_ws, &PyDict_Type,
                           &prompt_ws, &make))
         return nullptr;
-    unsigned long long at[7];
-    if (PyTuple_GET_SIZE(fns) != 7) {
-        PyErr_SetString(PyExc_ValueError, "bind needs seven functions");
+    unsigned long long at[8];
+    if (PyTuple_GET_SIZE(fns) != 8) {
+        PyErr_SetString(PyExc_ValueError, "bind needs eight functions");
         return nullptr;
     }
-    for (int i = 0; i < 7; ++i) {
+    for (int i = 0; i < 8; ++i) {
         at[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(fns, i));
         if (PyErr_Occurred()) return nullptr;
     }
     g_ops = {reinterpret_cast<decltype(Ops::norm)>(at[0]),         reinterpret_cast<decltype(Ops::append)>(at[1]),
              reinterpret_cast<decltype(Ops::read)>(at[2]),         reinterpret_cast<decltype(Ops::decode_bytes)>(at[3]),
              reinterpret_cast<decltype(Ops::decode)>(at[4]),       reinterpret_cast<decltype(Ops::prompt_bytes)>(at[5]),
-             reinterpret_cast<decltype(Ops::prompt)>(at[6])};
+             reinterpret_cast<decltype(Ops::prompt)>(at[6]),
+             reinterpret_cast<decltype(Ops::capture)>(at[7])};
     Py_XSETREF(g_ops_stream, Py_NewRef(stream));
     Py_XSETREF(g_decode_ws, Py_NewRef(decode_ws));
     Py_XSETREF(g_prompt_ws, Py_NewRef(prompt_ws));
@@ -140,19 +139,17 @@ struct Cache {
     }
 };
 
-// The workspace of an attention call: None the device's cached one, False none
+// The workspace of an attention call on `stream`: None the cached one, False none
 // (where allowed), or the caller's.
-bool workspace_of(PyObject* o, PyObject* cached, PyObject* any, int dev, int64_t need, Held& held, void*& ws,
-                  size_t& bytes) {
+bool workspace_of(PyObject* o, PyObject* cached, PyObject* any, int dev, void* stream, int64_t need, Held& held,
+                  void*& ws, size_t& bytes) {
     ws = nullptr;
     bytes = 0;
     if (o == Py_False) return true;
     const at::Tensor* t = nullptr;
     if (o == Py_None) {
         if (need == 0) return true;
-        const Held key{PyLong_FromLong(dev)};
-        held.o = key.o ? Py_XNewRef(PyDict_GetItemWithError(cached, key.o)) : nullptr;
-        if (!held.o && PyErr_Occurred()) return false;
+        if (!tf_binding::find_workspace(cached, g_ops.capture, dev, stream, held)) return false;
         t = held.o ? plain(held.o) : nullptr;
         if (!t || (int64_t)t->nbytes() < need) {
             const Held device{PyObject_GetAttr(any, g_name_device)};
@@ -348,9 +345,9 @@ PyObject* decode_common(PyObject* const* a, Py_ssize_t n) {
     void *ws, *stream;
     size_t ws_bytes;
     if (a[6] == Py_False) return not_here();
-    if (!workspace_of(a[6], g_decode_ws, a[0], dev, need, held, ws, ws_bytes))
-        return PyErr_Occurred() ? nullptr : not_here();
     if (!stream_of(dev, stream)) return nullptr;
+    if (!workspace_of(a[6], g_decode_ws, a[0], dev, stream, need, held, ws, ws_bytes))
+        return PyErr_Occurred() ? nullptr : not_here();
     at::Tensor made;
     if (!out) {
         made = at::empty(q->sizes(), q->options().requires_grad(false));
@@ -391,9 +388,9 @@ PyObject* prompt_common(PyObject* const* a, Py_ssize_t n) {
     Held held;
     void *ws, *stream;
     size_t ws_bytes;
-    if (!workspace_of(a[8], g_prompt_ws, a[0], dev, need, held, ws, ws_bytes))
-        return PyErr_Occurred() ? nullptr : not_here();
     if (!stream_of(dev, stream)) return nullptr;
+    if (!workspace_of(a[8], g_prompt_ws, a[0], dev, stream, need, held, ws, ws_bytes))
+        return PyErr_Occurred() ? nullptr : not_here();
     at::Tensor made;
     if (!out) {
         made = at::empty({T, H, D}, q->options().requires_grad(false));

@@ -1,0 +1,33 @@
+// What the native parts of the binding share: the look-up of a cached workspace
+// (tilefuse.py makes them and says how they are kept).
+#pragma once
+
+#include <Python.h>
+
+#include <cstdint>
+
+namespace tf_binding {
+
+// A reference held until the end of the scope.
+struct Held {
+    PyObject* o = nullptr;
+    ~Held() { Py_XDECREF(o); }
+};
+
+// The runtime's query of a stream's capture: its state (0: none) and its number.
+using CaptureFn = int (*)(void* stream, int* state, unsigned long long* number);
+
+// The workspace kept in `cached` under (device, stream, capture), or none (null).
+// False: not to be told here, or a Python error.
+inline bool find_workspace(PyObject* cached, CaptureFn capture, int dev, void* stream, Held& found) {
+    int state = 0;
+    unsigned long long number = 0;
+    // (the default stream cannot be captured)
+    if (stream && (!capture || capture(stream, &state, &number) != 0)) return false;
+    const Held key{Py_BuildValue("(iKK)", dev, (unsigned long long)(uintptr_t)stream, state ? number + 1 : 0ULL)};
+    if (!key.o) return false;
+    found.o = Py_XNewRef(PyDict_GetItemWithError(cached, key.o));
+    return found.o || !PyErr_Occurred();
+}
+
+}  // namespace tf_binding

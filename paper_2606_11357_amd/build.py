@@ -110,7 +110,7 @@ def build_binding(src: str | None = None, out: str | None = None) -> str:
 
     import torch
     from torch.utils import cpp_extension
-    inc = [f"-I{d}" for d in cpp_extension.include_paths()] + [f"-I{INCLUDE}", f"-I{sysconfig.get_paths()['include']}"]
+    inc = [f"-I{d}" for d in cpp_extension.include_paths()] + [f"-I{INCLUDE}", f"-I{os.path.join(PKG, 'binding')}", f"-I{sysconfig.get_paths()['include']}"]
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *inc, src,

@@ -154,6 +154,55 @@ def workspace_bytes(bits: int, M: int, K: int, N: int, group: int = 128) -> int:
     return int(n)
 
 
+# Arrival counters are in the first bytes of every workspace; nothing else in one
+# needs an initial value.
+_COUNTER_BYTES = 8192
+
+
+def _capture_of(stream: int) -> int:
+    """The graph capture that the stream of that handle is in: a number that no other
+    capture has, or 0 where it is in none."""
+    if stream == 0:                      # the default stream cannot be captured
+        return 0
+    state, number = ctypes.c_int(0), ctypes.c_ulonglong(0)
+    if load().hipStreamGetCaptureInfo(ctypes.c_void_p(stream), ctypes.byref(state), ctypes.byref(number)) != 0:
+        raise TileFuseError(TF_ERR_HIP, "hipStreamGetCaptureInfo")
+    return number.value + 1 if state.value else 0
+
+
+def _place(device):
+    """What a cached workspace is kept under: device, current stream, its capture."""
+    torch = _torch()
+    device = torch.device(device)
+    index = torch.cuda.current_device() if device.index is None else device.index
+    stream = torch.cuda.current_stream(index).cuda_stream
+    return index, stream, _capture_of(stream)
+
+
+def _stream_workspace(cache, device, nbytes, counters=True):
+    """A workspace of at least nbytes for calls on the current stream, cached.
+
+    Each stream has its own, made, used and (where a call needs more) given back in
+    that stream's order.  A call under capture takes one of the graph's: from the
+    memory of the graph (torch.cuda.graph's), its counters cleared by a captured
+    fill, so that neither a replay nor an eager call ever meets what the other
+    left.  It serves the calls of that capture; the next capture gives it back."""
+    torch = _torch()
+    key = _place(device)
+    buf = cache.get(key)
+    if buf is None or buf.numel() < nbytes:
+        if key[2]:
+            for old in [k for k in list(cache) if k[2] not in (0, key[2])]:
+                cache.pop(old, None)
+            buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            if counters:
+                buf[:_COUNTER_BYTES].zero_()
+        else:
+            buf = (torch.zeros if counters else torch.empty)(nbytes, dtype=torch.uint8, device=device)
+        cache[key] = buf
+    return buf
+
+
 _default_ws = {}
 
 
@@ -410,7 +459,8 @@ def _native_ops():
         at = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value  # noqa: E731
         native.bind(tuple(at(n) for n in ("tf_add_rms_norm", "tf_kv4_append", "tf_kv4_read",
                                               "tf_kv4_attention_workspace_bytes", "tf_kv4_attention",
-                                              "tf_prompt_attention_workspace_bytes", "tf_prompt_attention")),
+                                              "tf_prompt_attention_workspace_bytes", "tf_prompt_attention",
+                                              "hipStreamGetCaptureInfo")),
                         torch._C._cuda_getCurrentRawStream, _attention_ws, _prompt_ws, _cached_workspace)
         _ops = {n: getattr(native, n) for n in names}
     return _ops
@@ -601,14 +651,9 @@ _attention_ws, _prompt_ws = {}, {}
 
 
 def _cached_workspace(cache, device, nbytes):
-    """A zero-filled workspace for the attention calls, cached per device (decode
-    and prompt attention have one each); like the matmuls' (default_workspace) it
-    must not be shared by calls that run concurrently on different streams."""
-    torch = _torch()
-    buf = cache.get(device.index)
-    if buf is None or buf.numel() < nbytes:
-        buf = cache[device.index] = torch.zeros(nbytes, dtype=torch.uint8, device=device)
-    return buf
+    """The attention calls' workspace (decode and prompt attention have one each), of
+    which prompts need no counters."""
+    return _stream_workspace(cache, device, nbytes, cache is not _prompt_ws)
 
 
 def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
@@ -617,9 +662,10 @@ def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
     q: [batch, q_heads, head_dim] or [batch, q_len, q_heads, head_dim] (q_len up
     to 8), lens: int32 [batch], the cached tokens with the asking ones; token i
     sees the positions up to lens - q_len + i.  scale: 1 / sqrt(head_dim) unless
-    given.  workspace: None for the cached per-device one, or zero-filled bytes
-    (kv4_attention_workspace_bytes) of the caller's for calls on several
-    streams.  Returns a tensor of q's shape."""
+    given.  workspace: None for a cached one of the current stream (under
+    torch.cuda.graph one of the graph's), or zero-filled bytes
+    (kv4_attention_workspace_bytes) of the caller's, which calls that may run
+    concurrently must not share.  Returns a tensor of q's shape."""
     got = _call("decode", "tf_kv4_attention", q, cache, table, lens, scale, out, workspace)
     if got is not NotImplemented:
         return got
@@ -665,10 +711,11 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None
     """Attention over packed prompts: q [tokens, q_heads, head_dim], k and v
     [keys, kv_heads, head_dim] (parts of one packed projection are fine), cu_q and
     cu_k int32 [batch + 1] (cu_k is cu_q unless given).  causal: the queries are
-    the last of their sequence's keys.  workspace: None for the cached per-device
-    one, False for none (keys are then never split over workgroups), or bytes
-    (prompt_attention_workspace_bytes) of the caller's for calls on several
-    streams.  Returns [tokens, q_heads, head_dim]."""
+    the last of their sequence's keys.  workspace: None for a cached one of the
+    current stream (under torch.cuda.graph one of the graph's), False for none
+    (keys are then never split over workgroups), or bytes
+    (prompt_attention_workspace_bytes) of the caller's, which calls that may run
+    concurrently must not share.  Returns [tokens, q_heads, head_dim]."""
     got = _call("prompt", "tf_prompt_attention", q, k, v, cu_q, cu_k, scale, causal, out, workspace)
     if got is not NotImplemented:
         return got
