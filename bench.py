@@ -576,7 +576,7 @@ def main():
     # follow each other on the GPU without gaps; each graph replay costs a
     # launch gap of its own, which one replay per phase keeps out of the
     # per-kernel figures.
-    gemm_one(gemm[0], 0)     # allocates the default workspace before capture
+    gemm_one(gemm[0], 0)     # once outside a capture, which brings its own workspace
     torch.cuda.synchronize()
     graphs = []
     for g in gemm:

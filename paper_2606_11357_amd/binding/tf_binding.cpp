@@ -18,7 +18,11 @@
 
 #include <cstdint>
 
+#include "tf_workspace.h"
+
 namespace {
+
+using tf_binding::Held;
 
 using MatmulFn = int (*)(const uint16_t*, const void*, uint16_t*, int64_t, int64_t, int64_t, int, void*, size_t, void*);
 using BytesFn = int64_t (*)(int, int64_t, int64_t, int64_t, int);
@@ -27,15 +31,17 @@ constexpr int kFns = 8;                  // (bits 4, 8) x (gemm, gemv) x (fp16, 
 MatmulFn g_fn[kFns];
 BytesFn g_bytes;
 PyObject* g_stream;                      // device index -> current stream's handle
-PyObject* g_workspaces;                  // device index -> cached workspace
+tf_binding::CaptureFn g_capture;         // a stream's capture
+PyObject* g_workspaces;                  // (device, stream, capture) -> cached workspace
 PyObject* g_workspace;                   // (device, bytes) -> workspace, grown if need be
 
 // bind((address of each matmul function), address of tf_workspace_bytes,
-//      current stream function, workspace dict, default_workspace)
+//      current stream function, workspace dict, default_workspace,
+//      address of the query of a stream's capture)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject *fns, *stream, *dict, *ws;
-    unsigned long long bytes;
-    if (!PyArg_ParseTuple(args, "O!KOO!O", &PyTuple_Type, &fns, &bytes, &stream, &PyDict_Type, &dict, &ws))
+    unsigned long long bytes, capture = 0;
+    if (!PyArg_ParseTuple(args, "O!KOO!O|K", &PyTuple_Type, &fns, &bytes, &stream, &PyDict_Type, &dict, &ws, &capture))
         return nullptr;
     if (PyTuple_GET_SIZE(fns) != kFns) {
         PyErr_SetString(PyExc_ValueError, "bind needs eight functions");
@@ -47,6 +53,7 @@ PyObject* bind(PyObject*, PyObject* args) {
         g_fn[i] = reinterpret_cast<MatmulFn>(a);
     }
     g_bytes = reinterpret_cast<BytesFn>(bytes);
+    g_capture = reinterpret_cast<tf_binding::CaptureFn>(capture);
     Py_XSETREF(g_stream, Py_NewRef(stream));
     Py_XSETREF(g_workspaces, Py_NewRef(dict));
     Py_XSETREF(g_workspace, Py_NewRef(ws));
@@ -55,17 +62,19 @@ PyObject* bind(PyObject*, PyObject* args) {
 
 PyObject* not_here() { return Py_NewRef(Py_NotImplemented); }
 
-// A reference held until the end of the scope.
-struct Held {
-    PyObject* o = nullptr;
-    ~Held() { Py_XDECREF(o); }
-};
-
 // A plain tensor (no subclass) on the GPU, contiguous.
 const at::Tensor* plain(PyObject* o) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
     return t.is_cuda() && t.layout() == at::kStrided && t.is_contiguous() ? &t : nullptr;
+}
+
+bool stream_of(int dev, void*& stream) {
+    const Held index{PyLong_FromLong(dev)};
+    const Held handle{index.o ? PyObject_CallOneArg(g_stream, index.o) : nullptr};
+    if (!handle.o) return false;
+    stream = PyLong_AsVoidPtr(handle.o);
+    return true;
 }
 
 PyObject* matmul_common(PyObject* const* a, Py_ssize_t n) {
@@ -92,14 +101,14 @@ PyObject* matmul_common(PyObject* const* a, Py_ssize_t n) {
     Held held;                       // the cached workspace, over the call
     void* ws = nullptr;
     size_t ws_bytes = 0;
+    void* stream = nullptr;
     if (ws_o == Py_None) {
         const int64_t need = g_bytes((int)bits, M, K, N, (int)group);
         if (need < 0) return not_here();
         if (need > 0) {
-            const Held key{PyLong_FromLong(dev)};
-            if (!key.o) return nullptr;
-            held.o = Py_XNewRef(PyDict_GetItemWithError(g_workspaces, key.o));
-            if (!held.o && PyErr_Occurred()) return nullptr;
+            if (!stream_of(dev, stream)) return nullptr;
+            if (!tf_binding::find_workspace(g_workspaces, g_capture, dev, stream, held))
+                return PyErr_Occurred() ? nullptr : not_here();
             const at::Tensor* t = held.o ? plain(held.o) : nullptr;
             if (!t || t->numel() < need) {
                 const Held device{PyObject_GetAttrString(a[2], "device")};
@@ -129,10 +138,7 @@ PyObject* matmul_common(PyObject* const* a, Py_ssize_t n) {
             out->size(1) != N)
             return not_here();
     }
-    const Held index{PyLong_FromLong(dev)};
-    const Held handle{index.o ? PyObject_CallOneArg(g_stream, index.o) : nullptr};
-    if (!handle.o) return nullptr;
-    void* stream = PyLong_AsVoidPtr(handle.o);
+    if (!held.o && !stream_of(dev, stream)) return nullptr;
     const MatmulFn fn = g_fn[(bits == 8 ? 4 : 0) + (gemv ? 2 : 0) + (bf ? 1 : 0)];
     const uint16_t* x = static_cast<const uint16_t*>(A->data_ptr());
     const void* pk = packed->data_ptr();

@@ -207,20 +207,14 @@ _default_ws = {}
 
 
 def default_workspace(device, nbytes: int):
-    """A zero-filled workspace of at least `nbytes`, cached per device.
+    """A zero-filled workspace of at least `nbytes`, cached per device and stream
+    (and, under capture, per capture: _stream_workspace).
 
     Every call returns the workspace's arrival counters to zero, so the cached
-    buffer serves later calls of any shape without clearing; it must not be
-    shared by calls running concurrently on different streams (pass your own
-    workspace for that).
+    buffer serves later calls of any shape on its stream without clearing; it must
+    not be shared by calls running concurrently on different streams.
     """
-    torch = _torch()
-    key = torch.device(device).index if torch.device(device).index is not None else torch.cuda.current_device()
-    buf = _default_ws.get(key)
-    if buf is None or buf.numel() < nbytes:
-        buf = torch.zeros(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
-        _default_ws[key] = buf
-    return buf
+    return _stream_workspace(_default_ws, device, max(nbytes, 1 << 20))
 
 
 def pack_w4(qweight, qzeros, scales, K: int, N: int, group: int = 128, out=None):
@@ -281,7 +275,8 @@ def _native():
         fns = tuple(at(f"tf_w{bits}a16_{kind}{dt}") for bits in (4, 8) for kind in ("gemm", "gemv")
                     for dt in ("", "_bf16"))
         stream = torch._C._cuda_getCurrentRawStream
-        _tf_binding.bind(fns, at("tf_workspace_bytes"), stream, _default_ws, default_workspace)
+        _tf_binding.bind(fns, at("tf_workspace_bytes"), stream, _default_ws, default_workspace,
+                         at("hipStreamGetCaptureInfo"))
         _bound = _tf_binding.matmul
     return _bound
 
@@ -301,7 +296,7 @@ def _matmul(bits, kind, A, packed, K, N, group, out, workspace):
 def _matmul_general(bits, kind, A, packed, K, N, group, out, workspace):
     """A fp16 or bfloat16 [M, K] selects the entry point (the packed scales must
     hold the same dtype's bits); the output has A's dtype.
-    workspace: None -> the cached per-device default, False -> none (single-pass
+    workspace: None -> the current stream's cached default, False -> none (single-pass
     kernels), or a caller tensor (zero-filled before its first use)."""
     torch = _torch()
     _need_cuda(A, packed, out)

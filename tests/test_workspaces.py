@@ -54,6 +54,11 @@ def test_attention_workspaces(monkeypatch):
     check_cached(Caller(monkeypatch), decode_ws(cache), cache)
 
 
+def test_matmul_workspaces(monkeypatch):
+    monkeypatch.setattr(tf, "_default_ws", {})
+    check_cached(Caller(monkeypatch), lambda n: tf.default_workspace(torch.device("cpu", 0), n), tf._default_ws)
+
+
 # ---------------------------------------------------------------------------
 # on the GPU
 # ---------------------------------------------------------------------------
@@ -81,6 +86,17 @@ def chunk_case(n, past):
     q, k = torch.randn(n, 16, 128, device="cuda").bfloat16(), torch.randn(n + past, 2, 128, device="cuda").bfloat16()
     cu, ck = i32(0, n), i32(0, n + past)
     return lambda: tf.prompt_attention(q, k, k, cu, ck)
+
+
+def matmul_case(M, K, N, kind):
+    """A matmul whose K is split over workgroups."""
+    torch.manual_seed(5)
+    word = lambda *shape: torch.randint(-2 ** 31, 2 ** 31, shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    s = (0.01 * torch.rand((K // 128, N), device="cuda")).half()
+    packed = tf.pack_w4(word(K, N // 8), word(K // 128, N // 8), s, K, N)
+    x = torch.randn(M, K, device="cuda").half()
+    assert tf.workspace_bytes(4, M, K, N) > 0
+    return lambda: getattr(tf, f"w4a16_{kind}")(x, packed, K, N)
 
 
 def captured(call):
@@ -111,8 +127,10 @@ def test_captures_are_told_apart():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("small,large", [(lambda: decode_case([9000, 50], 1), lambda: decode_case([9000, 50], 4)),
-                                         (lambda: chunk_case(200, 3000), lambda: chunk_case(500, 7000))],
-                         ids=["decode", "prompt"])
+                                         (lambda: chunk_case(200, 3000), lambda: chunk_case(500, 7000)),
+                                         (lambda: matmul_case(1, 14336, 4096, "gemv"),
+                                          lambda: matmul_case(200, 12288, 4096, "gemm"))],
+                         ids=["decode", "prompt", "matmul"])
 def test_graph_on_the_default_workspace(small, large):
     """Captured, then a call that needs more and tensors of every size, then replays:
     each as the eager call, with eager calls in between, and no tensor touched."""
@@ -134,9 +152,11 @@ def test_graph_on_the_default_workspace(small, large):
 
 
 @pytest.mark.gpu
-def test_first_call_on_a_stream_is_a_captured_one():
+@pytest.mark.parametrize("case", [lambda: decode_case([9000, 50], 1), lambda: matmul_case(1, 14336, 4096, "gemv")],
+                         ids=["decode", "matmul"])
+def test_first_call_on_a_stream_is_a_captured_one(case):
     """Eager calls on the stream of a capture, before any replay of its graph."""
-    call = decode_case([9000, 50], 1)
+    call = case()
     want = call()
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
@@ -158,14 +178,16 @@ def test_first_call_on_a_stream_is_a_captured_one():
 def test_streams_side_by_side():
     """The default workspace on two streams at once."""
     a, b = decode_case([9000, 50], 1), decode_case([7000, 5000], 1)
-    want = a(), b()
+    c, d = matmul_case(1, 14336, 4096, "gemv"), matmul_case(2, 14336, 4096, "gemv")
+    calls = a, b, c, d
+    want = [f() for f in calls]
     torch.cuda.synchronize()
     streams = torch.cuda.Stream(), torch.cuda.Stream()
     got = []
     for _ in range(20):
-        for s, f in zip(streams, (a, b)):
-            with torch.cuda.stream(s):
+        for i, f in enumerate(calls):
+            with torch.cuda.stream(streams[i % 2]):
                 got.append(f())
     torch.cuda.synchronize()
     for i, t in enumerate(got):
-        assert torch.equal(t, want[i % 2])
+        assert torch.equal(t, want[i % 4])
