@@ -55,6 +55,19 @@ struct AttnArgs {
 template <bool BF> constexpr float kOffA = BF ? 128.f : 1024.f;   // nibbles 0, 2
 template <bool BF> constexpr float kOffB = BF ? 128.f : 64.f;     // nibbles 1, 3
 
+// The weights go to the matrix cores as e s_v, e = 2^(scale2 x - base).  With base
+// the maximum, e <= 1, fp16 has no room for them: under a scale of 2^-8 a key of
+// 2^-6 of the largest weight would lose digits and one of 2^-17 be lost, in the
+// numerator alone.  So base is the maximum less `places`, the most for which no e s_v
+// passes 2^12 (2^15 is there: the maximum's own rounding may add some), by the
+// exponent of the largest |s_v| that the row has seen: |s_v| < 2^(field - 14).  (8192
+// keys, a sink of 91% of the weight, values of 0.1: error 1.2e-3 -> 1e-5 before the
+// output's rounding; 65536, 10% outside the sink, of 0.05: 0.16 -> 5e-6.)  The sums of
+// weights have the same power, which so leaves with them.  bf16 has fp32's exponents.
+// It costs 1 or 2% (64 ragged sequences 50.2 -> 50.3 us, one of 513 keys 8.7 -> 8.9,
+// two of 65537 with four tokens of one head of 256, for a spill, 27.1 -> 28.4).
+constexpr int kMostPlaces = 12 + 14;
+
 struct Magic { uint32_t a, b; };
 template <bool BF>
 __device__ __forceinline__ Magic magics(uint32_t sign) {
@@ -91,6 +104,12 @@ __device__ __forceinline__ float max_over_groups(float v) {
     const SwapPair r = swap16(v);
     const SwapPair h = swap32(fmaxf(r.a, r.b));
     return fmaxf(h.a, h.b);
+}
+
+__device__ __forceinline__ uint32_t max_over_groups(uint32_t v) {
+    auto most = [](auto r) { return r[0] > r[1] ? r[0] : r[1]; };
+    v = most(__builtin_amdgcn_permlane16_swap(v, v, false, false));
+    return most(__builtin_amdgcn_permlane32_swap(v, v, false, false));
 }
 
 // What lane % 16 of the first group holds.
@@ -535,8 +554,10 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
         }
         float4_t o[SUMS], osum[NR];       // osum: rows 0..2 of the further operand
         float m[NR], l[NR];               // maximum of scale-free scores; sum of weights
+        int places[NR];                   // the weights' powers of two (see kMostPlaces)
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
+            places[n] = BF ? 0 : kMostPlaces;
             m[n] = -__builtin_inff();
             l[n] = 0.f;
             osum[n] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -576,6 +597,15 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
                 // slot i of the lane: key 16 (i / 4) + 4 g + i % 4 of the tile
                 const int key0 = (int)(t * kKvTile) + 4 * g;
                 const bool edge = !here || (int)(t * kKvTile) + kKvTile - 1 > (int)len - a.q_len;
+                uint32_t scale_bits = 0;  // fp16: of the largest |s_v| of the lane's keys
+                if constexpr (!BF) {
+                    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+                    u16x2 most = {0, 0};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, meta[2][i] & 0x7FFF7FFFu));
+                    scale_bits = most[0] > most[1] ? most[0] : most[1];
+                }
                 u32x4 p[NR], zrow = meta[3];
                 if (edge) {               // no zero-points of positions that were never written
 #pragma unroll
@@ -590,18 +620,32 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
                     for (int i = 0; i < 8; ++i)
                         x[i] = fmaf(-meta_f32<BF>(meta[1], i), sum_q[n], s[n][i / 4][i % 4]) *
                                meta_f32<BF>(meta[0], i);
+                    uint32_t bits = scale_bits;             // ... that the row sees
                     if (edge) {
                         const int seen = (here ? limit[n] : -1) - key0;
+                        bits = 0;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (16 * (i / 4) + i % 4 > seen) x[i] = -__builtin_inff();
+                        for (int i = 0; i < 8; ++i) {
+                            if (16 * (i / 4) + i % 4 > seen) {
+                                x[i] = -__builtin_inff();
+                            } else if constexpr (!BF) {
+                                const uint32_t sv = meta[2][i / 2] >> 16 * (i % 2) & 0x7FFFu;
+                                bits = sv > bits ? sv : bits;
+                            }
+                        }
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
                     top = max_over_groups(top);
-                    if (__any(top > m[n])) {
+                    if (__any(top > m[n] || (!BF && (int)(bits >> 10) > kMostPlaces - places[n]))) {
+                        int fewer = 0;
+                        if constexpr (!BF) {                // (a NaN among the scales makes the row NaN)
+                            const int room = kMostPlaces - (int)(max_over_groups(bits) >> 10);
+                            fewer = room < places[n] ? places[n] - room : 0;
+                            places[n] -= fewer;
+                        }
                         const float f =
-                            top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m[n] - top) * a.scale2);
+                            top == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m[n] - top) * a.scale2 - fewer);
                         const bool sums_yet = __any(m[n] != -__builtin_inff());
                         m[n] = top;
                         if (sums_yet) {
@@ -611,7 +655,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
                             for (int k = 0; k < NT; ++k) o[n * NT + k] *= f;
                         }
                     }
-                    const float base = m[n] == -__builtin_inff() ? 0.f : m[n] * a.scale2;
+                    const float base = m[n] == -__builtin_inff() ? 0.f : fmaf(m[n], a.scale2, -places[n]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const float e = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale2, -base));
@@ -666,8 +710,9 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
                 o[n * NT + w] -= ca;
                 o[n * NT + NW + w] -= cb;
             }
+            m[n] = fmaf(m[n], a.scale2, -places[n]);
             if (g == 0) {
-                ms[n * 16 + c][wave] = m[n] * a.scale2;
+                ms[n * 16 + c][wave] = m[n];
                 ls[n * 16 + c][wave] = l[n];
             }
         }
@@ -691,7 +736,7 @@ __global__ __launch_bounds__(64 * W, waves_per_simd(D, NR)) void kv4_attn_kernel
             sums[n] = 0.f;
 #pragma unroll
             for (int w = 0; w < W; ++w) sums[n] = fmaf(lw[w], weight_of(mw[w], tops[n]), sums[n]);
-            const float f = weight_of(m[n] * a.scale2, tops[n]);
+            const float f = weight_of(m[n], tops[n]);
 #pragma unroll
             for (int k = 0; k < NT; ++k) o[n * NT + k] *= f;
         }
