@@ -89,3 +89,29 @@ def test_decode_of_hidden_large_values(tf, new):
         out.append(tf.kv4_attention(q, cache, table, i32([n + 1 if new > 1 else n])))
     seen = new - 1 if new > 1 else 1
     assert torch.equal(out[0][:, :seen], out[1][:, :seen])
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("split", [False, None], ids=["whole", "split"])
+@pytest.mark.parametrize("heads,n_q,n_k,margin", [((4, 1, 128), 9, 30000, 16.23), ((2, 2, 64), 3, 65536, 16.23),
+                                                  ((2, 1, 256), 5, 20000, 15.5), ((2, 1, 128), 130, 4000, 12.0)], ids=str)
+def test_prompt_beside_a_key_that_takes_most(tf, dt, split, heads, n_q, n_k, margin):
+    """Per query: u for the output, u sum p |v| for the rounded weights (fp16: those
+    under 2^-21 of the largest lose at most 2^-32 each), the scores' fp32 error e as in
+    check_prompt."""
+    Hq, Hk, D = heads
+    rng = np.random.default_rng(n_k)
+    d = rng.choice([-1.0, 1.0], D)
+    k = 0.01 * rng.standard_normal((n_k, Hk, D))
+    k[0] = d * margin / D ** 0.5
+    v = rng.standard_normal((n_k, Hk, D)) + 0.5
+    v[0] *= 0.01
+    (q, qv), (k, kv), (v, vv) = (up(t, dt) for t in (np.broadcast_to(d, (n_q, Hq, D)), k, v))
+    got = down(tf.prompt_attention(q, k, v, i32([0, n_q]), i32([0, n_k]), workspace=split))
+    u, least = (2.0 ** -11, 2.0 ** -32) if dt == "f16" else (2.0 ** -8, 0.0)
+    for h in range(Hq):
+        one = (qv[:, h], kv[:, h * Hk // Hq], vv[:, h * Hk // Hq], D ** -0.5, n_k - n_q + np.arange(n_q))
+        want, bound = oracle.attend(*one), oracle.attend_bound(*one)
+        e = 2.0 ** -21 * D ** -0.5 * D * np.abs(kv).max()
+        tol = u * np.abs(want) + (u + 2 * e + 2.0 ** -20) * bound + least * (n_k * np.abs(vv).max() + 128)
+        assert (np.abs(got[:, h] - want) <= tol).all(), (h, np.abs(got[:, h] - want).max(), tol.min())
