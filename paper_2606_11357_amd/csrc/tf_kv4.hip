@@ -11,6 +11,14 @@ typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 // Measured, 8 heads of 128, us row by row and tile by tile: 2000 tokens (2 M
 // values) 5.4 / 6.3, 4097 8.5 / 7.7, 8192 13.2 / 10.9.
 constexpr int64_t kTileValues = 1 << 22;
+// What a sequence has to have of them for that, and of tokens: each brings tiles of
+// which part is read for nothing.  And the most sequences, in all and by the elements
+// of a token: a workgroup for tiles looks through all of them.  Measured likewise,
+// tokens x sequences: 8 heads of 128, 1 x 5120 14.5 / 619, 16 x 320 9.5 / 14.4, 64 x 80
+// 8.5 / 8.3, 64 x 1024 91 / 81, 128 x 2048 578 / 464, 256 x 4000 2285 / 3767; 2 of 256,
+// 64 x 512 24.8 / 20.9; 4 of 64, 64 x 512 18.0 / 19.8, 128 x 1024 65.7 / 63.8, 128 x
+// 2048 139 / 178; 1 of 64, 512 x 128 7.8 / 9.4, 8192 x 64 42 / 45.
+constexpr int64_t kTileValuesEach = 1 << 15, kTileTokensEach = 64, kTileLeastElements = 128, kTileMostBatch = 2048;
 constexpr int kStagedBatch = 1024;     // up to this many sequences' offsets are searched in LDS
 
 struct AppendArgs {
@@ -467,6 +475,13 @@ int64_t most_tiles(int64_t batch, int64_t tokens) {
     return (tokens + 62 * runs) / kKvTile;
 }
 
+// Whether a read goes tile by tile; elements: of a token's keys.
+bool by_tiles(int64_t batch, int64_t tokens, int64_t elements) {
+    const int64_t values = tokens * elements, most = 4 * elements < kTileMostBatch ? 4 * elements : kTileMostBatch;
+    return values >= kTileValues && values >= kTileValuesEach * batch && tokens >= kTileTokensEach * batch &&
+           elements >= kTileLeastElements && batch <= most;
+}
+
 Kv4 device_view(const tf_kv4_cache& c) {
     Kv4 v;
     v.data = static_cast<uint8_t*>(c.data);
@@ -509,11 +524,11 @@ int launch_kv4_read(const tf_kv4_cache& c, const int32_t* cu, const int32_t* sta
     return by_head_dim(c.head_dim, [&](auto d) {
         constexpr int D = decltype(d)::value;
         const bool bf = c.dtype == TF_BF16;
-        if (tokens * c.kv_heads * D >= kTileValues) {
-            const uint32_t per_slot = (uint32_t)(2 * c.kv_heads + 3) / 4;
-            const dim3 grid((unsigned)most_tiles(batch, tokens) * per_slot);
-            return bf ? launch(kv4_read_tiles_kernel<true, D>, grid, dim3(256), 0, s, a, per_slot)
-                      : launch(kv4_read_tiles_kernel<false, D>, grid, dim3(256), 0, s, a, per_slot);
+        const int64_t per_slot = (2 * (int64_t)c.kv_heads + 3) / 4, wgs = most_tiles(batch, tokens) * per_slot;
+        if (by_tiles(batch, tokens, c.kv_heads * D) && wgs * 256 <= UINT32_MAX) {
+            const dim3 grid((unsigned)wgs);
+            return bf ? launch(kv4_read_tiles_kernel<true, D>, grid, dim3(256), 0, s, a, (uint32_t)per_slot)
+                      : launch(kv4_read_tiles_kernel<false, D>, grid, dim3(256), 0, s, a, (uint32_t)per_slot);
         }
         const dim3 grid((unsigned)((tokens * 2 * c.kv_heads * (D / 16) + 255) / 256));
         return bf ? launch(kv4_read_kernel<true, D>, grid, dim3(256), 0, s, a)
