@@ -171,9 +171,7 @@ def main(argv=None):
     pos = torch.full((a.batch,), a.prompt, device="cuda", dtype=torch.int32)
     lens = pos + 1
     token = torch.randn(a.batch, cfg.hidden, device="cuda").to(dtype)
-    stream = torch.cuda.Stream()
-    with torch.cuda.stream(stream):
-        stack(token, table, one, pos, lens)      # workspaces are made outside the capture
+    stack(token, table, one, pos, lens)          # once outside the capture
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
