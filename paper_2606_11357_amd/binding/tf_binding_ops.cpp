@@ -333,8 +333,8 @@ PyObject* decode_common(PyObject* const* a, Py_ssize_t n) {
     if (q->scalar_type() != cache.type || q->get_device() != dev || D != cache.c.head_dim || q->stride(-1) != 1 ||
         (H > 1 && q->stride(-2) != D) || !is(lens, at::kInt, dev, one) || Q > TF_KV4_MAX_Q || H > TF_MAX_HEADS)
         return not_here();
-    if (many && B > 1 && q->stride(0) != Q * q->stride(1)) return not_here();
-    const int64_t stride = many ? (B * Q > 1 ? q->stride(1) : H * D) : B > 1 ? q->stride(0) : H * D;
+    if (Q > 1 && B > 1 && q->stride(0) != Q * q->stride(1)) return not_here();
+    const int64_t stride = Q > 1 ? q->stride(1) : B > 1 ? q->stride(0) : H * D;
     float scale = 1.0f / std::sqrt((float)D);
     if (a[4] != Py_None && !as_float(a[4], scale)) return not_here();
     const at::Tensor* out = nullptr;

@@ -671,9 +671,14 @@ def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
     B, q_len = q.shape[0], 1 if q.dim() == 3 else q.shape[1]
     q_heads, D = q.shape[-2:]
     _same(q, cache.dtype, dev, (*q.shape[:-1], cache.head_dim), "q")
-    if q.dim() == 4 and B > 1 and q.stride(0) != q_len * q.stride(1):
+    if q_len > 1 and B > 1 and q.stride(0) != q_len * q.stride(1):
         raise ValueError("the tokens of q must be equally spaced")
-    rows = q if q.dim() == 3 else q.as_strided((B * q_len, q_heads, D), q.stride()[1:])
+    if q.dim() == 3:
+        rows = q
+    elif q_len == 1:
+        rows = q[:, 0]
+    else:
+        rows = q.as_strided((B * q_len, q_heads, D), q.stride()[1:])
     stride = _heads_of(rows, "q")
     _int32(lens, (B,), dev, "lens")
     st = cache._with(table, B)

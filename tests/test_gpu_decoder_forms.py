@@ -1,0 +1,30 @@
+"""Forms of the attention calls' arguments, on the native and the general path."""
+from __future__ import annotations
+
+import pytest
+
+from test_gpu_decoder_ops import filled, i32, tf  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(params=["native", "general"])
+def path(request, tf, monkeypatch):
+    if request.param == "general":
+        monkeypatch.setattr(tf, "_ops", dict.fromkeys(("norm", "append", "read", "decode", "prompt"),
+                                                      lambda *call: NotImplemented))
+
+
+@pytest.mark.parametrize("lens", [[70, 33, 5], [40]], ids=str)
+def test_decode_of_one_token_with_an_axis_of_its_own(tf, path, lens):
+    """[batch, 1, heads, D] of a wider projection, whose token axis may have any
+    stride."""
+    B = len(lens)
+    cache, table, *_ = filled(tf, "bf16", (8, 2, 128), lens, 32, 3)
+    wide = torch.randn(B, 12, 128, device="cuda").bfloat16()
+    q = wide[:, :8]
+    want = tf.kv4_attention(q.contiguous(), cache, table, i32(lens))
+    for form in (q.unsqueeze(1), wide[:, None][:, :, :8], q.as_strided((B, 1, 8, 128), (12 * 128, 8, 128, 1))):
+        got = tf.kv4_attention(form, cache, table, i32(lens))
+        assert got.shape == (B, 1, 8, 128) and torch.equal(got[:, 0], want)
