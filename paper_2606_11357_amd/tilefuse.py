@@ -715,7 +715,8 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None
     current stream (under torch.cuda.graph one of the graph's), False for none
     (keys are then never split over workgroups), or bytes
     (prompt_attention_workspace_bytes) of the caller's, which calls that may run
-    concurrently must not share.  Returns [tokens, q_heads, head_dim]."""
+    concurrently must not share.  Returns [tokens, q_heads, head_dim]: zeros for a
+    query that sees no key; rows that no sequence owns are not written."""
     got = _call("prompt", "tf_prompt_attention", q, k, v, cu_q, cu_k, scale, causal, out, workspace)
     if got is not NotImplemented:
         return got
@@ -735,8 +736,9 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None
     else:
         _need_cuda(out)
         _same(out, q.dtype, q.device, (T, q_heads, D), "out")
-    if T > 0 and Tk == 0:
-        return out.zero_()
+    if T > 0 and Tk == 0:                # one key that no sequence owns, for the call's checks and rows
+        k = v = torch.zeros((1, kv_heads, D), dtype=q.dtype, device=q.device)
+        Tk, strides[1:] = 1, [kv_heads * D] * 2
     if T > 0:
         if workspace is None:
             need = prompt_attention_workspace_bytes(B, T, Tk, q_heads, kv_heads, D)

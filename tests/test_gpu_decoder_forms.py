@@ -28,3 +28,15 @@ def test_decode_of_one_token_with_an_axis_of_its_own(tf, path, lens):
     for form in (q.unsqueeze(1), wide[:, None][:, :, :8], q.as_strided((B, 1, 8, 128), (12 * 128, 8, 128, 1))):
         got = tf.kv4_attention(form, cache, table, i32(lens))
         assert got.shape == (B, 1, 8, 128) and torch.equal(got[:, 0], want)
+
+
+def test_prompt_without_keys(tf, path):
+    """Zeros in the rows that a sequence owns, the others as they were; the refusals of
+    any other call."""
+    q, none = torch.randn(7, 4, 64, device="cuda").half(), torch.empty(0, 2, 64, device="cuda").half()
+    out = torch.full_like(q, 3.0)
+    assert tf.prompt_attention(q, none, none, i32([0, 2, 5]), i32([0, 0, 0]), out=out) is out
+    assert (out[:5] == 0).all() and (out[5:] == 3).all()
+    with pytest.raises(tf.TileFuseError) as e:
+        tf.prompt_attention(q, none, none, i32([0, 2, 5]), i32([0, 0, 0]), scale=-1.0)
+    assert e.value.status == tf.TF_ERR_ARG
