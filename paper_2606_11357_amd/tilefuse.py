@@ -691,6 +691,8 @@ def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
         return out
     if workspace is None:
         workspace = _cached_workspace(_attention_ws, dev, kv4_attention_workspace_bytes(B, q_len, q_heads, cache.kv_heads, D))
+    elif workspace is False:
+        raise ValueError("decode attention needs a workspace")
     else:
         _need_cuda(workspace)
     _check(load().tf_kv4_attention(st, _ptr(q), stride, _ptr(lens), B, q_len, q_heads, D ** -0.5 if scale is None else scale, _ptr(out),

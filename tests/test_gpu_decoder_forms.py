@@ -40,3 +40,9 @@ def test_prompt_without_keys(tf, path):
     with pytest.raises(tf.TileFuseError) as e:
         tf.prompt_attention(q, none, none, i32([0, 2, 5]), i32([0, 0, 0]), scale=-1.0)
     assert e.value.status == tf.TF_ERR_ARG
+
+
+def test_decode_without_a_workspace_is_refused(tf, path):
+    cache, table, *_ = filled(tf, "f16", (4, 2, 64), [40], 32, 1)
+    with pytest.raises(ValueError, match="workspace"):
+        tf.kv4_attention(torch.zeros(1, 4, 64, device="cuda").half(), cache, table, i32([40]), workspace=False)
