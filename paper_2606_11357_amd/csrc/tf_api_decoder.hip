@@ -41,6 +41,9 @@ int check_cache_shape(int64_t pages, int page_size, int kv_heads, int head_dim) 
     if (bad_head_dim(head_dim) || bad_heads(kv_heads)) return TF_ERR_SHAPE;
     if (page_size <= 0 || page_size % tf::kKvTile != 0 || page_size > TF_MAX_DIM) return TF_ERR_SHAPE;
     if (pages < 1 || pages > INT32_MAX) return TF_ERR_SHAPE;
+    // offsets are 64-bit
+    const int64_t page = (int64_t)kv_heads * (page_size / tf::kKvTile) * tf::kv4_tile_bytes(head_dim);
+    if (pages > INT64_MAX / page) return TF_ERR_SHAPE;
     return TF_OK;
 }
 
