@@ -4,8 +4,11 @@
 // HBM-bound: x and residual are read once, r and out written once (8 bytes an
 // element), the row staying in registers between its sums and its outputs.
 // Sums are fp32; each output is rounded once, and the norm takes r before that
-// rounding.  Measured: 8192 rows of 4096 48.4 us, 5.5 TB/s (a large copy: 5.25);
-// one row of 4096 2.9 us in the kernel, the latency of its loads and two sums.
+// rounding.  Outputs go past the L2: rows of 4096, inputs changing from call to call,
+// us through and past it: 512 5.8 / 5.1, 1024 8.5 / 6.7, 2048 13.9 / 11.1, 4096 26.9 /
+// 25.6, 8192 48.8 / 48.2 (5.6 TB/s; a copy of 1 GiB 5.15), 32768 184 / 181; a layer's
+// step takes the same time either way.  One row of 4096 takes 2.9 us in the kernel,
+// the latency of its loads and two sums.
 #include "tf_internal.h"
 
 namespace tf {
@@ -19,13 +22,7 @@ struct NormArgs {
     int64_t gate_stride, M;
     int N;
     float scale, offset, eps;
-    bool past;                        // outputs past the L2
 };
-
-// Elements of an output up to which it is stored past the L2.  Measured, rows of
-// 4096, us through and past it: 512 5.8 / 4.7, 1024 9.2 / 7.5, 2048 12.6 / 11.8,
-// 4096 22.5 / 21.6, 8192 44.1 / 47.9.
-constexpr int64_t kMostPast = 1 << 24;
 
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
@@ -103,7 +100,7 @@ __global__ __launch_bounds__(WR == 1 ? 256 : 64 * WR) void add_rms_norm_kernel(N
             u16x8 o;
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = round_out<BF>(r[i][j]);
-            store_past_if(a.past, reinterpret_cast<u16x8*>(a.r_out + row * a.N + c), o);
+            store_past(reinterpret_cast<u16x8*>(a.r_out + row * a.N + c), o);
         }
     }
     if (!a.y) return;
@@ -116,7 +113,7 @@ __global__ __launch_bounds__(WR == 1 ? 256 : 64 * WR) void add_rms_norm_kernel(N
         u16x8 o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = round_out<BF>(r[i][j] * norm * (scale_f32<BF>(wv[j]) + a.offset));
-        store_past_if(a.past, reinterpret_cast<u16x8*>(a.y + row * a.N + c), o);
+        store_past(reinterpret_cast<u16x8*>(a.y + row * a.N + c), o);
     }
 }
 
@@ -140,7 +137,7 @@ int launch_add_rms_norm(bool bf, const void* x, const void* residual, const void
                         int64_t N, void* r_out, void* y, hipStream_t s) {
     auto in = [](const void* p) { return static_cast<const uint16_t*>(p); };
     const NormArgs a{in(x), in(residual), in(post), in(gate), in(weight), static_cast<uint16_t*>(r_out),
-                     static_cast<uint16_t*>(y), gate_stride, M, (int)N, scale, offset, eps, M * N <= kMostPast};
+                     static_cast<uint16_t*>(y), gate_stride, M, (int)N, scale, offset, eps};
     return bf ? launch_dt<true>(a, s) : launch_dt<false>(a, s);
 }
 
