@@ -21,7 +21,9 @@
  * Conventions for every entry point:
  *  - All array pointers are DEVICE pointers (hipMalloc / torch CUDA tensors).
  *  - fp16 values travel as uint16_t bit patterns.
- *  - `stream` is a hipStream_t passed as void*; NULL means the null stream.
+ *  - `stream` is a hipStream_t passed as void*; NULL means the null stream.  The
+ *    current device of the calling thread has to be that of the stream and the
+ *    arrays (the Python binding sees to it).
  *    Calls only enqueue work on `stream` and return; the caller synchronizes.
  *  - The caller allocates and frees every buffer; the library keeps no device
  *    memory.  Its only global state is a per-device cache of the compute-unit

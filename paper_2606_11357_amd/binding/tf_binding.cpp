@@ -18,7 +18,7 @@
 
 #include <cstdint>
 
-#include "tf_workspace.h"
+#include "tf_binding_shared.h"
 
 namespace {
 
@@ -69,13 +69,6 @@ const at::Tensor* plain(PyObject* o) {
     return t.is_cuda() && t.layout() == at::kStrided && t.is_contiguous() ? &t : nullptr;
 }
 
-bool stream_of(int dev, void*& stream) {
-    const Held index{PyLong_FromLong(dev)};
-    const Held handle{index.o ? PyObject_CallOneArg(g_stream, index.o) : nullptr};
-    if (!handle.o) return false;
-    stream = PyLong_AsVoidPtr(handle.o);
-    return true;
-}
 
 PyObject* matmul_common(PyObject* const* a, Py_ssize_t n) {
     if (n != 9 || !g_bytes) return not_here();
@@ -106,7 +99,7 @@ PyObject* matmul_common(PyObject* const* a, Py_ssize_t n) {
         const int64_t need = g_bytes((int)bits, M, K, N, (int)group);
         if (need < 0) return not_here();
         if (need > 0) {
-            if (!stream_of(dev, stream)) return nullptr;
+            if (!tf_binding::stream_of(g_stream, dev, stream)) return PyErr_Occurred() ? nullptr : not_here();
             if (!tf_binding::find_workspace(g_workspaces, g_capture, dev, stream, held))
                 return PyErr_Occurred() ? nullptr : not_here();
             const at::Tensor* t = held.o ? plain(held.o) : nullptr;
@@ -138,7 +131,7 @@ PyObject* matmul_common(PyObject* const* a, Py_ssize_t n) {
             out->size(1) != N)
             return not_here();
     }
-    if (!held.o && !stream_of(dev, stream)) return nullptr;
+    if (!held.o && !tf_binding::stream_of(g_stream, dev, stream)) return PyErr_Occurred() ? nullptr : not_here();
     const MatmulFn fn = g_fn[(bits == 8 ? 4 : 0) + (gemv ? 2 : 0) + (bf ? 1 : 0)];
     const uint16_t* x = static_cast<const uint16_t*>(A->data_ptr());
     const void* pk = packed->data_ptr();

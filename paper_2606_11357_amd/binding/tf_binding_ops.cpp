@@ -13,7 +13,7 @@
 #include <cmath>
 #include <cstdint>
 
-#include "tf_workspace.h"
+#include "tf_binding_shared.h"
 #include "tilefuse.h"
 
 namespace {
@@ -95,13 +95,6 @@ bool as_float(PyObject* o, float& v) {
     else return false;
     if (PyErr_Occurred()) { PyErr_Clear(); return false; }
     return true;
-}
-bool stream_of(int dev, void*& stream) {
-    const Held index{PyLong_FromLong(dev)};
-    const Held handle{index.o ? PyObject_CallOneArg(g_ops_stream, index.o) : nullptr};
-    if (!handle.o) return false;
-    stream = PyLong_AsVoidPtr(handle.o);
-    return !PyErr_Occurred();
 }
 const void* ptr(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
 const int32_t* ints(const at::Tensor* t) { return static_cast<const int32_t*>(t->data_ptr()); }
@@ -198,7 +191,7 @@ PyObject* norm_common(PyObject* const* a, Py_ssize_t n) {
     }
     const bool keep = !in[0] && !in[2] && !gate && scale == 1.0f && !in[4];
     void* stream;
-    if (!stream_of(dev, stream)) return nullptr;
+    if (!tf_binding::stream_of(g_ops_stream, dev, stream)) return PyErr_Occurred() ? nullptr : not_here();
     at::Tensor y, r;
     if (!in[3]) y = at::empty({M, N}, x->options().requires_grad(false));
     if (!in[4] && !keep) r = at::empty({M, N}, x->options().requires_grad(false));
@@ -261,7 +254,7 @@ PyObject* append_common(PyObject* const* a, Py_ssize_t n) {
     const int keys = a[9] == Py_True ? 1 : a[9] == Py_False ? 0 : -1;
     if (keys < 0) return not_here();
     void* stream;
-    if (!stream_of(dev, stream)) return nullptr;
+    if (!tf_binding::stream_of(g_ops_stream, dev, stream)) return PyErr_Occurred() ? nullptr : not_here();
     at::Tensor made_q, made_k;
     if (q && !q_out) {
         made_q = at::empty(qs, k->options().requires_grad(false));
@@ -303,7 +296,7 @@ PyObject* read_common(PyObject* const* a, Py_ssize_t n) {
     for (int i = 0; i < 2; ++i)
         if (a[5 + i] != Py_None && !is(out[i] = plain(a[5 + i]), cache.type, dev, kv)) return not_here();
     void* stream;
-    if (!stream_of(dev, stream)) return nullptr;
+    if (!tf_binding::stream_of(g_ops_stream, dev, stream)) return PyErr_Occurred() ? nullptr : not_here();
     at::Tensor made[2];
     for (int i = 0; i < 2; ++i)
         if (!out[i])
@@ -345,7 +338,7 @@ PyObject* decode_common(PyObject* const* a, Py_ssize_t n) {
     void *ws, *stream;
     size_t ws_bytes;
     if (a[6] == Py_False) return not_here();
-    if (!stream_of(dev, stream)) return nullptr;
+    if (!tf_binding::stream_of(g_ops_stream, dev, stream)) return PyErr_Occurred() ? nullptr : not_here();
     if (!workspace_of(a[6], g_decode_ws, a[0], dev, stream, need, held, ws, ws_bytes))
         return PyErr_Occurred() ? nullptr : not_here();
     at::Tensor made;
@@ -388,7 +381,7 @@ PyObject* prompt_common(PyObject* const* a, Py_ssize_t n) {
     Held held;
     void *ws, *stream;
     size_t ws_bytes;
-    if (!stream_of(dev, stream)) return nullptr;
+    if (!tf_binding::stream_of(g_ops_stream, dev, stream)) return PyErr_Occurred() ? nullptr : not_here();
     if (!workspace_of(a[8], g_prompt_ws, a[0], dev, stream, need, held, ws, ws_bytes))
         return PyErr_Occurred() ? nullptr : not_here();
     at::Tensor made;

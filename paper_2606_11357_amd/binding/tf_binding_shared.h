@@ -1,8 +1,10 @@
-// What the native parts of the binding share: the look-up of a cached workspace
-// (tilefuse.py makes them and says how they are kept).
+// What the native parts of the binding share: the current stream of a device, and
+// the look-up of a cached workspace (tilefuse.py makes them and says how they are
+// kept).
 #pragma once
 
 #include <Python.h>
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 
 #include <cstdint>
 
@@ -13,6 +15,18 @@ struct Held {
     PyObject* o = nullptr;
     ~Held() { Py_XDECREF(o); }
 };
+
+// The current stream of the tensors' device, from `current` (device index -> handle).
+// False: a Python error, or not the current device, to which a launch would go
+// whatever its stream is (the general path makes it current).
+inline bool stream_of(PyObject* current, int dev, void*& stream) {
+    if (c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index() != dev) return false;
+    const Held index{PyLong_FromLong(dev)};
+    const Held handle{index.o ? PyObject_CallOneArg(current, index.o) : nullptr};
+    if (!handle.o) return false;
+    stream = PyLong_AsVoidPtr(handle.o);
+    return !PyErr_Occurred();
+}
 
 // The runtime's query of a stream's capture: its state (0: none) and its number.
 using CaptureFn = int (*)(void* stream, int* state, unsigned long long* number);

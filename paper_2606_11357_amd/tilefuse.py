@@ -123,9 +123,14 @@ def _torch():
     return torch
 
 
-def _stream(device):
+def _launch(name, device, *args):
+    """One call of the library on the device's current stream, with the device current
+    (a launch goes to the current one, whatever its stream is)."""
     torch = _torch()
-    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    if device.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
+            return _launch(name, device, *args)
+    _check(getattr(load(), name)(*args, ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(device.index))), name)
 
 
 def _ptr(t):
@@ -224,8 +229,7 @@ def pack_w4(qweight, qzeros, scales, K: int, N: int, group: int = 128, out=None)
     _need_cuda(qweight, qzeros, scales)
     if out is None:
         out = torch.empty(packed_bytes(4, K, N, group), dtype=torch.uint8, device=qweight.device)
-    _check(load().tf_pack_w4(_ptr(qweight), _ptr(qzeros), _ptr(scales), K, N, group, _ptr(out),
-                             _stream(qweight.device)), "tf_pack_w4")
+    _launch("tf_pack_w4", qweight.device, _ptr(qweight), _ptr(qzeros), _ptr(scales), K, N, group, _ptr(out))
     return out
 
 
@@ -235,8 +239,7 @@ def pack_w8(qweight, zeros, scales, K: int, N: int, group: int = 128, out=None):
     _need_cuda(qweight, zeros, scales)
     if out is None:
         out = torch.empty(packed_bytes(8, K, N, group), dtype=torch.uint8, device=qweight.device)
-    _check(load().tf_pack_w8(_ptr(qweight), _ptr(zeros), _ptr(scales), K, N, group, _ptr(out),
-                             _stream(qweight.device)), "tf_pack_w8")
+    _launch("tf_pack_w8", qweight.device, _ptr(qweight), _ptr(zeros), _ptr(scales), K, N, group, _ptr(out))
     return out
 
 
@@ -247,8 +250,7 @@ def pack_w8_sym(qweight, scales, K: int, N: int, group: int = 128, out=None):
     _need_cuda(qweight, scales)
     if out is None:
         out = torch.empty(packed_bytes(8, K, N, group), dtype=torch.uint8, device=qweight.device)
-    _check(load().tf_pack_w8_sym(_ptr(qweight), _ptr(scales), K, N, group, _ptr(out),
-                                 _stream(qweight.device)), "tf_pack_w8_sym")
+    _launch("tf_pack_w8_sym", qweight.device, _ptr(qweight), _ptr(scales), K, N, group, _ptr(out))
     return out
 
 
@@ -316,9 +318,7 @@ def _matmul_general(bits, kind, A, packed, K, N, group, out, workspace):
         _need_cuda(workspace)
         ws_ptr, ws_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
     name = f"tf_w{bits}a16_{kind}" + ("_bf16" if A.dtype == torch.bfloat16 else "")
-    rc = getattr(load(), name)(_ptr(A), _ptr(packed), _ptr(out), M, K, N, group, ws_ptr, ws_bytes,
-                               _stream(A.device))
-    _check(rc, name)
+    _launch(name, A.device, _ptr(A), _ptr(packed), _ptr(out), M, K, N, group, ws_ptr, ws_bytes)
     return out
 
 
@@ -350,8 +350,7 @@ def w4a16_gemv_noalloc(A, packed, K: int, N: int, group: int = 128, out=None):
         out = torch.empty((M, N), dtype=A.dtype, device=A.device)
     elif out.dtype != A.dtype or tuple(out.shape) != (M, N):
         raise ValueError("out must have A's dtype and shape [M, N]")
-    _check(load().tf_w4a16_gemv_noalloc(_ptr(A), _ptr(packed), _ptr(out), M, K, N, group, _stream(A.device)),
-           "tf_w4a16_gemv_noalloc")
+    _launch("tf_w4a16_gemv_noalloc", A.device, _ptr(A), _ptr(packed), _ptr(out), M, K, N, group)
     return out
 
 
@@ -361,8 +360,7 @@ def unpack(bits: int, packed, K: int, N: int, group: int = 128):
     _need_cuda(packed)
     q = torch.empty((K, N), dtype=torch.uint8, device=packed.device)
     z = torch.empty((K // group, N), dtype=torch.uint8, device=packed.device)
-    _check(load().tf_unpack(bits, _ptr(packed), K, N, group, _ptr(q), _ptr(z),
-                            _stream(packed.device)), "tf_unpack")
+    _launch("tf_unpack", packed.device, bits, _ptr(packed), K, N, group, _ptr(q), _ptr(z))
     return q, z
 
 
@@ -374,8 +372,7 @@ def dequant(bits: int, packed, K: int, N: int, group: int = 128, dtype=None):
     _need_cuda(packed)
     code = {torch.float16: TF_F16, torch.float32: TF_F32, torch.bfloat16: TF_BF16}[dtype]
     w = torch.empty((K, N), dtype=dtype, device=packed.device)
-    _check(load().tf_dequant(bits, _ptr(packed), K, N, group, code, _ptr(w),
-                             _stream(packed.device)), "tf_dequant")
+    _launch("tf_dequant", packed.device, bits, _ptr(packed), K, N, group, code, _ptr(w))
     return w
 
 
@@ -392,7 +389,7 @@ def silu_mul(gu, out=None):
     elif out.dtype != gu.dtype:
         raise ValueError("out must have gu's dtype")
     name = "tf_silu_mul_bf16" if gu.dtype == torch.bfloat16 else "tf_silu_mul"
-    _check(getattr(load(), name)(_ptr(gu), M, N, _ptr(out), _stream(gu.device)), name)
+    _launch(name, gu.device, _ptr(gu), M, N, _ptr(out))
     return out
 
 
@@ -513,9 +510,8 @@ def add_rms_norm(x, residual=None, weight=None, *, post_weight=None, gate=None, 
     if residual_out is None and not keep:
         residual_out = torch.empty_like(x)
     if M > 0:
-        _check(load().tf_add_rms_norm(code, _ptr(x), _ptr(residual), _ptr(post_weight), _ptr(gate), gate_stride, scale,
-                                      _ptr(weight), offset, eps, M, N, _ptr(residual_out), _ptr(out),
-                                      _stream(x.device)), "tf_add_rms_norm")
+        _launch("tf_add_rms_norm", x.device, code, _ptr(x), _ptr(residual), _ptr(post_weight), _ptr(gate),
+                gate_stride, scale, _ptr(weight), offset, eps, M, N, _ptr(residual_out), _ptr(out))
     return out, x if keep else residual_out
 
 
@@ -605,9 +601,8 @@ def kv4_append(cache, table, cu, starts, k, v, cos=None, sin=None, q=None, keys=
         for t, what in ((cos, "cos"), (sin, "sin")):
             _same(t, torch.float32, dev, (positions, cache.head_dim // 2), what)
     if T > 0:
-        _check(load().tf_kv4_append(st, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(cos), _ptr(sin),
-                                    positions, _ptr(cu), _ptr(starts), B, T, q_heads, _ptr(q_out), _ptr(k_out),
-                                    _stream(dev)), "tf_kv4_append")
+        _launch("tf_kv4_append", dev, st, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(cos),
+                _ptr(sin), positions, _ptr(cu), _ptr(starts), B, T, q_heads, _ptr(q_out), _ptr(k_out))
     return q_out, k_out
 
 
@@ -630,8 +625,7 @@ def kv4_read(cache, table, cu, starts, tokens: int, k_out=None, v_out=None):
         _need_cuda(t)
         _same(t, cache.dtype, dev, shape, what)
     if tokens > 0:
-        _check(load().tf_kv4_read(st, _ptr(cu), _ptr(starts), B, tokens, _ptr(k_out), _ptr(v_out), _stream(dev)),
-               "tf_kv4_read")
+        _launch("tf_kv4_read", dev, st, _ptr(cu), _ptr(starts), B, tokens, _ptr(k_out), _ptr(v_out))
     return k_out, v_out
 
 
@@ -695,9 +689,9 @@ def kv4_attention(q, cache, table, lens, scale=None, out=None, workspace=None):
         raise ValueError("decode attention needs a workspace")
     else:
         _need_cuda(workspace)
-    _check(load().tf_kv4_attention(st, _ptr(q), stride, _ptr(lens), B, q_len, q_heads, D ** -0.5 if scale is None else scale, _ptr(out),
-                                   _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(dev)),
-           "tf_kv4_attention")
+    _launch("tf_kv4_attention", dev, st, _ptr(q), stride, _ptr(lens), B, q_len, q_heads,
+            D ** -0.5 if scale is None else scale, _ptr(out), _ptr(workspace),
+            workspace.numel() * workspace.element_size())
     return out
 
 
@@ -751,8 +745,7 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None
         else:
             _need_cuda(workspace)
             ws_bytes = workspace.numel() * workspace.element_size()
-        _check(load().tf_prompt_attention(code, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v), strides[2],
-                                          _ptr(cu_q), _ptr(cu_k), B, T, Tk, q_heads, kv_heads, D,
-                                          D ** -0.5 if scale is None else scale, int(causal), _ptr(out), _ptr(workspace), ws_bytes,
-                                          _stream(q.device)), "tf_prompt_attention")
+        _launch("tf_prompt_attention", q.device, code, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
+                strides[2], _ptr(cu_q), _ptr(cu_k), B, T, Tk, q_heads, kv_heads, D,
+                D ** -0.5 if scale is None else scale, int(causal), _ptr(out), _ptr(workspace), ws_bytes)
     return out
