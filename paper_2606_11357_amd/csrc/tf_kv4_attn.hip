@@ -15,7 +15,7 @@
 // and the softmax of 16 columns, of which q_len * group are real, but is not what
 // is waited for: a copy with half the softmax ran 2% faster, one with shares that
 // let all workgroups of a compute unit end together 1%.  Few tokens cost the chain
-// lengths - table - tiles - sums: one sequence of 513 keys 9.3 us.
+// lengths - table - tiles - sums: one sequence of 513 keys 8.9 us (fp16).
 #include "tf_kv4.h"
 
 namespace tf {

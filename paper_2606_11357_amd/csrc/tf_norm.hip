@@ -6,7 +6,7 @@
 // Sums are fp32; each output is rounded once, and the norm takes r before that
 // rounding.  Outputs go past the L2: rows of 4096, inputs changing from call to call,
 // us through and past it: 512 5.8 / 5.1, 1024 8.5 / 6.7, 2048 13.9 / 11.1, 4096 26.9 /
-// 25.6, 8192 48.8 / 48.2 (5.6 TB/s; a copy of 1 GiB 5.15), 32768 184 / 181; a layer's
+// 25.6, 8192 48.8 / 48.2 (5.6 TB/s; a copy of 1 GiB 5.1 to 5.2), 32768 184 / 181; a layer's
 // step takes the same time either way.  One row of 4096 takes 2.9 us in the kernel,
 // the latency of its loads and two sums.
 #include "tf_internal.h"

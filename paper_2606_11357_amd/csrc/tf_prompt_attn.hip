@@ -12,10 +12,11 @@
 // product takes from it.
 //
 // Four waves of 32 queries share each step's 64 keys and values in LDS: with 128
-// dims a wave reads 32 KB of them a step for 1024 cycles of matrix instructions.  Measured (bf16, one causal prompt of 8192): 32 heads on 8 of 128
-// 527 to 540 us, 1.02 to 1.04 PFLOP/s, matrix cores busy 57% of the time and vector units 49%, at
-// the clock that the card's power leaves; 16 heads of 64 165 us, 833 TFLOP/s; 8 of
-// 256 326 us, 843.
+// dims a wave reads 32 KB of them a step for 1024 cycles of matrix instructions.
+// Measured (bf16, one causal prompt of 8192): 32 heads on 8 of 128 519 to 543 us, from
+// card to card, 1.01 to 1.06 PFLOP/s, matrix cores busy 57% of the time and vector
+// units 49%, at the 1.83 GHz at which a large matrix product starts too; 16 heads of 64
+// 162 us, 848 TFLOP/s, vector units 70% busy; 8 of 256 325 us, 845, one wave a SIMD.
 #include "tf_internal.h"
 
 namespace tf {
