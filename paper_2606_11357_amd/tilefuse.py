@@ -418,6 +418,8 @@ def _heads_of(t, what):
     if t.dim() != 3:
         raise ValueError(f"{what} must be [tokens, heads, head_dim]")
     T, H, D = t.shape
+    if t.is_contiguous():                # (one without elements whatever its strides are)
+        return H * D
     if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
         raise ValueError(f"the heads of {what} must be contiguous")
     return t.stride(0) if T > 1 else H * D

@@ -46,3 +46,13 @@ def test_decode_without_a_workspace_is_refused(tf, path):
     cache, table, *_ = filled(tf, "f16", (4, 2, 64), [40], 32, 1)
     with pytest.raises(ValueError, match="workspace"):
         tf.kv4_attention(torch.zeros(1, 4, 64, device="cuda").half(), cache, table, i32([40]), workspace=False)
+
+
+def test_no_keys_of_any_stride(tf, path):
+    """A tensor without elements is contiguous whatever its strides are."""
+    q, none = torch.randn(3, 4, 64, device="cuda").half(), torch.empty_strided((0, 2, 64), (1, 1, 1), device="cuda").half()
+    none = none.as_strided((0, 2, 64), (7, 3, 5))
+    assert none.is_contiguous()
+    assert (tf.prompt_attention(q, none, none, i32([0, 3]), i32([0, 0])) == 0).all()
+    cache = tf.kv4_cache(1, 32, 2, 64)
+    assert tf.kv4_append(cache, i32([0]).view(1, 1), i32([0, 0]), i32([0]), none, none, keys=True)[1].shape == (0, 2, 64)
