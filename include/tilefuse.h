@@ -405,6 +405,100 @@ int tf_prompt_attention(int dtype, const void* Q, int64_t q_stride, const void* 
                         int64_t tokens_k, int q_heads, int kv_heads, int head_dim, float scale, int causal, void* O,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Linear layers whose activations are 8-bit integers too, and layers made of
+ * experts (not part of the paper's method).  A row of activations stands as codes
+ * q in -127..127 with a scale of its own, a weight's column as the signed INT8
+ * codes of tf_pack_w8_sym with a scale of its own, and the product is one of
+ * integers:
+ *   C[m, n] = s_a[m] * s_w[n] * sum_k qa[m, k] * qw[k, n].
+ * The sums are exact (int32); each output is rounded once.  `dtype` is TF_F16 or
+ * TF_BF16, the type of the 16-bit tensors of a call.
+ * ---------------------------------------------------------------------------
+ */
+
+/* Largest accepted numbers of experts, of choices a token, and of rows of an
+ * expert product (tokens times choices). */
+#define TF_MAX_EXPERTS 1024
+#define TF_MAX_TOP_K 32
+#define TF_MAX_SLOTS (TF_MAX_M * TF_MAX_TOP_K)
+
+/*
+ * Codes of the rows of X [M, N], or with `gated` of H[m, n] = silu(X[m, n]) *
+ * X[m, N + n], X being [M, 2 N] (H in fp32, not rounded between):
+ *   scales[m] = max|row| / 127,   codes[m, n] = round(row[n] * (127 / max|row|)).
+ * Rows of X are x_stride elements apart; codes [M, N] and scales fp32 [M] are
+ * contiguous.  A row whose values are all under 2^-100 has the scale 0 and codes
+ * 0, one with a value that is not finite the scale NaN and codes 0.  N % 16 == 0,
+ * x_stride % 8 == 0, 16-byte aligned X and codes.
+ */
+int tf_quantize_rows(int dtype, const void* X, int64_t x_stride, int64_t M, int64_t N, int gated, int8_t* codes,
+                     float* scales, void* stream);
+
+/*
+ * Pre-tiling of `experts` weights (1 for a dense layer): qweight int8
+ * [experts, K, N] in -128..127, scales [experts, N] of scale_dtype (TF_F16,
+ * TF_BF16 or TF_F32).  packed: experts * tf_w8a8_packed_bytes(K, N) bytes, 256-byte
+ * aligned, one expert after the other; it serves outputs of either type.
+ * K % 16 == 0, N % 8 == 0.  A weight whose signs and scales suit tf_pack_w8_sym
+ * suits this call as it is.
+ */
+int64_t tf_w8a8_packed_bytes(int64_t K, int64_t N);
+int tf_pack_w8a8(const int8_t* qweight, const void* scales, int scale_dtype, int64_t K, int64_t N, int64_t experts,
+                 void* packed, void* stream);
+
+/* C [M, N] = the product above of codes A [M, K], their scales and a packed weight. */
+int tf_w8a8_gemm(int dtype, const int8_t* A, const float* a_scales, const void* packed, void* C, int64_t M, int64_t K,
+                 int64_t N, void* stream);
+
+/*
+ * The choice of experts for each of T tokens and the order in which their
+ * products take the tokens.  From logits [T, experts] (TF_F16, TF_BF16 or TF_F32,
+ * rows `stride` elements apart), in fp64:
+ *   score  = softmax over the experts, or sigmoid (scoring 0 or 1),
+ *   choice = score + bias (fp32 [experts], or NULL);
+ * with groups > 1 (experts / groups neighbours each) only the experts of the
+ * top_groups best groups take part, a group's value being the largest choice in it
+ * or (group_score 1) the sum of its two largest; the top_k largest choices are the
+ * token's experts, in that order.  Of equal groups or choices the lower index goes
+ * first.  weights = score * scale, with `renormalize` divided by the sum of the
+ * token's chosen scores before (zeros where that is 0).  An expert whose logit is
+ * -infinity or NaN (or whose choice is NaN) comes after all others, with weight 0
+ * where it is chosen for want of them, and is left out of a group's sum; infinite logits share the
+ * softmax.  Outputs:
+ *   weights fp32 [T, top_k], chosen int32 [T, top_k],
+ *   offsets int32 [experts + 1]  expert e has the slots offsets[e] .. offsets[e+1] - 1,
+ *   tokens  int32 [T * top_k]    the token of each slot, ascending within an expert,
+ *   places  int32 [T, top_k]     the slot of each choice.
+ * groups <= 64 divides experts; top_k is at most what the top groups hold.
+ */
+int tf_route_experts(int dtype, const void* logits, int64_t stride, const float* bias, int64_t T, int experts,
+                     int top_k, int scoring, int groups, int top_groups, int group_score, int renormalize, float scale,
+                     float* weights, int32_t* chosen, int32_t* offsets, int32_t* tokens, int32_t* places,
+                     void* stream);
+
+/*
+ * The experts' products: row i of C [slots, N], offsets[e] <= i < offsets[e + 1], is
+ * row rows[i] (rows NULL: i) of the codes A [a_rows, K] times weight e of `packed`.
+ * offsets int32 [experts + 1] and rows int32 [slots] stay on the device; an offset
+ * outside 0..slots counts as the nearer end, one below an earlier one as that.  Rows of C that no expert has are not
+ * written; one whose row of A is outside 0..a_rows - 1 is zeros.  With rows, A
+ * holds less than 2^32 - 256 bytes.
+ */
+int tf_w8a8_expert_gemm(int dtype, const int8_t* A, const float* a_scales, int64_t a_rows, const void* packed,
+                        const int32_t* offsets, const int32_t* rows, void* C, int64_t slots, int64_t K, int64_t N,
+                        int64_t experts, void* stream);
+
+/*
+ * out[t] = add[t] + sum_j weights[t, j] * Y[places[t, j]] in fp32, rounded once:
+ * Y [slots, N] contiguous, weights fp32 and places int32 [T, top_k], add [T, N] or
+ * NULL.  A choice of weight 0, or whose place is outside 0..slots - 1, adds nothing,
+ * whatever is in Y.  out may be add itself.  N % 8 == 0.
+ */
+int tf_combine_experts(int dtype, const void* Y, int64_t slots, const float* weights, const int32_t* places,
+                       const void* add, int64_t T, int top_k, int64_t N, void* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

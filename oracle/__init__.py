@@ -33,3 +33,12 @@ from .decoder_oracle import (  # noqa: F401
     rotate,
     round16,
 )
+from .experts_oracle import (  # noqa: F401
+    combine,
+    expert_order,
+    expert_products,
+    gated_rows,
+    route,
+    row_codes,
+    w8a8,
+)

@@ -8,6 +8,7 @@ the matmul calls only saves host time; without it they run through ctypes.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 import warnings
@@ -36,7 +37,8 @@ EXPORTS = (
     "tf_w8a16_gemv_bf16", "tf_unpack", "tf_dequant", "tf_silu_mul", "tf_silu_mul_bf16",
     "tf_add_rms_norm", "tf_kv4_cache_bytes", "tf_kv4_append", "tf_kv4_read",
     "tf_kv4_attention_workspace_bytes", "tf_kv4_attention", "tf_prompt_attention_workspace_bytes",
-    "tf_prompt_attention",
+    "tf_prompt_attention", "tf_quantize_rows", "tf_w8a8_packed_bytes", "tf_pack_w8a8", "tf_w8a8_gemm",
+    "tf_route_experts", "tf_w8a8_expert_gemm", "tf_combine_experts",
 )
 
 
@@ -97,6 +99,13 @@ def load() -> ctypes.CDLL:
         "tf_kv4_attention": (I, [C, P, I64, P, I64, I, I, F, P, P, SZ, P]),
         "tf_prompt_attention": (I, [I, P, I64, P, I64, P, I64, P, P, I64, I64, I64, I, I, I, F, I, P, P, SZ, P]),
         "tf_prompt_attention_workspace_bytes": (I64, [I64, I64, I64, I, I, I]),
+        "tf_quantize_rows": (I, [I, P, I64, I64, I64, I, P, P, P]),
+        "tf_w8a8_packed_bytes": (I64, [I64, I64]),
+        "tf_pack_w8a8": (I, [P, P, I, I64, I64, I64, P, P]),
+        "tf_w8a8_gemm": (I, [I, P, P, P, P, I64, I64, I64, P]),
+        "tf_route_experts": (I, [I, P, I64, P, I64, I, I, I, I, I, I, I, F, P, P, P, P, P, P]),
+        "tf_w8a8_expert_gemm": (I, [I, P, P, I64, P, P, P, P, I64, I64, I64, I64, P]),
+        "tf_combine_experts": (I, [I, P, I64, P, P, P, I64, I, I64, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -750,4 +759,189 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None
         _launch("tf_prompt_attention", q.device, code, _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
                 strides[2], _ptr(cu_q), _ptr(cu_k), B, T, Tk, q_heads, kv_heads, D,
                 D ** -0.5 if scale is None else scale, int(causal), _ptr(out), _ptr(workspace), ws_bytes)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# 8-bit activations, and layers made of experts
+# ---------------------------------------------------------------------------
+def quantize_rows(x, gated=False, codes=None, scales=None):
+    """Codes (int8 [M, N]) and scales (fp32 [M]) of the rows of a fp16 or bf16 [M, N]
+    matrix: scale = max|row| / 127, codes = round(row * 127 / max|row|).  gated: x
+    is [M, 2N] and the rows are silu(x[:, :N]) * x[:, N:].  Rows may be strided (by a
+    multiple of 8 elements).  A row with a value that is not finite has the scale NaN."""
+    torch = _torch()
+    if not x.is_cuda:
+        raise ValueError("tensors must be on the GPU (the library has no CPU path)")
+    code = _dtype_code(x.dtype, "x")
+    if x.dim() != 2 or (gated and x.shape[1] % 2 != 0):
+        raise ValueError("x must be fp16 or bf16 [M, N], gated [M, 2N]")
+    M, N = x.shape[0], x.shape[1] // (2 if gated else 1)
+    if x.shape[1] > 1 and x.stride(1) != 1 and not x.is_contiguous():
+        raise ValueError("the rows of x must be contiguous")
+    codes = torch.empty((M, N), dtype=torch.int8, device=x.device) if codes is None else codes
+    scales = torch.empty((M,), dtype=torch.float32, device=x.device) if scales is None else scales
+    _need_cuda(codes, scales)
+    _same(codes, torch.int8, x.device, (M, N), "codes")
+    _same(scales, torch.float32, x.device, (M,), "scales")
+    if M > 0:
+        _launch("tf_quantize_rows", x.device, code, _ptr(x), x.stride(0) if M > 1 else x.shape[1], M, N, int(gated),
+                _ptr(codes), _ptr(scales))
+    return codes, scales
+
+
+def w8a8_packed_bytes(K: int, N: int) -> int:
+    """Bytes of one packed weight (of each expert's)."""
+    n = load().tf_w8a8_packed_bytes(K, N)
+    if n < 0:
+        raise TileFuseError(int(n), "tf_w8a8_packed_bytes")
+    return int(n)
+
+
+def pack_w8a8(qweight, scales, out=None):
+    """Pre-tile signed INT8 weights for w8a8_gemm (int8 [K, N], scales fp16, bf16 or
+    fp32 [N]) or for w8a8_expert_gemm (int8 [experts, K, N], scales [experts, N])."""
+    torch = _torch()
+    _need_cuda(qweight, scales, out)
+    if qweight.dtype != torch.int8 or qweight.dim() not in (2, 3):
+        raise ValueError("qweight must be int8 [K, N] or [experts, K, N]")
+    if scales.dtype not in (torch.float16, torch.bfloat16, torch.float32):
+        raise ValueError("scales must be fp16, bf16 or fp32")
+    _same(scales, scales.dtype, qweight.device, (*qweight.shape[:-2], qweight.shape[-1]), "scales")
+    (K, N), E = qweight.shape[-2:], qweight.shape[0] if qweight.dim() == 3 else 1
+    need = E * w8a8_packed_bytes(K, N)
+    if out is None:
+        out = torch.empty(need, dtype=torch.uint8, device=qweight.device)
+    elif out.device != qweight.device or out.nbytes < need:
+        raise ValueError(f"out must hold {need} bytes on {qweight.device}")
+    code = TF_F32 if scales.dtype == torch.float32 else _dtype_code(scales.dtype, "scales")
+    _launch("tf_pack_w8a8", qweight.device, _ptr(qweight), _ptr(scales), code, K, N, E, _ptr(out))
+    return out
+
+
+def _codes_of(a, scales, packed, K, N, weights, dtype):
+    """Checks the operands of an 8-bit matmul; the output's type and its code."""
+    torch = _torch()
+    _need_cuda(a, scales, packed)
+    if a.dtype != torch.int8 or a.dim() != 2 or a.shape[1] != K:
+        raise ValueError("the codes must be int8 [M, K]")
+    _same(scales, torch.float32, a.device, (a.shape[0],), "scales")
+    if packed.device != a.device or packed.nbytes < weights * w8a8_packed_bytes(K, N):
+        raise ValueError("packed must be what pack_w8a8 made for this K and N, on the codes' GPU")
+    dtype = dtype or torch.float16
+    return dtype, _dtype_code(dtype, "dtype")
+
+
+def _product_out(out, dtype, device, shape):
+    if out is None:
+        return _torch().empty(shape, dtype=dtype, device=device)
+    _need_cuda(out)
+    _same(out, dtype, device, shape, "out")
+    return out
+
+
+def w8a8_gemm(codes, scales, packed, K: int, N: int, dtype=None, out=None):
+    """The product of int8 codes [M, K] with a scale a row (quantize_rows) and a packed
+    weight (pack_w8a8): [M, N] of dtype (fp16 unless given, or bf16).  Sums are exact."""
+    dtype, code = _codes_of(codes, scales, packed, K, N, 1, dtype if out is None else dtype or out.dtype)
+    M = codes.shape[0]
+    out = _product_out(out, dtype, codes.device, (M, N))
+    if M > 0:
+        _launch("tf_w8a8_gemm", codes.device, code, _ptr(codes), _ptr(scales), _ptr(packed), _ptr(out), M, K, N)
+    return out
+
+
+Routing = collections.namedtuple("Routing", "weights experts offsets tokens places")
+Routing.__doc__ = """What route_experts gives: weights fp32 and experts int32 [T, top_k]; offsets int32
+[experts + 1] of the experts' slots; tokens int32 [T * top_k], the token of each slot; places int32
+[T, top_k], the slot of each choice."""
+
+
+def route_experts(logits, top_k: int, *, bias=None, scoring="softmax", groups=1, top_groups=None, group_score="top2",
+                  renormalize=False, scale=1.0):
+    """Chooses top_k of the experts for each token of logits [T, experts] (fp16, bf16
+    or fp32) and orders the choices by expert.
+
+    score = softmax or sigmoid of the logits; the choice is by score + bias (fp32
+    [experts]), within the top_groups best of `groups` neighbouring groups where
+    given, a group's value being the sum of its two largest choices ("top2") or the
+    largest ("max"); ties go to the lower index.  weights = score, divided by the sum
+    of the chosen ones with renormalize, times scale.  An expert whose logit is
+    -infinity or NaN comes last, with weight 0.  Returns a Routing."""
+    torch = _torch()
+    if not logits.is_cuda:
+        raise ValueError("tensors must be on the GPU (the library has no CPU path)")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T, experts]")
+    dev = logits.device
+    code = TF_F32 if logits.dtype == torch.float32 else _dtype_code(logits.dtype, "logits of other types than fp32")
+    T, E = logits.shape
+    if E > 1 and logits.stride(1) != 1 and not logits.is_contiguous():
+        raise ValueError("the rows of logits must be contiguous")
+    if bias is not None:
+        _need_cuda(bias)
+        _same(bias, torch.float32, dev, (E,), "bias")
+    if scoring not in ("softmax", "sigmoid"):
+        raise ValueError("scoring must be softmax or sigmoid")
+    if group_score not in ("top2", "max"):
+        raise ValueError("group_score must be top2 or max")
+    make = lambda n, dt=torch.int32: torch.empty(n, dtype=dt, device=dev)  # noqa: E731
+    r = Routing(make((T, top_k), torch.float32), make((T, top_k)), make(E + 1), make(T * top_k), make((T, top_k)))
+    if T == 0:
+        r.offsets.zero_()
+        return r
+    _launch("tf_route_experts", dev, code, _ptr(logits), logits.stride(0) if T > 1 else E, _ptr(bias), T, E, top_k,
+            int(scoring == "sigmoid"), groups, groups if top_groups is None else top_groups,
+            int(group_score == "top2"), int(renormalize), scale, *(_ptr(t) for t in r))
+    return r
+
+
+def w8a8_expert_gemm(codes, scales, packed, K: int, N: int, offsets, rows=None, dtype=None, out=None):
+    """The experts' products: slot i of expert e (offsets[e] <= i < offsets[e + 1],
+    int32 [experts + 1] on the device) is row rows[i] (int32 [slots]; i without rows)
+    of the codes times weight e.  Returns [slots, N] of dtype (fp16 unless given):
+    rows that no expert has are not written, one whose row of the codes does not
+    exist is zeros."""
+    torch = _torch()
+    _need_cuda(offsets, rows)
+    E = offsets.shape[0] - 1 if offsets.dim() == 1 else -1
+    if E < 1:
+        raise ValueError("offsets must be int32 [experts + 1]")
+    dtype, code = _codes_of(codes, scales, packed, K, N, E, dtype if out is None else dtype or out.dtype)
+    _int32(offsets, (E + 1,), codes.device, "offsets")
+    slots = codes.shape[0]
+    if rows is not None:
+        slots = rows.numel()
+        _int32(rows, (slots,), codes.device, "rows")
+    out = _product_out(out, dtype, codes.device, (slots, N))
+    if slots > 0 and codes.shape[0] == 0:        # no row exists: one that none asks for, for the call's checks
+        codes = torch.zeros((1, K), dtype=torch.int8, device=out.device)
+        scales = torch.zeros(1, dtype=torch.float32, device=out.device)
+        rows = torch.full_like(rows, -1)
+    if slots > 0:
+        _launch("tf_w8a8_expert_gemm", codes.device, code, _ptr(codes), _ptr(scales), codes.shape[0], _ptr(packed),
+                _ptr(offsets), _ptr(rows), _ptr(out), slots, K, N, E)
+    return out
+
+
+def combine_experts(y, weights, places, add=None, out=None):
+    """out[t] = add[t] + sum_j weights[t, j] * y[places[t, j]] for y [slots, N] (fp16 or
+    bf16), weights fp32 and places int32 [T, top_k], add [T, N] or None; sums in fp32.
+    A choice of weight 0 or of a place outside y adds nothing.  out may be add."""
+    torch = _torch()
+    _need_cuda(y, weights, places, add, out)
+    code = _dtype_code(y.dtype, "y")
+    if y.dim() != 2 or places.dim() != 2:
+        raise ValueError("y must be [slots, N] and places int32 [T, top_k]")
+    (T, k), N, dev = places.shape, y.shape[1], y.device
+    _int32(places, (T, k), dev, "places")
+    _same(weights, torch.float32, dev, (T, k), "weights")
+    if add is not None:
+        _same(add, y.dtype, dev, (T, N), "add")
+    out = _product_out(out, y.dtype, dev, (T, N))
+    if T > 0 and y.shape[0] == 0:                # no row exists: one that none asks for, for the call's checks
+        y, places = torch.zeros((1, N), dtype=y.dtype, device=dev), torch.full_like(places, -1)
+    if T > 0:
+        _launch("tf_combine_experts", dev, code, _ptr(y), y.shape[0], _ptr(weights), _ptr(places), _ptr(add), T, k, N,
+                _ptr(out))
     return out
