@@ -138,7 +138,7 @@ int launch_direct(const W8Args& a, hipStream_t s) {
 
 }  // namespace
 
-int launch_w8a8_tile(const W8Args& a, hipStream_t s);
+int launch_w8a8_tile(const W8Args& a, int form, hipStream_t s);
 
 int launch_w8a8(const W8Args& a, hipStream_t s) {
     // rows of a weight, on average
@@ -147,7 +147,7 @@ int launch_w8a8(const W8Args& a, hipStream_t s) {
     if (rows <= 32) return launch_direct<2, 1, 8, 4>(a, s);
     if (rows <= 64) return launch_direct<4, 2, 4, 4>(a, s);
     if (rows <= 192) return launch_direct<4, 4, 4, 3>(a, s);
-    return launch_w8a8_tile(a, s);
+    return launch_w8a8_tile(a, 0, s);
 }
 
 }  // namespace tf

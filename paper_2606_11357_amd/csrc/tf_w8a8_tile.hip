@@ -22,11 +22,23 @@
 namespace tf {
 namespace {
 
-constexpr int kBM = 256, kBN = 256, kThreads = 256, kXcds = 8;
-constexpr int kRB = kBM / 16;                    // 16-row blocks
-constexpr int kPairBytes = kBM * 128;            // A of two steps: 32 KB
-constexpr int kPairs = 4;                        // buffers
-constexpr int kRowGroup = 8;                     // row tiles that share the columns' order
+constexpr int kThreads = 256, kXcds = 8;
+
+// A form: RB row blocks of 16, CB column blocks of 16 a wave; P buffers of A, each of
+// two steps (a pair); weights R steps deep in registers; WGS workgroups a compute
+// unit.
+template <int RB_, int CB_, int P_, int R_, int WGS_>
+struct Form {
+    static constexpr int RB = RB_, CB = CB_, P = P_, R = R_, WGS = WGS_;
+    static constexpr int BM = 16 * RB, BN = 64 * CB;
+    static constexpr int kPairBytes = BM * 128;
+    static constexpr int kDma = RB / 4;                      // direct loads of a wave and step
+    static constexpr int kSlots = RB * CB;                   // matrix instructions of a wave and step
+    static constexpr bool kAhead = kSlots <= 8;              // two sets of fragments
+    static constexpr bool kOften = kSlots >= 64;             // a barrier every step: see the loop
+    static constexpr int kRowGroup = 2048 / BM;              // row tiles that share the columns' order
+    static_assert((P & (P - 1)) == 0 && R % 4 == 0, "buffers by a mask, whole pairs a pass of the loop");
+};
 
 __device__ __forceinline__ int a_swz(int row) { return row & 7; }
 
@@ -49,9 +61,20 @@ __device__ __forceinline__ u32x4 lds_read_block(uint32_t addr, int i) {
     }
 }
 __device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// All but the last NOW of this wave's reads are done (they return in order).
+template <int NOW>
+__device__ __forceinline__ void lds_wait_but() {
+    static_assert(NOW >= 0 && NOW < 16, "lgkmcnt holds 4 bits");
+    asm volatile("s_waitcnt lgkmcnt(%0)" ::"i"(NOW) : "memory");
+}
 
 __device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t r, uint32_t voff) {
     return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, 0, 0));
+}
+
+// A direct load: 16 bytes from each lane's offset to `to` + 16 lane in LDS.
+__device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, void* to, uint32_t voff) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, voff, 0, 0, 0);
 }
 
 // Accumulators are pinned to AGPRs; mfma_hazard_gap() stands between their
@@ -76,28 +99,31 @@ __device__ __forceinline__ void barrier_after_loads() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
+template <class F>
 struct TileShared {
-    uint8_t a[kPairs * kPairBytes];
-    float scale[kBM];
+    uint8_t a[F::P * F::kPairBytes];
+    float scale[F::BM];
 };
 
 // Tile number `at` of row tiles x column tiles, rows in groups of kRowGroup.
+template <class F>
 __device__ __forceinline__ void tile_of(int at, int tiles_m, int tiles_n, int& tm, int& tn) {
-    const int group = at / (kRowGroup * tiles_n), rest = at - group * kRowGroup * tiles_n;
-    const int height = min(kRowGroup, tiles_m - group * kRowGroup);
+    const int group = at / (F::kRowGroup * tiles_n), rest = at - group * F::kRowGroup * tiles_n;
+    const int height = min(F::kRowGroup, tiles_m - group * F::kRowGroup);
     tn = rest / height;
-    tm = group * kRowGroup + rest - tn * height;
+    tm = group * F::kRowGroup + rest - tn * height;
 }
 
 // Rows row0 .. row0 + rows - 1 of C (A's, or those that a.rows names) by columns
-// col0 .. col0 + 255 of `packed`.
-template <bool GATHER>
+// col0 .. col0 + BN - 1 of `packed`.
+template <class F, bool GATHER>
 __device__ __forceinline__ void tile_product(const W8Args& a, const uint8_t* packed, int64_t row0, int rows,
-                                             int64_t col0, TileShared& sm) {
+                                             int64_t col0, TileShared<F>& sm) {
+    constexpr int RB = F::RB, CB = F::CB, P = F::P, R = F::R, S = F::kSlots;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kg = lane >> 4;
-    const int steps = a.na, pairs = steps / 2, chunks = (steps + 3) / 4;
+    const int steps = a.na, pairs = steps / 2;
 
     // A: rows that are not there repeat one that is; they are not stored.
     // Rows of A are counted from `base`, of which `there` are.
@@ -109,138 +135,174 @@ __device__ __forceinline__ void tile_product(const W8Args& a, const uint8_t* pac
         return GATHER ? a.rows[row0 + min(r, rows - 1)] : r;
     };
     auto in = [&](int at) { return (uint32_t)at < (uint32_t)there; };
-    // Direct load r of wave w fills rows 64 w + 8 r .. + 7 of a buffer, eight lanes a row.
-    uint32_t avoff[8];
+    // Direct load r of wave w fills rows 4 RB w + 8 r .. + 7 of a buffer, eight lanes a row.
+    uint32_t avoff[RB / 2];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const int row = 64 * wave + 8 * r + (lane >> 3);
+    for (int r = 0; r < RB / 2; ++r) {
+        const int row = 4 * RB * wave + 8 * r + (lane >> 3);
         const int at = row_of(row);
         avoff[r] = (uint32_t)(in(at) ? at : 0) * (uint32_t)a.K + (uint32_t)((lane & 7) ^ a_swz(row)) * 16u;
     }
-    auto dma_a = [&](int pair, uint32_t buf, int r) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            ar, (__attribute__((address_space(3))) void*)(sm.a + buf + (8 * wave + r) * 1024), 16,
-            avoff[r] + (uint32_t)min(pair, pairs - 1) * 128u, 0, 0, 0);
+    auto dma_a = [&](int pair, int buf, int r) {
+        dma16(ar, sm.a + buf * F::kPairBytes + (RB / 2 * wave + r) * 1024, avoff[r] + (uint32_t)min(pair, pairs - 1) * 128u);
     };
     const uint32_t lds = (uint32_t)reinterpret_cast<uintptr_t>(sm.a);
     uint32_t a_lane[2];
 #pragma unroll
     for (int odd = 0; odd < 2; ++odd) a_lane[odd] = lds + (uint32_t)(c * 128 + ((kg + 4 * odd) ^ a_swz(c)) * 16);
 
-    // B: this wave's four panels; one past N is empty, and so is what follows K.
-    __amdgpu_buffer_rsrc_t wr[4];
+    // B: this wave's panels; one past N is empty, and so is what follows K.
+    __amdgpu_buffer_rsrc_t wr[CB];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int64_t panel = col0 / kW8Panel + 4 * wave + t;
+    for (int t = 0; t < CB; ++t) {
+        const int64_t panel = col0 / kW8Panel + CB * wave + t;
         const bool here = panel < a.np;
         wr[t] = make_rsrc(packed + (here ? panel : 0) * a.na * kW8AtomBytes, here ? (uint32_t)a.na * kW8AtomBytes : 0u);
     }
-    u32x4 ring[4][4];
+    u32x4 ring[R][CB];
     auto load_b = [&](int step, int t, u32x4& v) { v = load16(wr[t], (uint32_t)(lane * 16 + step * kW8AtomBytes)); };
 
-    uint32_t b0 = 0, b1 = kPairBytes, b2 = 2 * kPairBytes, b3 = 3 * kPairBytes;
-#pragma unroll
-    for (int r = 0; r < 8; ++r) dma_a(0, b0, r);
-#pragma unroll
-    for (int r = 0; r < 8; ++r) dma_a(1, b1, r);
-#pragma unroll
-    for (int j = 0; j < 3; ++j)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) load_b(j, t, ring[j][t]);
-#pragma unroll
-    for (int r = 0; r < 8; ++r) dma_a(2, b2, r);
-    i32x4 acc[kRB][4];
-#pragma unroll
-    for (int i = 0; i < kRB; ++i)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) acc[i][t] = i32x4{0, 0, 0, 0};
-    {
+    float row_scale = 0.f;
+    if (tid < F::BM) {
         const int at = row_of(tid);
         const float s = a.a_scale[in(at) ? base + at : 0];
-        sm.scale[tid] = in(at) ? s : 0.f;
+        row_scale = in(at) ? s : 0.f;
     }
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    u32x4 af[kRB];
+    // What is on its way when the loop begins: its own loads of the R - 1 steps before it,
+    // in its order (so that the same counts tell what has landed), and before them the
+    // halves of pairs that earlier steps would have brought, which are waited for.
+    constexpr int kOps = F::kDma + CB;                // vector-memory operations of a wave and step
+    constexpr int kHalf0 = F::kOften ? 2 * P - 2 : 2 * P - 3;      // half of a pair that step 0 brings
+    constexpr int kBefore = kHalf0 - (R - 1);
+    static_assert(kBefore >= 2, "the first pair is among those waited for");
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < kRB / 2; ++i) af[i] = lds_read_block(a_lane[0] + b0, i);
+    for (int h = 0; h < kBefore; ++h)
+#pragma unroll
+        for (int r = 0; r < F::kDma; ++r) dma_a(h / 2, h / 2, F::kDma * (h % 2) + r);
+#pragma unroll
+    for (int j = 0; j < R - 1; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int r = 0; r < F::kDma; ++r)
+            dma_a((kBefore + j) / 2, (kBefore + j) / 2, F::kDma * ((kBefore + j) % 2) + r);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < CB; ++t) load_b(j, t, ring[j][t]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    i32x4 acc[RB][CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int t = 0; t < CB; ++t) acc[i][t] = i32x4{0, 0, 0, 0};
+    if (tid < F::BM) sm.scale[tid] = row_scale;
     lds_wait();
+    barrier_after_loads<(R - 1) * kOps < 63 ? (R - 1) * kOps : 63>();
+    u32x4 af[F::kAhead ? 2 : 1][RB];
+#pragma unroll
+    for (int i = 0; i < (F::kAhead ? RB : RB - 1); ++i) af[0][i] = lds_read_block(a_lane[0], i);
     mfma_hazard_gap();
 
-    // Step s = 4 ch + j, 64 slots of one matrix instruction (row block q / 4, column
-    // block q % 4), each followed by at most one other:
-    //   0         wait for the fragments of row blocks 0..7
-    //   0..7      fragments of blocks 8..15
-    //   8..14     direct loads 4 (j % 2) .. + 3 of the pair three ahead
-    //   16..28    weights of step s + 3
-    //   32        wait for blocks 8..15
-    //   32..39    fragments of blocks 0..7 of step s + 1
-    // A pair is read from half a step before its first step on: at the end of the even
-    // step before, its direct loads have to have landed, which leaves this wave's later
-    // operations: the weights of the step of its last direct loads, and eight operations
-    // in each of three steps since.  The barrier of odd steps frees the pair's buffer.
-    for (int ch = 0; ch < chunks; ++ch) {
+    // Steps in turn, R to a pass of the loop (so that the ring has fixed places; steps
+    // past K multiply zeros), S slots each of one matrix instruction (row block q / CB,
+    // column block q % CB) and at most one of the others beside it, which are spread over
+    // the step: four waves at once ask LDS and the memory pipe for four times what one
+    // does, and an instruction that has to wait for its turn holds up those behind it.
+    //  - before slot CB i: wait for the fragment of row block i
+    //  - at slot CB i: read that of block i - 1 for the next step (block RB - 1 of this
+    //    step at slot 0).  Small forms (kAhead) read all of the next step's into a second
+    //    set.
+    //  - every S / kOps slots: a direct load (half a pair a step) or one of the weights of
+    //    step s + R - 1.
+    // Pair p is read from step 2 p - 1 on: at the end of step 2 p - 2 its direct loads
+    // have to have landed, which leaves this wave's later operations on their way (they
+    // complete in order).  After the barrier there no wave reads pair p - 2 any more, and
+    // the next two steps fill its buffer with pair p - 2 + P: one barrier for two steps.
+    // With kOften a second barrier ends the odd steps, after which pair p - 1 is done, and
+    // steps 2 p and 2 p + 1 fill its buffer: a step earlier, where four buffers of 32 KB
+    // are all there is.
+    constexpr int kLater = CB + (F::kOften ? 2 * P - 5 : 2 * P - 6) * kOps;
+    for (int s0 = 0; s0 < steps; s0 += R) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int step = 4 * ch + j, odd = j & 1;
-            const uint32_t bcur = j < 2 ? b0 : b1;
-            const uint32_t bnxt = j == 0 ? b0 : (j == 3 ? b2 : b1);
-            const uint32_t bdma = j < 2 ? b3 : b0;
-            const int dpair = 2 * ch + 3 + (j >> 1);
+        for (int j = 0; j < R; ++j) {
+            const int step = s0 + j, odd = j & 1;
+            auto place = [&](int pair) { return (uint32_t)((s0 / 2 + pair) & (P - 1)) * F::kPairBytes; };
+            const uint32_t cur = place(j / 2), next = place((j + 1) / 2);
+            // the pair whose half is filled in this step
+            const int fill = s0 / 2 + (F::kOften ? j / 2 + P - 1 : (j + 1) / 2 + P - 2);
+            const int half = F::kOften ? odd : odd ^ 1;
+            constexpr int kSets = F::kAhead ? 2 : 1;
+            u32x4 (&now)[RB] = af[j % kSets];
+            u32x4 (&nxt)[RB] = af[(j + 1) % kSets];
 #pragma unroll
-            for (int q = 0; q < 64; ++q) {
-                const int i = q / 4, t = q % 4;
+            for (int q = 0; q < S; ++q) {
+                const int i = q / CB, t = q % CB;
                 __builtin_amdgcn_sched_barrier(0);
-                if (q == 0 || q == 32) lds_wait();
-                mfma_i8(acc[i][t], ring[j][t], af[i]);
-                if (q < 8) af[8 + q] = lds_read_block(a_lane[odd] + bcur, 8 + q);
-                if (q >= 32 && q < 40) af[q - 32] = lds_read_block(a_lane[odd ^ 1] + bnxt, q - 32);
-                if (q >= 8 && q < 16 && q % 2 == 0) dma_a(dpair, bdma, 4 * odd + (q - 8) / 2);
-                if (q >= 16 && q < 32 && q % 4 == 0) load_b(step + 3, (q - 16) / 4, ring[(j + 3) % 4][(q - 16) / 4]);
+                if constexpr (F::kAhead) {
+                    if (q == 0) lds_wait();
+                } else {
+                    if (t == 0) lds_wait_but<RB - 2>();
+                }
+                mfma_i8(acc[i][t], ring[j % R][t], now[i]);
+                if constexpr (F::kAhead) {
+#pragma unroll
+                    for (int r = q * RB / S; r < (q + 1) * RB / S; ++r) nxt[r] = lds_read_block(a_lane[odd ^ 1] + next, r);
+                } else if (t == 0) {
+                    if (i == 0) now[RB - 1] = lds_read_block(a_lane[odd] + cur, RB - 1);
+                    else nxt[i - 1] = lds_read_block(a_lane[odd ^ 1] + next, i - 1);
+                }
+#pragma unroll
+                for (int o = 0; o < kOps; ++o) {
+                    if (q != o * S / kOps + CB / 2) continue;
+                    if (o < F::kDma) dma_a(fill, fill & (P - 1), F::kDma * half + o);
+                    else load_b(step + R - 1, o - F::kDma, ring[(j + R - 1) % R][o - F::kDma]);
+                }
             }
-            if (odd) barrier_only();
-            else barrier_after_loads<4 + 3 * 8>();
+            if (!odd) barrier_after_loads<kLater < 63 ? kLater : 63>();
+            else if (F::kOften) barrier_only();
         }
-        const uint32_t x0 = b0, x1 = b1;
-        b0 = b2;
-        b1 = b3;
-        b2 = x0;
-        b3 = x1;
     }
+    // The last step's reads, which nothing uses, keep their registers until they are done.
+    lds_wait();
+#pragma unroll
+    for (int i = 0; i < RB; ++i) asm volatile("" ::"v"(af[0][i]), "v"(af[F::kAhead ? 1 : 0][i]));
     mfma_hazard_gap();
     __builtin_amdgcn_s_waitcnt(0);       // the direct loads past the end have landed
     __syncthreads();                     // and no wave reads the buffers, which the output passes through
 
-    // A row block at a time through LDS (rows of 144 bytes), stored as 16 bytes a
-    // lane, eight whole 128-byte rows an instruction.
+    // A row block at a time through LDS (rows padded by 16 bytes), stored as 16 bytes a
+    // lane, 2 CB lanes a row.
     const float* scales = reinterpret_cast<const float*>(packed + a.s_off);
-    const int64_t wcol = col0 + 64 * wave;
-    float4_t sw[4];
+    const int64_t wcol = col0 + 16 * CB * wave;
+    float4_t sw[CB];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < CB; ++t) {
         const int64_t n = wcol + 16 * t + 4 * kg;
         sw[t] = n < a.np * 16 ? *reinterpret_cast<const float4_t*>(scales + n) : float4_t{0.f, 0.f, 0.f, 0.f};
     }
-    uint8_t* stage = sm.a + wave * 4096;
-    constexpr int kStageRow = 144;
-    const int rr = lane >> 3, cc = lane & 7;
+    constexpr int kStageRow = 32 * CB + 16, kLanes = 2 * CB, kAtOnce = 64 / kLanes;
+    uint8_t* stage = sm.a + wave * 16 * kStageRow;
+    const int rr = lane / kLanes, cc = lane % kLanes;
 #pragma unroll
-    for (int i = 0; i < kRB; ++i) {
+    for (int i = 0; i < RB; ++i) {
         __builtin_amdgcn_sched_barrier(0);
         const float sa = sm.scale[16 * i + c];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < CB; ++t)
             *reinterpret_cast<uint2*>(stage + c * kStageRow + 32 * t + 8 * kg) = w8_scaled(a.bf, acc[i][t], sa, sw[t]);
         __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): this wave's stores landed
-        u32x4 v[2];
+        constexpr int kTimes = kAtOnce > 16 ? 1 : 16 / kAtOnce;
+        u32x4 v[kTimes];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const u32x4*>(stage + (rr + 8 * h) * kStageRow + 16 * cc);
+        for (int h = 0; h < kTimes; ++h)
+            v[h] = *reinterpret_cast<const u32x4*>(stage + (rr % 16 + kAtOnce * h) * kStageRow + 16 * cc);
         __builtin_amdgcn_s_waitcnt(0xC07F);       // read before the area is written again
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = 16 * i + rr + 8 * h;
+        for (int h = 0; h < kTimes; ++h) {
+            const int r = 16 * i + rr + kAtOnce * h;
             const int64_t n = wcol + 8 * cc;
-            if (r < rows && n < a.N) *reinterpret_cast<u32x4*>(a.C + (row0 + r) * a.N + n) = v[h];
+            if (rr < 16 && r < rows && n < a.N) *reinterpret_cast<u32x4*>(a.C + (row0 + r) * a.N + n) = v[h];
         }
     }
 }
@@ -252,23 +314,24 @@ __device__ __forceinline__ int place_of(int b, int total) {
     return i < per + (x < rem ? 1 : 0) ? x * per + min(x, rem) + i : -1;
 }
 
-__global__ __launch_bounds__(kThreads, 1) void w8a8_tile_kernel(W8Args a, int tiles_m, int tiles_n) {
-    __shared__ __align__(16) TileShared sm;
+template <class F>
+__global__ __launch_bounds__(kThreads, F::WGS) void w8a8_tile_kernel(W8Args a, int tiles_m, int tiles_n) {
+    __shared__ __align__(16) TileShared<F> sm;
     const int at = place_of(blockIdx.x, tiles_m * tiles_n);
     if (at < 0) return;
     int tm, tn;
-    tile_of(at, tiles_m, tiles_n, tm, tn);
+    tile_of<F>(at, tiles_m, tiles_n, tm, tn);
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
-    const int64_t row0 = (int64_t)tm * kBM;
-    tile_product<false>(a, a.packed, row0, (int)min((int64_t)kBM, a.M - row0), (int64_t)tn * kBN, sm);
+    const int64_t row0 = (int64_t)tm * F::BM;
+    tile_product<F, false>(a, a.packed, row0, (int)min((int64_t)F::BM, a.M - row0), (int64_t)tn * F::BN, sm);
 }
 
 // By expert: the row tiles of all experts in one list, found from the offsets by
 // every workgroup (thread t has experts 4 t .. 4 t + 3).
-template <bool GATHER>
-__global__ __launch_bounds__(kThreads, 1) void w8a8_tile_experts_kernel(W8Args a, int tiles_n) {
-    __shared__ __align__(16) TileShared sm;
+template <class F, bool GATHER>
+__global__ __launch_bounds__(kThreads, F::WGS) void w8a8_tile_experts_kernel(W8Args a, int tiles_n) {
+    __shared__ __align__(16) TileShared<F> sm;
     int* ints = reinterpret_cast<int*>(sm.a);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // offsets with a running maximum within the call's slots
@@ -299,7 +362,7 @@ __global__ __launch_bounds__(kThreads, 1) void w8a8_tile_experts_kernel(W8Args a
         end[u] = max(end[u], before);
         if (4 * tid + u >= a.experts) end[u] = before;
         before = end[u];
-        tiles[u] = (end[u] - start[u] + kBM - 1) / kBM;
+        tiles[u] = (end[u] - start[u] + F::BM - 1) / F::BM;
         mine += tiles[u];
     }
     int scan = mine;
@@ -318,37 +381,49 @@ __global__ __launch_bounds__(kThreads, 1) void w8a8_tile_experts_kernel(W8Args a
     const int at = place_of(blockIdx.x, total * tiles_n);
     if (at < 0) return;                               // (the whole workgroup)
     int tm, tn;
-    tile_of(at, total, tiles_n, tm, tn);
+    tile_of<F>(at, total, tiles_n, tm, tn);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         if (tm >= from && tm < from + tiles[u]) {
             ints[16] = 4 * tid + u;
-            ints[17] = start[u] + (tm - from) * kBM;
+            ints[17] = start[u] + (tm - from) * F::BM;
             ints[18] = end[u];
         }
         from += tiles[u];
     }
     __syncthreads();
     const int e = __builtin_amdgcn_readfirstlane(ints[16]), row0 = __builtin_amdgcn_readfirstlane(ints[17]);
-    const int rows = min(kBM, __builtin_amdgcn_readfirstlane(ints[18]) - row0);
+    const int rows = min(F::BM, __builtin_amdgcn_readfirstlane(ints[18]) - row0);
     tn = __builtin_amdgcn_readfirstlane(tn);
     __syncthreads();                                  // the buffers take this place
-    tile_product<GATHER>(a, a.packed + e * a.total, row0, rows, (int64_t)tn * kBN, sm);
+    tile_product<F, GATHER>(a, a.packed + e * a.total, row0, rows, (int64_t)tn * F::BN, sm);
+}
+
+template <class F>
+int launch_form(const W8Args& a, hipStream_t s) {
+    const int64_t tiles_n = (a.N + F::BN - 1) / F::BN;
+    if (a.experts) {
+        const int64_t most = std::min<int64_t>(a.M, a.M / F::BM + a.experts);     // row tiles
+        const dim3 grid((unsigned)((most * tiles_n + 7) / 8 * 8));
+        return a.rows ? launch(w8a8_tile_experts_kernel<F, true>, grid, dim3(kThreads), 0, s, a, (int)tiles_n)
+                      : launch(w8a8_tile_experts_kernel<F, false>, grid, dim3(kThreads), 0, s, a, (int)tiles_n);
+    }
+    const int64_t tiles_m = (a.M + F::BM - 1) / F::BM;
+    return launch(w8a8_tile_kernel<F>, dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8)), dim3(kThreads), 0, s, a,
+                  (int)tiles_m, (int)tiles_n);
 }
 
 }  // namespace
 
-int launch_w8a8_tile(const W8Args& a, hipStream_t s) {
-    const int64_t tiles_n = (a.N + kBN - 1) / kBN;
-    if (a.experts) {
-        const int64_t most = std::min<int64_t>(a.M, a.M / kBM + a.experts);     // row tiles
-        const dim3 grid((unsigned)((most * tiles_n + 7) / 8 * 8));
-        return a.rows ? launch(w8a8_tile_experts_kernel<true>, grid, dim3(kThreads), 0, s, a, (int)tiles_n)
-                      : launch(w8a8_tile_experts_kernel<false>, grid, dim3(kThreads), 0, s, a, (int)tiles_n);
+int launch_w8a8_tile(const W8Args& a, int form, hipStream_t s) {
+    switch (form) {
+        case 0: return launch_form<Form<16, 4, 4, 4, 1>>(a, s);
+        case 1: return launch_form<Form<8, 4, 8, 8, 1>>(a, s);
+        case 2: return launch_form<Form<8, 4, 4, 4, 2>>(a, s);
+        case 3: return launch_form<Form<8, 2, 8, 8, 1>>(a, s);
+        case 4: return launch_form<Form<4, 2, 8, 8, 2>>(a, s);
+        default: return launch_form<Form<4, 1, 8, 8, 2>>(a, s);
     }
-    const int64_t tiles_m = (a.M + kBM - 1) / kBM;
-    return launch(w8a8_tile_kernel, dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8)), dim3(kThreads), 0, s, a,
-                  (int)tiles_m, (int)tiles_n);
 }
 
 }  // namespace tf
