@@ -138,16 +138,6 @@ int launch_direct(const W8Args& a, hipStream_t s) {
 
 }  // namespace
 
-int launch_w8a8_tile(const W8Args& a, int form, hipStream_t s);
-
-int launch_w8a8(const W8Args& a, hipStream_t s) {
-    // rows of a weight, on average
-    const int64_t rows = a.experts ? (a.M + a.experts - 1) / a.experts : a.M;
-    if (rows <= 16) return launch_direct<1, 1, 8, 8>(a, s);
-    if (rows <= 32) return launch_direct<2, 1, 8, 4>(a, s);
-    if (rows <= 64) return launch_direct<4, 2, 4, 4>(a, s);
-    if (rows <= 192) return launch_direct<4, 4, 4, 3>(a, s);
-    return launch_w8a8_tile(a, 0, s);
-}
+int launch_w8a8_direct(const W8Args& a, hipStream_t s) { return launch_direct<1, 1, 4, 8>(a, s); }
 
 }  // namespace tf

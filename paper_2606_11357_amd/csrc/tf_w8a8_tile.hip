@@ -77,6 +77,28 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, void* to, uint32
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 16, voff, 0, 0, 0);
 }
 
+// v as a value of its own, so that what is computed from it for one tile is computed
+// again for the next and not held in registers between.
+__device__ __forceinline__ int again(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+constexpr uint32_t kNowhere = 0xFFFFFF00u;        // an offset that no buffer reaches: not stored
+__device__ __forceinline__ void store16(__amdgpu_buffer_rsrc_t r, const u32x4& v, uint32_t voff) {
+    __builtin_amdgcn_raw_buffer_store_b128(v, r, voff, 0, kSc1);
+}
+__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t r, const uint2& v, uint32_t voff) {
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{v.x, v.y}, r, voff, 0, kSc1);
+}
+// Rows of 16 lanes swapped: lanes of row 2 g get (x, x of row 2 g + 1), those of row
+// 2 g + 1 (y of row 2 g, y).
+__device__ __forceinline__ u32x4 rows_swapped(const uint2& x, const uint2& y) {
+    const auto p = __builtin_amdgcn_permlane16_swap(x.x, y.x, false, false);
+    const auto q = __builtin_amdgcn_permlane16_swap(x.y, y.y, false, false);
+    return u32x4{p[0], q[0], p[1], q[1]};
+}
+
 // Accumulators are pinned to AGPRs; mfma_hazard_gap() stands between their
 // initialisation and the first, and between the last and their first read.
 __device__ __forceinline__ void mfma_i8(i32x4& acc, const u32x4& a, const u32x4& b) {
@@ -102,7 +124,16 @@ __device__ __forceinline__ void barrier_after_loads() {
 template <class F>
 struct TileShared {
     uint8_t a[F::P * F::kPairBytes];
-    float scale[F::BM];
+    float rows[2][F::BM], columns[2][F::BN];          // scales of this tile and the next
+    int found[4];
+};
+
+// One tile of C: rows row0 .. row0 + rows - 1 (A's, or those that a.rows names) by
+// columns col0 .. col0 + BN - 1 of `packed`.
+struct Tile {
+    const uint8_t* packed;
+    int64_t row0, col0;
+    int rows;
 };
 
 // Tile number `at` of row tiles x column tiles, rows in groups of kRowGroup.
@@ -114,94 +145,110 @@ __device__ __forceinline__ void tile_of(int at, int tiles_m, int tiles_n, int& t
     tm = group * F::kRowGroup + rest - tn * height;
 }
 
-// Rows row0 .. row0 + rows - 1 of C (A's, or those that a.rows names) by columns
-// col0 .. col0 + BN - 1 of `packed`.
-template <class F, bool GATHER>
-__device__ __forceinline__ void tile_product(const W8Args& a, const uint8_t* packed, int64_t row0, int rows,
-                                             int64_t col0, TileShared<F>& sm) {
+// Tiles next(0), next(1), ... (false: no more).  The loads that a tile begins with are
+// issued before the outputs of the one before are scaled and stored.
+template <class F, bool GATHER, class Next>
+__device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile, TileShared<F>& sm) {
     constexpr int RB = F::RB, CB = F::CB, P = F::P, R = F::R, S = F::kSlots;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kg = lane >> 4;
     const int steps = a.na, pairs = steps / 2;
 
-    // A: rows that are not there repeat one that is; they are not stored.
-    // Rows of A are counted from `base`, of which `there` are.
-    const int64_t base = GATHER ? 0 : row0;
-    const int there = GATHER ? (int)a.a_rows : (int)max(min(a.a_rows - row0, (int64_t)rows), (int64_t)0);
-    const __amdgpu_buffer_rsrc_t ar =
-        make_rsrc(a.A + base * a.K, (uint32_t)min((a.a_rows - base) * a.K, (int64_t)0xFFFFFF00));
-    auto row_of = [&](int r) {                        // a row of C as one of A; not there: negative or past `there`
-        return GATHER ? a.rows[row0 + min(r, rows - 1)] : r;
-    };
-    auto in = [&](int at) { return (uint32_t)at < (uint32_t)there; };
-    // Direct load r of wave w fills rows 4 RB w + 8 r .. + 7 of a buffer, eight lanes a row.
+    __amdgpu_buffer_rsrc_t ar, wr[CB];
     uint32_t avoff[RB / 2];
-#pragma unroll
-    for (int r = 0; r < RB / 2; ++r) {
-        const int row = 4 * RB * wave + 8 * r + (lane >> 3);
-        const int at = row_of(row);
-        avoff[r] = (uint32_t)(in(at) ? at : 0) * (uint32_t)a.K + (uint32_t)((lane & 7) ^ a_swz(row)) * 16u;
-    }
+    float row_scale = 0.f, column_scale = 0.f;
+    // Direct load r of wave w fills rows 4 RB w + 8 r .. + 7 of a buffer, eight lanes a row.
     auto dma_a = [&](int pair, int buf, int r) {
         dma16(ar, sm.a + buf * F::kPairBytes + (RB / 2 * wave + r) * 1024, avoff[r] + (uint32_t)min(pair, pairs - 1) * 128u);
     };
+    u32x4 ring[R][CB];
+    auto load_b = [&](int step, int t, u32x4& v) { v = load16(wr[t], (uint32_t)(lane * 16 + step * kW8AtomBytes)); };
+
+    constexpr int kOps = F::kDma + CB;                // vector-memory operations of a wave and step
+    constexpr int kHalf0 = F::kOften ? 2 * P - 2 : 2 * P - 3;      // half of a pair that step 0 brings
+    constexpr int kBefore = kHalf0 - (R - 1);
+    static_assert(kBefore >= 2, "the first pair is among those waited for");
+    // A tile's operands, and what is on its way when its loop begins: the loop's own loads
+    // of the R - 1 steps before it, in its order (so that the same counts tell what has
+    // landed), and before them the halves of pairs that earlier steps would have brought,
+    // which are waited for.
+    auto begin = [&](const Tile& t) {
+        const int lane = again(threadIdx.x & 63), tid = 64 * wave + lane;
+        // Rows of A are counted from `base`, of which `there` are; rows that are not there
+        // repeat one that is, and are not stored or scaled by 0.
+        const int64_t base = GATHER ? 0 : t.row0;
+        const int there = GATHER ? (int)a.a_rows : (int)max(min(a.a_rows - t.row0, (int64_t)t.rows), (int64_t)0);
+        const int64_t first = there > 0 ? base : 0;
+        ar = make_rsrc(a.A + first * a.K, (uint32_t)min((a.a_rows - first) * a.K, (int64_t)0xFFFFFF00));
+        auto row_of = [&](int r) { return GATHER ? a.rows[t.row0 + min(r, t.rows - 1)] : r; };
+        auto in = [&](int at) { return (uint32_t)at < (uint32_t)there; };
+#pragma unroll
+        for (int r = 0; r < RB / 2; ++r) {
+            const int row = 4 * RB * wave + 8 * r + (lane >> 3);
+            const int at = row_of(row);
+            avoff[r] = (uint32_t)(in(at) ? at : 0) * (uint32_t)a.K + (uint32_t)((lane & 7) ^ a_swz(row)) * 16u;
+        }
+        // this wave's panels; one past N is empty, and so is what follows K
+#pragma unroll
+        for (int u = 0; u < CB; ++u) {
+            const int64_t panel = t.col0 / kW8Panel + CB * wave + u;
+            const bool here = panel < a.np;
+            wr[u] = make_rsrc(t.packed + (here ? panel : 0) * a.na * kW8AtomBytes, here ? (uint32_t)a.na * kW8AtomBytes : 0u);
+        }
+        if (tid < F::BM) {
+            const int at = row_of(tid);
+            const float s = a.a_scale[in(at) ? base + at : 0];
+            row_scale = in(at) ? s : 0.f;
+        }
+        if (tid < F::BN) {
+            const int64_t n = t.col0 + tid;
+            column_scale = reinterpret_cast<const float*>(t.packed + a.s_off)[n < a.np * 16 ? n : 0];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int h = 0; h < kBefore; ++h)
+#pragma unroll
+            for (int r = 0; r < F::kDma; ++r) dma_a(h / 2, h / 2, F::kDma * (h % 2) + r);
+#pragma unroll
+        for (int j = 0; j < R - 1; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int r = 0; r < F::kDma; ++r)
+                dma_a((kBefore + j) / 2, (kBefore + j) / 2, F::kDma * ((kBefore + j) % 2) + r);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < CB; ++u) load_b(j, u, ring[j][u]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
     const uint32_t lds = (uint32_t)reinterpret_cast<uintptr_t>(sm.a);
     uint32_t a_lane[2];
 #pragma unroll
     for (int odd = 0; odd < 2; ++odd) a_lane[odd] = lds + (uint32_t)(c * 128 + ((kg + 4 * odd) ^ a_swz(c)) * 16);
 
-    // B: this wave's panels; one past N is empty, and so is what follows K.
-    __amdgpu_buffer_rsrc_t wr[CB];
-#pragma unroll
-    for (int t = 0; t < CB; ++t) {
-        const int64_t panel = col0 / kW8Panel + CB * wave + t;
-        const bool here = panel < a.np;
-        wr[t] = make_rsrc(packed + (here ? panel : 0) * a.na * kW8AtomBytes, here ? (uint32_t)a.na * kW8AtomBytes : 0u);
-    }
-    u32x4 ring[R][CB];
-    auto load_b = [&](int step, int t, u32x4& v) { v = load16(wr[t], (uint32_t)(lane * 16 + step * kW8AtomBytes)); };
-
-    float row_scale = 0.f;
-    if (tid < F::BM) {
-        const int at = row_of(tid);
-        const float s = a.a_scale[in(at) ? base + at : 0];
-        row_scale = in(at) ? s : 0.f;
-    }
-    // What is on its way when the loop begins: its own loads of the R - 1 steps before it,
-    // in its order (so that the same counts tell what has landed), and before them the
-    // halves of pairs that earlier steps would have brought, which are waited for.
-    constexpr int kOps = F::kDma + CB;                // vector-memory operations of a wave and step
-    constexpr int kHalf0 = F::kOften ? 2 * P - 2 : 2 * P - 3;      // half of a pair that step 0 brings
-    constexpr int kBefore = kHalf0 - (R - 1);
-    static_assert(kBefore >= 2, "the first pair is among those waited for");
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int h = 0; h < kBefore; ++h)
-#pragma unroll
-        for (int r = 0; r < F::kDma; ++r) dma_a(h / 2, h / 2, F::kDma * (h % 2) + r);
-#pragma unroll
-    for (int j = 0; j < R - 1; ++j) {
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int r = 0; r < F::kDma; ++r)
-            dma_a((kBefore + j) / 2, (kBefore + j) / 2, F::kDma * ((kBefore + j) % 2) + r);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int t = 0; t < CB; ++t) load_b(j, t, ring[j][t]);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    Tile tile;
+    if (!next_tile(0, tile)) return;
+    begin(tile);
+    constexpr int kStores = RB * CB / 2;              // of a wave and tile
+    for (int turn = 0;; ++turn) {
     i32x4 acc[RB][CB];
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
         for (int t = 0; t < CB; ++t) acc[i][t] = i32x4{0, 0, 0, 0};
-    if (tid < F::BM) sm.scale[tid] = row_scale;
+    if (tid < F::BM) sm.rows[turn & 1][tid] = row_scale;
+    if (tid < F::BN) sm.columns[turn & 1][tid] = column_scale;
     lds_wait();
-    barrier_after_loads<(R - 1) * kOps < 63 ? (R - 1) * kOps : 63>();
+    // (the outputs of the tile before were stored after these loads were issued)
+    constexpr int kFirst = (R - 1) * kOps, kNext = kFirst + kStores;
+    if (turn == 0) barrier_after_loads<kFirst < 63 ? kFirst : 63>();
+    else barrier_after_loads<kNext < 63 ? kNext : 63>();
     u32x4 af[F::kAhead ? 2 : 1][RB];
 #pragma unroll
     for (int i = 0; i < (F::kAhead ? RB : RB - 1); ++i) af[0][i] = lds_read_block(a_lane[0], i);
+    lds_wait();
     mfma_hazard_gap();
 
     // Steps in turn, R to a pass of the loop (so that the ring has fixed places; steps
@@ -269,62 +316,83 @@ __device__ __forceinline__ void tile_product(const W8Args& a, const uint8_t* pac
     for (int i = 0; i < RB; ++i) asm volatile("" ::"v"(af[0][i]), "v"(af[F::kAhead ? 1 : 0][i]));
     mfma_hazard_gap();
     __builtin_amdgcn_s_waitcnt(0);       // the direct loads past the end have landed
-    __syncthreads();                     // and no wave reads the buffers, which the output passes through
+    __syncthreads();                     // and no wave reads the buffers
+    const Tile done = tile;
+    const bool more = next_tile(turn + 1, tile);
+    if (more) begin(tile);
 
-    // A row block at a time through LDS (rows padded by 16 bytes), stored as 16 bytes a
-    // lane, 2 CB lanes a row.
-    const float* scales = reinterpret_cast<const float*>(packed + a.s_off);
-    const int64_t wcol = col0 + 16 * CB * wave;
+    // Outputs.  Lane (c, kg) holds row 16 i + c, columns 16 t + 4 kg + 0..3 of the wave's;
+    // rows of 16 lanes swapped between blocks t and t + 1 make that eight columns a lane,
+    // 64 bytes of a row of C a store.  Rows and columns past the end have offsets that the
+    // buffer drops: the number of stores is the same for every tile.
+    {
+    const int lane = again(threadIdx.x & 63), c = lane & 15, kg = lane >> 4;
+    const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.C + done.row0 * a.N, (uint32_t)done.rows * (uint32_t)a.N * 2u);
+    const float* sr = sm.rows[turn & 1];
+    const float* sc = sm.columns[turn & 1] + 16 * CB * wave + 4 * kg;
     float4_t sw[CB];
 #pragma unroll
-    for (int t = 0; t < CB; ++t) {
-        const int64_t n = wcol + 16 * t + 4 * kg;
-        sw[t] = n < a.np * 16 ? *reinterpret_cast<const float4_t*>(scales + n) : float4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < CB; ++t) sw[t] = *reinterpret_cast<const float4_t*>(sc + 16 * t);
+    uint32_t to[(CB + 1) / 2];
+#pragma unroll
+    for (int t = 0; t < CB; t += 2) {
+        const int64_t n = done.col0 + 16 * CB * wave + (CB > 1 ? 16 * (t + (kg & 1)) + 8 * (kg >> 1) : 4 * kg);
+        to[t / 2] = n < a.N ? (uint32_t)n * 2u : kNowhere;
     }
-    constexpr int kStageRow = 32 * CB + 16, kLanes = 2 * CB, kAtOnce = 64 / kLanes;
-    uint8_t* stage = sm.a + wave * 16 * kStageRow;
-    const int rr = lane / kLanes, cc = lane % kLanes;
+    uint32_t row = (uint32_t)c * (uint32_t)a.N * 2u, sixteen = 32u * (uint32_t)a.N;
+    int left = done.rows;
+    auto store_all = [&](auto is_bf) {
+        constexpr bool bf = decltype(is_bf)::value;
 #pragma unroll
-    for (int i = 0; i < RB; ++i) {
-        __builtin_amdgcn_sched_barrier(0);
-        const float sa = sm.scale[16 * i + c];
+        for (int i = 0; i < RB; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            const float sa = sr[16 * i + c];
+            const bool here = c < left;
 #pragma unroll
-        for (int t = 0; t < CB; ++t)
-            *reinterpret_cast<uint2*>(stage + c * kStageRow + 32 * t + 8 * kg) = w8_scaled(a.bf, acc[i][t], sa, sw[t]);
-        __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): this wave's stores landed
-        constexpr int kTimes = kAtOnce > 16 ? 1 : 16 / kAtOnce;
-        u32x4 v[kTimes];
-#pragma unroll
-        for (int h = 0; h < kTimes; ++h)
-            v[h] = *reinterpret_cast<const u32x4*>(stage + (rr % 16 + kAtOnce * h) * kStageRow + 16 * cc);
-        __builtin_amdgcn_s_waitcnt(0xC07F);       // read before the area is written again
-#pragma unroll
-        for (int h = 0; h < kTimes; ++h) {
-            const int r = 16 * i + rr + kAtOnce * h;
-            const int64_t n = wcol + 8 * cc;
-            if (rr < 16 && r < rows && n < a.N) *reinterpret_cast<u32x4*>(a.C + (row0 + r) * a.N + n) = v[h];
+            for (int t = 0; t < CB; t += 2) {
+                const uint32_t off = here && to[t / 2] != kNowhere ? row + to[t / 2] : kNowhere;
+                const uint2 x = w8_scaled(bf, acc[i][t], sa, sw[t]);
+                if constexpr (CB > 1) {
+                    const uint2 y = w8_scaled(bf, acc[i][t + 1], sa, sw[t + 1]);
+                    store16(cr, rows_swapped(x, y), off);
+                } else {
+                    store8(cr, x, off);
+                }
+            }
+            row += sixteen;
+            left -= 16;
         }
+    };
+    if (a.bf) store_all(std::true_type{});
+    else store_all(std::false_type{});
+    }
+    if (!more) return;
     }
 }
 
-// The place in the list of workgroup b's tile: each XCD (workgroups go to the eight in
-// turn) has a contiguous part of the list.  Past the end: -1.
-__device__ __forceinline__ int place_of(int b, int total) {
-    const int per = total / kXcds, rem = total % kXcds, x = b % kXcds, i = b / kXcds;
+// The place in the list of workgroup b's tile number k: each XCD (workgroups go to the
+// eight in turn) has a contiguous part of the list and goes through it in order.  Past
+// the end: -1.
+__device__ __forceinline__ int place_of(int b, int grid, int k, int total) {
+    const int per = total / kXcds, rem = total % kXcds, x = b % kXcds, i = b / kXcds + k * (grid / kXcds);
     return i < per + (x < rem ? 1 : 0) ? x * per + min(x, rem) + i : -1;
 }
 
 template <class F>
 __global__ __launch_bounds__(kThreads, F::WGS) void w8a8_tile_kernel(W8Args a, int tiles_m, int tiles_n) {
     __shared__ __align__(16) TileShared<F> sm;
-    const int at = place_of(blockIdx.x, tiles_m * tiles_n);
-    if (at < 0) return;
-    int tm, tn;
-    tile_of<F>(at, tiles_m, tiles_n, tm, tn);
-    tm = __builtin_amdgcn_readfirstlane(tm);
-    tn = __builtin_amdgcn_readfirstlane(tn);
-    const int64_t row0 = (int64_t)tm * F::BM;
-    tile_product<F, false>(a, a.packed, row0, (int)min((int64_t)F::BM, a.M - row0), (int64_t)tn * F::BN, sm);
+    auto next_tile = [&](int k, Tile& t) {
+        const int at = place_of(blockIdx.x, gridDim.x, k, tiles_m * tiles_n);
+        if (at < 0) return false;
+        int tm, tn;
+        tile_of<F>(at, tiles_m, tiles_n, tm, tn);
+        t.packed = a.packed;
+        t.row0 = (int64_t)__builtin_amdgcn_readfirstlane(tm) * F::BM;
+        t.col0 = (int64_t)__builtin_amdgcn_readfirstlane(tn) * F::BN;
+        t.rows = (int)min((int64_t)F::BM, a.M - t.row0);
+        return true;
+    };
+    tile_products<F, false>(a, next_tile, sm);
 }
 
 // By expert: the row tiles of all experts in one list, found from the offsets by
@@ -378,39 +446,42 @@ __global__ __launch_bounds__(kThreads, F::WGS) void w8a8_tile_experts_kernel(W8A
         if (w < wave) from += ints[8 + w];
         total += ints[8 + w];
     }
-    const int at = place_of(blockIdx.x, total * tiles_n);
-    if (at < 0) return;                               // (the whole workgroup)
-    int tm, tn;
-    tile_of<F>(at, total, tiles_n, tm, tn);
+    __syncthreads();                                  // the buffers take the place of these numbers
+    auto next_tile = [&](int k, Tile& t) {
+        const int at = place_of(blockIdx.x, gridDim.x, k, total * tiles_n);
+        if (at < 0) return false;                     // (the whole workgroup)
+        int tm, tn, f = from;
+        tile_of<F>(at, total, tiles_n, tm, tn);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        if (tm >= from && tm < from + tiles[u]) {
-            ints[16] = 4 * tid + u;
-            ints[17] = start[u] + (tm - from) * F::BM;
-            ints[18] = end[u];
+        for (int u = 0; u < 4; ++u) {
+            if (tm >= f && tm < f + tiles[u]) {
+                sm.found[0] = 4 * tid + u;
+                sm.found[1] = start[u] + (tm - f) * F::BM;
+                sm.found[2] = end[u];
+            }
+            f += tiles[u];
         }
-        from += tiles[u];
-    }
-    __syncthreads();
-    const int e = __builtin_amdgcn_readfirstlane(ints[16]), row0 = __builtin_amdgcn_readfirstlane(ints[17]);
-    const int rows = min(F::BM, __builtin_amdgcn_readfirstlane(ints[18]) - row0);
-    tn = __builtin_amdgcn_readfirstlane(tn);
-    __syncthreads();                                  // the buffers take this place
-    tile_product<F, GATHER>(a, a.packed + e * a.total, row0, rows, (int64_t)tn * F::BN, sm);
+        __syncthreads();
+        t.packed = a.packed + __builtin_amdgcn_readfirstlane(sm.found[0]) * a.total;
+        t.row0 = __builtin_amdgcn_readfirstlane(sm.found[1]);
+        t.rows = min(F::BM, __builtin_amdgcn_readfirstlane(sm.found[2]) - (int)t.row0);
+        t.col0 = (int64_t)__builtin_amdgcn_readfirstlane(tn) * F::BN;
+        return true;                                  // (barriers follow before the next call)
+    };
+    tile_products<F, GATHER>(a, next_tile, sm);
 }
 
 template <class F>
 int launch_form(const W8Args& a, hipStream_t s) {
     const int64_t tiles_n = (a.N + F::BN - 1) / F::BN;
-    if (a.experts) {
-        const int64_t most = std::min<int64_t>(a.M, a.M / F::BM + a.experts);     // row tiles
-        const dim3 grid((unsigned)((most * tiles_n + 7) / 8 * 8));
-        return a.rows ? launch(w8a8_tile_experts_kernel<F, true>, grid, dim3(kThreads), 0, s, a, (int)tiles_n)
-                      : launch(w8a8_tile_experts_kernel<F, false>, grid, dim3(kThreads), 0, s, a, (int)tiles_n);
-    }
-    const int64_t tiles_m = (a.M + F::BM - 1) / F::BM;
-    return launch(w8a8_tile_kernel<F>, dim3((unsigned)((tiles_m * tiles_n + 7) / 8 * 8)), dim3(kThreads), 0, s, a,
-                  (int)tiles_m, (int)tiles_n);
+    const int64_t tiles_m = a.experts ? std::min<int64_t>(a.M, a.M / F::BM + a.experts)      // at most
+                                      : (a.M + F::BM - 1) / F::BM;
+    // as many workgroups as run at a time, whole eights
+    const int64_t most = (int64_t)device_cus(s) * F::WGS;
+    const dim3 grid((unsigned)((std::min(tiles_m * tiles_n, most) + kXcds - 1) / kXcds * kXcds));
+    if (!a.experts) return launch(w8a8_tile_kernel<F>, grid, dim3(kThreads), 0, s, a, (int)tiles_m, (int)tiles_n);
+    return a.rows ? launch(w8a8_tile_experts_kernel<F, true>, grid, dim3(kThreads), 0, s, a, (int)tiles_n)
+                  : launch(w8a8_tile_experts_kernel<F, false>, grid, dim3(kThreads), 0, s, a, (int)tiles_n);
 }
 
 }  // namespace
@@ -419,9 +490,8 @@ int launch_w8a8_tile(const W8Args& a, int form, hipStream_t s) {
     switch (form) {
         case 0: return launch_form<Form<16, 4, 4, 4, 1>>(a, s);
         case 1: return launch_form<Form<8, 4, 8, 8, 1>>(a, s);
-        case 2: return launch_form<Form<8, 4, 4, 4, 2>>(a, s);
-        case 3: return launch_form<Form<8, 2, 8, 8, 1>>(a, s);
-        case 4: return launch_form<Form<4, 2, 8, 8, 2>>(a, s);
+        case 2: return launch_form<Form<8, 2, 8, 8, 1>>(a, s);
+        case 3: return launch_form<Form<4, 2, 8, 8, 2>>(a, s);
         default: return launch_form<Form<4, 1, 8, 8, 2>>(a, s);
     }
 }
