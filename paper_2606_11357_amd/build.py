@@ -100,6 +100,8 @@ BINDING_SRC = os.path.join(PKG, "binding", "tf_binding.cpp")
 BINDING = os.path.join(PKG, "_tf_binding.so")
 BINDING_OPS_SRC = os.path.join(PKG, "binding", "tf_binding_ops.cpp")
 BINDING_OPS = os.path.join(PKG, "_tf_binding_ops.so")
+BINDING_EXPERTS_SRC = os.path.join(PKG, "binding", "tf_binding_experts.cpp")
+BINDING_EXPERTS = os.path.join(PKG, "_tf_binding_experts.so")
 
 
 def build_binding(src: str | None = None, out: str | None = None) -> str:
@@ -124,14 +126,15 @@ def build_binding(src: str | None = None, out: str | None = None) -> str:
 
 
 def build(verbose: bool = False) -> str:
-    with cf.ThreadPoolExecutor(2) as ex:
-        bindings = [ex.submit(build_binding), ex.submit(build_binding, BINDING_OPS_SRC, BINDING_OPS)]
+    with cf.ThreadPoolExecutor(3) as ex:
+        bindings = [ex.submit(build_binding), ex.submit(build_binding, BINDING_OPS_SRC, BINDING_OPS),
+                    ex.submit(build_binding, BINDING_EXPERTS_SRC, BINDING_EXPERTS)]
         _build_into(LIB)
         build_probe()
         for b in bindings:
             b.result()
     if verbose:
-        print(f"built {LIB}, {BINDING}, {BINDING_OPS} and {PROBE_LIB}")
+        print(f"built {LIB}, {BINDING}, {BINDING_OPS}, {BINDING_EXPERTS} and {PROBE_LIB}")
     return LIB
 
 

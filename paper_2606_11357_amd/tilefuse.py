@@ -765,11 +765,49 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None
 # ---------------------------------------------------------------------------
 # 8-bit activations, and layers made of experts
 # ---------------------------------------------------------------------------
+_experts = None
+
+
+def _native_experts():
+    """The native module's calls of these operators (as for the norm, cache and
+    attention, _native_ops)."""
+    global _experts
+    if _experts is None:
+        torch = _torch()
+        lib = load()
+        names = ("quantize", "gemm", "route", "expert_gemm", "combine")
+        try:
+            from . import _tf_binding_experts as native
+        except ImportError as e:
+            _experts = dict.fromkeys(names, lambda *call: NotImplemented)
+            warnings.warn(f"the native binding does not load ({e}): calls of 8-bit layers and experts take some 5 us more "
+                          "on the host; build it with `python -m paper_2606_11357_amd.build`", RuntimeWarning, stacklevel=4)
+            return _experts
+        at = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value  # noqa: E731
+        native.bind(tuple(at(n) for n in ("tf_quantize_rows", "tf_w8a8_packed_bytes", "tf_w8a8_gemm", "tf_route_experts",
+                                          "tf_w8a8_expert_gemm", "tf_combine_experts")),
+                    torch._C._cuda_getCurrentRawStream)
+        _experts = {n: getattr(native, n) for n in names}
+    return _experts
+
+
+def _expert_call(name, where, *args):
+    """One native call: its result, NotImplemented (for the general path), or the
+    library's refusal raised."""
+    got = (_experts or _native_experts())[name](*args)
+    if type(got) is int:
+        _check(got, where)
+    return got
+
+
 def quantize_rows(x, gated=False, codes=None, scales=None):
     """Codes (int8 [M, N]) and scales (fp32 [M]) of the rows of a fp16 or bf16 [M, N]
     matrix: scale = max|row| / 127, codes = round(row * 127 / max|row|).  gated: x
     is [M, 2N] and the rows are silu(x[:, :N]) * x[:, N:].  Rows may be strided (by a
     multiple of 8 elements).  A row with a value that is not finite has the scale NaN."""
+    got = _expert_call("quantize", "tf_quantize_rows", x, gated, codes, scales)
+    if got is not NotImplemented:
+        return got
     torch = _torch()
     if not x.is_cuda:
         raise ValueError("tensors must be on the GPU (the library has no CPU path)")
@@ -843,6 +881,9 @@ def _product_out(out, dtype, device, shape):
 def w8a8_gemm(codes, scales, packed, K: int, N: int, dtype=None, out=None):
     """The product of int8 codes [M, K] with a scale a row (quantize_rows) and a packed
     weight (pack_w8a8): [M, N] of dtype (fp16 unless given, or bf16).  Sums are exact."""
+    got = _expert_call("gemm", "tf_w8a8_gemm", codes, scales, packed, K, N, dtype, out)
+    if got is not NotImplemented:
+        return got
     dtype, code = _codes_of(codes, scales, packed, K, N, 1, dtype if out is None else dtype or out.dtype)
     M = codes.shape[0]
     out = _product_out(out, dtype, codes.device, (M, N))
@@ -868,6 +909,14 @@ def route_experts(logits, top_k: int, *, bias=None, scoring="softmax", groups=1,
     largest ("max"); ties go to the lower index.  weights = score, divided by the sum
     of the chosen ones with renormalize, times scale.  An expert whose logit is
     -infinity or NaN comes last, with weight 0.  Returns a Routing."""
+    if scoring not in ("softmax", "sigmoid"):
+        raise ValueError("scoring must be softmax or sigmoid")
+    if group_score not in ("top2", "max"):
+        raise ValueError("group_score must be top2 or max")
+    by = int(scoring == "sigmoid"), groups, groups if top_groups is None else top_groups, int(group_score == "top2")
+    got = _expert_call("route", "tf_route_experts", logits, top_k, bias, *by, renormalize, scale)
+    if got is not NotImplemented:
+        return Routing(*got)
     torch = _torch()
     if not logits.is_cuda:
         raise ValueError("tensors must be on the GPU (the library has no CPU path)")
@@ -881,18 +930,13 @@ def route_experts(logits, top_k: int, *, bias=None, scoring="softmax", groups=1,
     if bias is not None:
         _need_cuda(bias)
         _same(bias, torch.float32, dev, (E,), "bias")
-    if scoring not in ("softmax", "sigmoid"):
-        raise ValueError("scoring must be softmax or sigmoid")
-    if group_score not in ("top2", "max"):
-        raise ValueError("group_score must be top2 or max")
     make = lambda n, dt=torch.int32: torch.empty(n, dtype=dt, device=dev)  # noqa: E731
     r = Routing(make((T, top_k), torch.float32), make((T, top_k)), make(E + 1), make(T * top_k), make((T, top_k)))
     if T == 0:
         r.offsets.zero_()
         return r
     _launch("tf_route_experts", dev, code, _ptr(logits), logits.stride(0) if T > 1 else E, _ptr(bias), T, E, top_k,
-            int(scoring == "sigmoid"), groups, groups if top_groups is None else top_groups,
-            int(group_score == "top2"), int(renormalize), scale, *(_ptr(t) for t in r))
+            *by, int(renormalize), scale, *(_ptr(t) for t in r))
     return r
 
 
@@ -902,6 +946,9 @@ def w8a8_expert_gemm(codes, scales, packed, K: int, N: int, offsets, rows=None, 
     of the codes times weight e.  Returns [slots, N] of dtype (fp16 unless given):
     rows that no expert has are not written, one whose row of the codes does not
     exist is zeros."""
+    got = _expert_call("expert_gemm", "tf_w8a8_expert_gemm", codes, scales, packed, K, N, offsets, rows, dtype, out)
+    if got is not NotImplemented:
+        return got
     torch = _torch()
     _need_cuda(offsets, rows)
     E = offsets.shape[0] - 1 if offsets.dim() == 1 else -1
@@ -928,6 +975,9 @@ def combine_experts(y, weights, places, add=None, out=None):
     """out[t] = add[t] + sum_j weights[t, j] * y[places[t, j]] for y [slots, N] (fp16 or
     bf16), weights fp32 and places int32 [T, top_k], add [T, N] or None; sums in fp32.
     A choice of weight 0 or of a place outside y adds nothing.  out may be add."""
+    got = _expert_call("combine", "tf_combine_experts", y, weights, places, add, out)
+    if got is not NotImplemented:
+        return got
     torch = _torch()
     _need_cuda(y, weights, places, add, out)
     code = _dtype_code(y.dtype, "y")
