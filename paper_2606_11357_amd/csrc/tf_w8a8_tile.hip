@@ -99,10 +99,17 @@ __device__ __forceinline__ u32x4 rows_swapped(const uint2& x, const uint2& y) {
     return u32x4{p[0], q[0], p[1], q[1]};
 }
 
-// Accumulators are pinned to AGPRs; mfma_hazard_gap() stands between their
-// initialisation and the first, and between the last and their first read.
+// Accumulators are pinned to AGPRs; the loop begins and ends with the wait states that
+// the matrix instructions need behind writes and before reads of them.
 __device__ __forceinline__ void mfma_i8(i32x4& acc, const u32x4& a, const u32x4& b) {
     asm("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+
+// Four accumulators as they are, taken apart only here (else the compiler moves and
+// spills single ones, at the loop's end already).
+__device__ __forceinline__ i32x4 whole(i32x4 acc) {
+    asm volatile("" : "+a"(acc));
+    return acc;
 }
 
 __device__ __forceinline__ void barrier_only() {
@@ -249,7 +256,6 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
 #pragma unroll
     for (int i = 0; i < (F::kAhead ? RB : RB - 1); ++i) af[0][i] = lds_read_block(a_lane[0], i);
     lds_wait();
-    mfma_hazard_gap();
 
     // Steps in turn, R to a pass of the loop (so that the ring has fixed places; steps
     // past K multiply zeros), S slots each of one matrix instruction (row block q / CB,
@@ -282,6 +288,7 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
             constexpr int kSets = F::kAhead ? 2 : 1;
             u32x4 (&now)[RB] = af[j % kSets];
             u32x4 (&nxt)[RB] = af[(j + 1) % kSets];
+            if (j == 0) asm volatile("s_nop 1");     // (after the accumulators' zeros)
 #pragma unroll
             for (int q = 0; q < S; ++q) {
                 const int i = q / CB, t = q % CB;
@@ -306,6 +313,8 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
                     else load_b(step + R - 1, o - F::kDma, ring[(j + R - 1) % R][o - F::kDma]);
                 }
             }
+            // what follows the loop may read the accumulators at once
+            if (j == R - 1) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1");
             if (!odd) barrier_after_loads<kLater < 63 ? kLater : 63>();
             else if (F::kOften) barrier_only();
         }
@@ -314,7 +323,6 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
     lds_wait();
 #pragma unroll
     for (int i = 0; i < RB; ++i) asm volatile("" ::"v"(af[0][i]), "v"(af[F::kAhead ? 1 : 0][i]));
-    mfma_hazard_gap();
     __builtin_amdgcn_s_waitcnt(0);       // the direct loads past the end have landed
     __syncthreads();                     // and no wave reads the buffers
     const Tile done = tile;
@@ -351,9 +359,9 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
 #pragma unroll
             for (int t = 0; t < CB; t += 2) {
                 const uint32_t off = here && to[t / 2] != kNowhere ? row + to[t / 2] : kNowhere;
-                const uint2 x = w8_scaled(bf, acc[i][t], sa, sw[t]);
+                const uint2 x = w8_scaled(bf, whole(acc[i][t]), sa, sw[t]);
                 if constexpr (CB > 1) {
-                    const uint2 y = w8_scaled(bf, acc[i][t + 1], sa, sw[t + 1]);
+                    const uint2 y = w8_scaled(bf, whole(acc[i][t + 1]), sa, sw[t + 1]);
                     store16(cr, rows_swapped(x, y), off);
                 } else {
                     store8(cr, x, off);
