@@ -1,5 +1,6 @@
 // C-ABI entry points of the 8-bit linear layers and the layers made of experts:
-// argument checks, always before any HIP call, and dispatch to the launchers.
+// argument checks, always before any HIP call, and dispatch to the launchers.  Sizes
+// are looked at before pointers: tensors without elements have none.
 #include "tf_route.h"
 #include "tf_w8a8.h"
 
@@ -29,12 +30,12 @@ extern "C" {
 
 int tf_quantize_rows(int dtype, const void* X, int64_t x_stride, int64_t M, int64_t N, int gated, int8_t* codes,
                      float* scales, void* stream) {
-    if (!X || !codes || !scales) return TF_ERR_NULL;
     if (bad_dtype(dtype)) return TF_ERR_ARG;
     if (M < 1 || M > TF_MAX_SLOTS || N <= 0 || N > TF_MAX_DIM || N % 16 != 0) return TF_ERR_SHAPE;
     if (x_stride < (gated ? 2 * N : N) || x_stride % 8 != 0 || x_stride > (int64_t(1) << 40)) return TF_ERR_SHAPE;
     if (too_many(M * (N <= 512 ? 64 : N <= 1024 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024) + 255))
         return TF_ERR_SHAPE;
+    if (!X || !codes || !scales) return TF_ERR_NULL;
     if (misaligned(X) || misaligned(codes) || misaligned(scales, 4)) return TF_ERR_ALIGN;
     return tf::launch_quantize_rows(dtype == TF_BF16, X, x_stride, M, N, gated != 0, codes, scales,
                                     static_cast<hipStream_t>(stream));
@@ -47,18 +48,18 @@ int64_t tf_w8a8_packed_bytes(int64_t K, int64_t N) {
 
 int tf_pack_w8a8(const int8_t* qweight, const void* scales, int scale_dtype, int64_t K, int64_t N, int64_t experts,
                  void* packed, void* stream) {
-    if (!qweight || !scales || !packed) return TF_ERR_NULL;
     if (bad_dtype(scale_dtype) && scale_dtype != TF_F32) return TF_ERR_ARG;
     if (bad_kn(K, N) || experts < 1 || experts > TF_MAX_EXPERTS) return TF_ERR_SHAPE;
+    if (!qweight || !scales || !packed) return TF_ERR_NULL;
     if (misaligned(qweight) || misaligned(scales) || misaligned(packed, 256)) return TF_ERR_ALIGN;
     return tf::launch_pack_w8a8(qweight, scales, scale_dtype, K, N, experts, packed, static_cast<hipStream_t>(stream));
 }
 
 int tf_w8a8_gemm(int dtype, const int8_t* A, const float* a_scales, const void* packed, void* C, int64_t M, int64_t K,
                  int64_t N, void* stream) {
-    if (!A || !a_scales || !packed || !C) return TF_ERR_NULL;
     if (bad_dtype(dtype)) return TF_ERR_ARG;
     if (bad_kn(K, N) || M < 1 || M > TF_MAX_M) return TF_ERR_SHAPE;
+    if (!A || !a_scales || !packed || !C) return TF_ERR_NULL;
     if (misaligned(A) || misaligned(C) || misaligned(packed, 256) || misaligned(a_scales, 4)) return TF_ERR_ALIGN;
     const tf::W8Layout L = tf::w8_layout(K, N);
     const tf::W8Args a{A, a_scales, static_cast<const uint8_t*>(packed), static_cast<uint16_t*>(C), nullptr, nullptr,
@@ -70,7 +71,6 @@ int tf_route_experts(int dtype, const void* logits, int64_t stride, const float*
                      int top_k, int scoring, int groups, int top_groups, int group_score, int renormalize, float scale,
                      float* weights, int32_t* chosen, int32_t* offsets, int32_t* tokens, int32_t* places,
                      void* stream) {
-    if (!logits || !weights || !chosen || !offsets || !tokens || !places) return TF_ERR_NULL;
     if ((bad_dtype(dtype) && dtype != TF_F32) || scoring < 0 || scoring > 1 || group_score < 0 || group_score > 1)
         return TF_ERR_ARG;
     if (!(scale > 0.f) || scale > 1e30f) return TF_ERR_ARG;
@@ -78,6 +78,7 @@ int tf_route_experts(int dtype, const void* logits, int64_t stride, const float*
     if (stride < experts || stride > (int64_t(1) << 40)) return TF_ERR_SHAPE;
     if (groups < 1 || groups > 64 || experts % groups != 0 || top_groups < 1 || top_groups > groups) return TF_ERR_SHAPE;
     if (top_k < 1 || top_k > TF_MAX_TOP_K || top_k > experts / groups * top_groups) return TF_ERR_SHAPE;
+    if (!logits || !weights || !chosen || !offsets || !tokens || !places) return TF_ERR_NULL;
     if (misaligned(logits, dtype == TF_F32 ? 4 : 2)) return TF_ERR_ALIGN;
     for (const void* p : {(const void*)bias, (const void*)weights, (const void*)chosen, (const void*)offsets,
                           (const void*)tokens, (const void*)places})
@@ -92,11 +93,11 @@ int tf_route_experts(int dtype, const void* logits, int64_t stride, const float*
 int tf_w8a8_expert_gemm(int dtype, const int8_t* A, const float* a_scales, int64_t a_rows, const void* packed,
                         const int32_t* offsets, const int32_t* rows, void* C, int64_t slots, int64_t K, int64_t N,
                         int64_t experts, void* stream) {
-    if (!A || !a_scales || !packed || !offsets || !C) return TF_ERR_NULL;
     if (bad_dtype(dtype)) return TF_ERR_ARG;
     if (bad_kn(K, N) || experts < 1 || experts > TF_MAX_EXPERTS) return TF_ERR_SHAPE;
     if (slots < 1 || slots > TF_MAX_SLOTS || a_rows < 1 || a_rows > TF_MAX_SLOTS) return TF_ERR_SHAPE;
     if (rows && a_rows * K >= 0xFFFFFF00ll) return TF_ERR_SHAPE;      // gathered rows have 32-bit offsets
+    if (!A || !a_scales || !packed || !offsets || !C) return TF_ERR_NULL;
     if (misaligned(A) || misaligned(C) || misaligned(packed, 256) || misaligned(a_scales, 4) ||
         misaligned(offsets, 4) || misaligned(rows, 4))
         return TF_ERR_ALIGN;
@@ -108,12 +109,12 @@ int tf_w8a8_expert_gemm(int dtype, const int8_t* A, const float* a_scales, int64
 
 int tf_combine_experts(int dtype, const void* Y, int64_t slots, const float* weights, const int32_t* places,
                        const void* add, int64_t T, int top_k, int64_t N, void* out, void* stream) {
-    if (!Y || !weights || !places || !out) return TF_ERR_NULL;
     if (bad_dtype(dtype)) return TF_ERR_ARG;
     if (T < 1 || T > TF_MAX_M || slots < 1 || slots > TF_MAX_SLOTS || N <= 0 || N > TF_MAX_DIM || N % 8 != 0 ||
         top_k < 1 || top_k > TF_MAX_TOP_K)
         return TF_ERR_SHAPE;
     if (too_many(T * (N / 8) + 255)) return TF_ERR_SHAPE;
+    if (!Y || !weights || !places || !out) return TF_ERR_NULL;
     for (const void* p : {Y, add, (const void*)out})
         if (misaligned(p)) return TF_ERR_ALIGN;
     if (misaligned(weights, 4) || misaligned(places, 4)) return TF_ERR_ALIGN;

@@ -1,8 +1,10 @@
-"""Decoder layers of the library's operators: 4-bit linear layers, norms with the
-residual sum, rotation and a 4-bit paged key/value cache, attention over prompts
-and over the cache.
+"""Decoder layers of the library's operators: linear layers of 4-bit weights, or of
+8-bit weights and activations, norms with the residual sum, rotation and a 4-bit
+paged key/value cache, attention over prompts and over the cache, and MLPs made of
+experts.
 
     python -m paper_2606_11357_amd.decoder [--layers 2 --prompt 2048 --batch 8 --steps 16]
+                                           [--eight-bit] [--experts 8 --top-k 2]
 
 runs a prompt for each sequence, then decode steps (one captured graph, replayed),
 on layers of the Llama-3-8B shape with random weights, and prints what each took.
@@ -17,6 +19,15 @@ A layer (pre-norm, as Llama's):
            | kv4_attention(q, cache)               single tokens
     n, r   = add_rms_norm(w4a16(o, W_o), r, w_mlp)
     x      = w4a16(silu_mul(w4a16(n, W_gate_up)), W_down)
+
+An 8-bit linear layer is w8a8_gemm(*quantize_rows(x), W), its MLP's second one takes
+quantize_rows(gate_up, gated=True).  An MLP made of experts:
+
+    c, s   = quantize_rows(n)
+    route  = route_experts(w8a8_gemm(c, s, W_router), top_k)
+    g      = w8a8_expert_gemm(c, s, W_gate_up, offsets, tokens)     every expert's tokens
+    y      = w8a8_expert_gemm(*quantize_rows(g, gated=True), W_down, offsets)
+    x      = combine_experts(y, weights, places)
 """
 from __future__ import annotations
 
@@ -37,6 +48,8 @@ class Config:
     group: int = 128
     eps: float = 1e-5
     theta: float = 500000.0
+    experts: int = 0             # the MLP's, 0: a dense one
+    top_k: int = 2
 
     @property
     def qkv(self):
@@ -58,18 +71,44 @@ def rotation(cfg: Config, positions: int, device="cuda"):
 
 class Layer:
     """One decoder layer.  weights: for each linear layer the AWQ tensors
-    (qweight, qzeros, scales), packed here once, and the norm weights "norm_in"
-    and "norm_mlp"; the scales' type (fp16 or bf16) is the layer's."""
+    (qweight, qzeros, scales) or, for 8-bit activations, int8 weights and their
+    columns' scales (qweight, scales), packed here once, and the norm weights
+    "norm_in" and "norm_mlp", whose type (fp16 or bf16) is the layer's.  With
+    cfg.experts, "gate_up" and "down" are int8 [experts, K, N] with scales
+    [experts, N], and "router" int8 [hidden, experts] with its scales."""
 
     def __init__(self, cfg: Config, weights: dict):
         self.cfg = cfg
-        self.packed = {n: tf.pack_w4(*weights[n], K, N, cfg.group) for n, (K, N) in cfg.linears().items()}
+        self.eight_bit = {n for n in cfg.linears() if len(weights[n]) == 2}
+        if cfg.experts:
+            if not {"gate_up", "down"} <= self.eight_bit:
+                raise ValueError("experts' weights are int8 with a scale a column")
+            self.router = tf.pack_w8a8(*weights["router"])
+        self.packed = {n: tf.pack_w8a8(*weights[n]) if n in self.eight_bit else tf.pack_w4(*weights[n], K, N, cfg.group)
+                       for n, (K, N) in cfg.linears().items()}
         self.norm_in, self.norm_mlp = weights["norm_in"], weights["norm_mlp"]
 
-    def _linear(self, name, x):
+    def _linear(self, name, x, gated=False):
         K, N = self.cfg.linears()[name]
+        if name in self.eight_bit:
+            return tf.w8a8_gemm(*tf.quantize_rows(x, gated=gated), self.packed[name], K, N, dtype=x.dtype)
+        if gated:
+            x = tf.silu_mul(x)
         f = tf.w4a16_gemv if x.shape[0] == 1 else tf.w4a16_gemm
         return f(x, self.packed[name], K, N, self.cfg.group)
+
+    def _mlp(self, n):
+        c = self.cfg
+        if not c.experts:
+            return self._linear("down", self._linear("gate_up", n), gated=True)
+        codes, scales = tf.quantize_rows(n)
+        logits = tf.w8a8_gemm(codes, scales, self.router, c.hidden, c.experts, dtype=n.dtype)
+        route = tf.route_experts(logits, c.top_k, renormalize=True)
+        g = tf.w8a8_expert_gemm(codes, scales, self.packed["gate_up"], *c.linears()["gate_up"], route.offsets,
+                                route.tokens, dtype=n.dtype)
+        y = tf.w8a8_expert_gemm(*tf.quantize_rows(g, gated=True), self.packed["down"], *c.linears()["down"],
+                                route.offsets, dtype=n.dtype)
+        return tf.combine_experts(y, route.weights, route.places)
 
     def __call__(self, x, residual, cache, table, cu, starts, cos, sin, lens=None, prefix=None):
         """x, residual: [tokens, hidden] (residual None before the first layer), the
@@ -95,7 +134,7 @@ class Layer:
             cu_k, first, keys = prefix
             o = tf.prompt_attention(q, *tf.kv4_read(cache, table, cu_k, first, keys), cu, cu_k)
         n, residual = tf.add_rms_norm(self._linear("o", o.view(T, -1)), residual, self.norm_mlp, eps=c.eps)
-        return self._linear("down", tf.silu_mul(self._linear("gate_up", n))), residual
+        return self._mlp(n), residual
 
 
 class Stack:
@@ -114,15 +153,30 @@ class Stack:
         return tf.add_rms_norm(x, residual, self.final_norm, eps=self.cfg.eps)[0]
 
 
-def random_weights(cfg: Config, dtype, seed: int, device="cuda") -> dict:
-    """Random AWQ tensors of a layer; scales that keep its outputs near those of a
-    trained one (each linear layer's output of the size of its input)."""
+def random_weights(cfg: Config, dtype, seed: int, device="cuda", eight_bit=False) -> dict:
+    """Random weights of a layer (4-bit AWQ tensors, or int8 with a scale a column;
+    experts' are int8); scales that keep its outputs near those of a trained one (each
+    linear layer's output of the size of its input)."""
     import torch
     gen = torch.Generator(device=device)
     gen.manual_seed(seed)
     word = lambda *shape: torch.randint(-2 ** 31, 2 ** 31, shape, dtype=torch.int32, device=device, generator=gen)  # noqa: E731
     w = {}
+
+    def int8(*shape):
+        q = torch.randint(-127, 128, shape, dtype=torch.int8, device=device, generator=gen)
+        s = (1 + torch.rand((*shape[:-2], shape[-1]), device=device, generator=gen)) / (110 * shape[-2] ** 0.5)
+        return q, s.to(dtype)
+
+    if cfg.experts:
+        w["router"] = int8(cfg.hidden, cfg.experts)
     for name, (K, N) in cfg.linears().items():
+        if cfg.experts and name in ("gate_up", "down"):
+            w[name] = int8(cfg.experts, K, N)
+            continue
+        if eight_bit:
+            w[name] = int8(K, N)
+            continue
         step = (12 * K) ** -0.5 / 3         # codes minus zero-points spread over about 6.5 of 16 steps
         s = step * (1 + torch.rand((K // cfg.group, N), device=device, generator=gen))
         w[name] = (word(K, N // 8), word(K // cfg.group, N // 8), s.to(dtype))
@@ -141,10 +195,13 @@ def main(argv=None):
     ap.add_argument("--batch", type=int, default=8, help="sequences")
     ap.add_argument("--steps", type=int, default=16, help="decode steps")
     ap.add_argument("--dtype", choices=("f16", "bf16"), default="bf16")
+    ap.add_argument("--eight-bit", action="store_true", help="8-bit weights and activations in the linear layers")
+    ap.add_argument("--experts", type=int, default=0, help="experts of an MLP (a multiple of 8; 0: a dense MLP)")
+    ap.add_argument("--top-k", type=int, default=2, help="experts of a token")
     a = ap.parse_args(argv)
-    cfg, page = Config(), 64
+    cfg, page = Config(experts=a.experts, top_k=a.top_k), 64
     dtype = torch.float16 if a.dtype == "f16" else torch.bfloat16
-    layers = [Layer(cfg, random_weights(cfg, dtype, i)) for i in range(a.layers)]
+    layers = [Layer(cfg, random_weights(cfg, dtype, i, eight_bit=a.eight_bit)) for i in range(a.layers)]
     per_seq = -(-(a.prompt + a.steps + 1) // page)
     ones = torch.ones(cfg.hidden, device="cuda", dtype=dtype)
     stack = Stack(layers, ones, a.batch * per_seq, page, a.prompt + a.steps + 1, dtype)
