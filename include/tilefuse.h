@@ -448,9 +448,15 @@ int64_t tf_w8a8_packed_bytes(int64_t K, int64_t N);
 int tf_pack_w8a8(const int8_t* qweight, const void* scales, int scale_dtype, int64_t K, int64_t N, int64_t experts,
                  void* packed, void* stream);
 
-/* C [M, N] = the product above of codes A [M, K], their scales and a packed weight. */
+/*
+ * C [M, N] = the product above of codes A [M, K], their scales and a packed weight.
+ * workspace: NULL, or at least tf_w8a8_workspace_bytes(...) bytes (may be 0), 16-byte
+ * aligned, no initial value: few rows by few columns are then split over K too.  The
+ * result is the same bit for bit.  Calls that may run concurrently must not share one.
+ */
+int64_t tf_w8a8_workspace_bytes(int64_t M, int64_t K, int64_t N);
 int tf_w8a8_gemm(int dtype, const int8_t* A, const float* a_scales, const void* packed, void* C, int64_t M, int64_t K,
-                 int64_t N, void* stream);
+                 int64_t N, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The choice of experts for each of T tokens and the order in which their

@@ -39,31 +39,40 @@ bool is(const at::Tensor* t, at::ScalarType type, int dev, at::IntArrayRef shape
 struct Fns {
     decltype(&tf_quantize_rows) quantize;
     decltype(&tf_w8a8_packed_bytes) packed_bytes;
+    decltype(&tf_w8a8_workspace_bytes) workspace_bytes;
     decltype(&tf_w8a8_gemm) gemm;
     decltype(&tf_route_experts) route;
     decltype(&tf_w8a8_expert_gemm) expert_gemm;
     decltype(&tf_combine_experts) combine;
+    tf_binding::CaptureFn capture;
 } g_fns;
-PyObject* g_stream;
+PyObject *g_stream, *g_workspaces, *g_make_workspace, *g_name_device;
 
-// bind((addresses in the order of Fns), current stream function)
+// bind((addresses in the order of Fns), current stream function, workspaces of
+//          gemm, function (device, bytes) that makes one)
 PyObject* bind(PyObject*, PyObject* args) {
-    PyObject *fns, *stream;
-    if (!PyArg_ParseTuple(args, "O!O", &PyTuple_Type, &fns, &stream)) return nullptr;
-    unsigned long long at[6];
-    if (PyTuple_GET_SIZE(fns) != 6) {
-        PyErr_SetString(PyExc_ValueError, "bind needs six functions");
+    PyObject *fns, *stream, *cached, *make;
+    if (!PyArg_ParseTuple(args, "O!OO!O", &PyTuple_Type, &fns, &stream, &PyDict_Type, &cached, &make)) return nullptr;
+    unsigned long long at[8];
+    if (PyTuple_GET_SIZE(fns) != 8) {
+        PyErr_SetString(PyExc_ValueError, "bind needs eight functions");
         return nullptr;
     }
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < 8; ++i) {
         at[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(fns, i));
         if (PyErr_Occurred()) return nullptr;
     }
-    g_fns = {reinterpret_cast<decltype(Fns::quantize)>(at[0]), reinterpret_cast<decltype(Fns::packed_bytes)>(at[1]),
-             reinterpret_cast<decltype(Fns::gemm)>(at[2]),     reinterpret_cast<decltype(Fns::route)>(at[3]),
-             reinterpret_cast<decltype(Fns::expert_gemm)>(at[4]),
-             reinterpret_cast<decltype(Fns::combine)>(at[5])};
+    g_fns = {reinterpret_cast<decltype(Fns::quantize)>(at[0]),
+             reinterpret_cast<decltype(Fns::packed_bytes)>(at[1]),
+             reinterpret_cast<decltype(Fns::workspace_bytes)>(at[2]),
+             reinterpret_cast<decltype(Fns::gemm)>(at[3]),
+             reinterpret_cast<decltype(Fns::route)>(at[4]),
+             reinterpret_cast<decltype(Fns::expert_gemm)>(at[5]),
+             reinterpret_cast<decltype(Fns::combine)>(at[6]),
+             reinterpret_cast<tf_binding::CaptureFn>(at[7])};
     Py_XSETREF(g_stream, Py_NewRef(stream));
+    Py_XSETREF(g_workspaces, Py_NewRef(cached));
+    Py_XSETREF(g_make_workspace, Py_NewRef(make));
     Py_RETURN_NONE;
 }
 
@@ -143,10 +152,10 @@ struct Operands {
     }
 };
 
-// gemm(codes, scales, packed, K, N, dtype, out)
+// gemm(codes, scales, packed, K, N, dtype, out, workspace)
 PyObject* gemm_common(PyObject* const* a, Py_ssize_t n) {
     Operands op;
-    if (n != 7 || !g_fns.gemm || !op.read(a, 1)) return not_here();
+    if (n != 8 || !g_fns.gemm || !op.read(a, 1)) return not_here();
     const at::Tensor* out = a[6] == Py_None ? nullptr : plain(a[6]);
     at::ScalarType type;
     if ((a[6] != Py_None && !out) || !output_type(a[5], out, type)) return not_here();
@@ -154,6 +163,29 @@ PyObject* gemm_common(PyObject* const* a, Py_ssize_t n) {
     if (out && !is(out, type, op.dev, mat)) return not_here();
     void* stream;
     if (!tf_binding::stream_of(g_stream, op.dev, stream)) return PyErr_Occurred() ? nullptr : not_here();
+    // the workspace: False none, None the stream's cached one, or the caller's
+    Held held;
+    const at::Tensor* ws = nullptr;
+    if (a[7] == Py_None) {
+        const int64_t need = g_fns.workspace_bytes(op.M, op.K, op.N);
+        if (need < 0) return not_here();
+        if (need > 0) {
+            if (!tf_binding::find_workspace(g_workspaces, g_fns.capture, op.dev, stream, held))
+                return PyErr_Occurred() ? nullptr : not_here();
+            ws = held.o ? plain(held.o) : nullptr;
+            if (!ws || (int64_t)ws->nbytes() < need) {
+                const Held device{PyObject_GetAttr(a[0], g_name_device)};
+                if (!device.o) return nullptr;
+                Py_XSETREF(held.o, PyObject_CallFunction(g_make_workspace, "OL", device.o, (long long)need));
+                if (!held.o) return nullptr;
+                if (!(ws = plain(held.o))) return not_here();
+            }
+        }
+    } else if (a[7] != Py_False) {
+        if (!(ws = plain(a[7])) || ws->get_device() != op.dev) return not_here();
+    }
+    void* wsp = ws ? ws->data_ptr() : nullptr;
+    const size_t ws_bytes = ws ? ws->nbytes() : 0;
     at::Tensor made;
     if (!out) made = make(mat, type, *op.codes);
     void* c = out ? out->data_ptr() : made.data_ptr();
@@ -162,7 +194,7 @@ PyObject* gemm_common(PyObject* const* a, Py_ssize_t n) {
     const void* w = op.packed->data_ptr();
     int rc;
     Py_BEGIN_ALLOW_THREADS;
-    rc = g_fns.gemm(code16(type), q, s, w, c, op.M, op.K, op.N, stream);
+    rc = g_fns.gemm(code16(type), q, s, w, c, op.M, op.K, op.N, wsp, ws_bytes, stream);
     Py_END_ALLOW_THREADS;
     if (rc != 0) return PyLong_FromLong(rc);
     return out ? Py_NewRef(a[6]) : THPVariable_Wrap(std::move(made));
@@ -314,4 +346,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tf_binding_experts", nullptr, -1,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tf_binding_experts() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__tf_binding_experts() {
+    g_name_device = PyUnicode_InternFromString("device");
+    return g_name_device ? PyModule_Create(&module) : nullptr;
+}

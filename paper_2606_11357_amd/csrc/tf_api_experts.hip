@@ -9,7 +9,8 @@ int launch_quantize_rows(bool bf, const void* x, int64_t stride, int64_t M, int6
                          float* scale, hipStream_t s);
 int launch_pack_w8a8(const int8_t* w, const void* scales, int scale_dtype, int64_t K, int64_t N, int64_t experts,
                      void* packed, hipStream_t s);
-int launch_w8a8(const W8Args& a, hipStream_t s);
+int launch_w8a8(W8Args a, void* ws, int64_t ws_bytes, hipStream_t s);
+int64_t w8a8_workspace_bytes(int64_t M, int64_t K, int64_t N);
 int launch_route_experts(const RouteArgs& a, int32_t* offsets, int32_t* tokens, int32_t* places, hipStream_t s);
 int launch_combine_experts(const CombineArgs& a, bool bf, hipStream_t s);
 }  // namespace tf
@@ -55,16 +56,23 @@ int tf_pack_w8a8(const int8_t* qweight, const void* scales, int scale_dtype, int
     return tf::launch_pack_w8a8(qweight, scales, scale_dtype, K, N, experts, packed, static_cast<hipStream_t>(stream));
 }
 
+int64_t tf_w8a8_workspace_bytes(int64_t M, int64_t K, int64_t N) {
+    if (bad_kn(K, N) || M < 1 || M > TF_MAX_M) return TF_ERR_SHAPE;
+    return tf::w8a8_workspace_bytes(M, K, N);
+}
+
 int tf_w8a8_gemm(int dtype, const int8_t* A, const float* a_scales, const void* packed, void* C, int64_t M, int64_t K,
-                 int64_t N, void* stream) {
+                 int64_t N, void* workspace, size_t workspace_bytes, void* stream) {
     if (bad_dtype(dtype)) return TF_ERR_ARG;
     if (bad_kn(K, N) || M < 1 || M > TF_MAX_M) return TF_ERR_SHAPE;
     if (!A || !a_scales || !packed || !C) return TF_ERR_NULL;
-    if (misaligned(A) || misaligned(C) || misaligned(packed, 256) || misaligned(a_scales, 4)) return TF_ERR_ALIGN;
+    if (workspace && (int64_t)workspace_bytes < tf::w8a8_workspace_bytes(M, K, N)) return TF_ERR_ARG;
+    if (misaligned(A) || misaligned(C) || misaligned(packed, 256) || misaligned(a_scales, 4) || misaligned(workspace))
+        return TF_ERR_ALIGN;
     const tf::W8Layout L = tf::w8_layout(K, N);
     const tf::W8Args a{A, a_scales, static_cast<const uint8_t*>(packed), static_cast<uint16_t*>(C), nullptr, nullptr,
-                       M, M, K, N, L.total, L.s_off, (int)L.na, (int)L.np, 0, dtype == TF_BF16};
-    return tf::launch_w8a8(a, static_cast<hipStream_t>(stream));
+                       M, M, K, N, L.total, L.s_off, (int)L.na, (int)L.np, 0, dtype == TF_BF16, 1, nullptr};
+    return tf::launch_w8a8(a, workspace, (int64_t)workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 int tf_route_experts(int dtype, const void* logits, int64_t stride, const float* bias, int64_t T, int experts,
@@ -103,8 +111,8 @@ int tf_w8a8_expert_gemm(int dtype, const int8_t* A, const float* a_scales, int64
         return TF_ERR_ALIGN;
     const tf::W8Layout L = tf::w8_layout(K, N);
     const tf::W8Args a{A, a_scales, static_cast<const uint8_t*>(packed), static_cast<uint16_t*>(C), offsets, rows,
-                       slots, a_rows, K, N, L.total, L.s_off, (int)L.na, (int)L.np, (int)experts, dtype == TF_BF16};
-    return tf::launch_w8a8(a, static_cast<hipStream_t>(stream));
+                       slots, a_rows, K, N, L.total, L.s_off, (int)L.na, (int)L.np, (int)experts, dtype == TF_BF16, 1, nullptr};
+    return tf::launch_w8a8(a, nullptr, 0, static_cast<hipStream_t>(stream));
 }
 
 int tf_combine_experts(int dtype, const void* Y, int64_t slots, const float* weights, const int32_t* places,

@@ -210,25 +210,36 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int32_t* __res
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t run = (S + 256 * kPlanWaves - 1) / (256 * kPlanWaves) * 256;
     const int64_t i0 = min(S, wave * run), i1 = min(S, i0 + run);
-    auto load = [&](int64_t i, int (&c)[4]) {        // choices i + 4 lane .. + 3, those past the end E
-        const int64_t at = i + 4 * lane;
-        if (at + 4 <= i1 && (reinterpret_cast<uintptr_t>(chosen) & 15) == 0) {
-            const int4 v = *reinterpret_cast<const int4*>(chosen + at);
-            c[0] = v.x, c[1] = v.y, c[2] = v.z, c[3] = v.w;
-        } else {
+    // choices i + 256 b + 4 lane .. + 3 of kAtOnce blocks b, those past the end E
+    constexpr int kAtOnce = 4;
+    const bool whole = (reinterpret_cast<uintptr_t>(chosen) & 15) == 0;
+    auto load = [&](int64_t i, int (&c)[kAtOnce][4]) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) c[u] = at + u < i1 ? chosen[at + u] : E;
+        for (int b = 0; b < kAtOnce; ++b) {
+            const int64_t at = i + 256 * b + 4 * lane;
+            int4 v{E, E, E, E};
+            if (whole && at + 4 <= i1) {
+                v = *reinterpret_cast<const int4*>(chosen + at);
+            } else {
+                if (at < i1) v.x = chosen[at];
+                if (at + 1 < i1) v.y = chosen[at + 1];
+                if (at + 2 < i1) v.z = chosen[at + 2];
+                if (at + 3 < i1) v.w = chosen[at + 3];
+            }
+            c[b][0] = v.x, c[b][1] = v.y, c[b][2] = v.z, c[b][3] = v.w;
         }
     };
     int lower = 0, mine = 0;
-    for (int64_t i = i0; i < i1; i += 256) {
-        int c[4];
+    for (int64_t i = i0; i < i1; i += 256 * kAtOnce) {
+        int c[kAtOnce][4];
         load(i, c);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            lower += __builtin_popcountll(__ballot(c[u] < e));
-            mine += __builtin_popcountll(__ballot(c[u] == e));
-        }
+        for (int b = 0; b < kAtOnce; ++b)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                lower += __builtin_popcountll(__ballot(c[b][u] < e));
+                mine += __builtin_popcountll(__ballot(c[b][u] == e));
+            }
     }
     if (lane == 0) before[wave] = lower, own[wave] = mine;
     __syncthreads();
@@ -244,23 +255,28 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int32_t* __res
     }
     if (!mine) return;
     at += first;
-    for (int64_t i = i0; i < i1; i += 256) {
-        int c[4], slot = at;
+    for (int64_t i = i0; i < i1; i += 256 * kAtOnce) {
+        int c[kAtOnce][4];
         load(i, c);
-        bool is[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            is[u] = c[u] == e;
-            const uint64_t who = __ballot(is[u]);
-            slot += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
-            at += __builtin_popcountll(who);
-        }
+        for (int b = 0; b < kAtOnce; ++b) {
+            int slot = at;
+            uint64_t any = 0;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (!is[u]) continue;
-            const int64_t j = i + 4 * lane + u;
-            tokens[slot] = per_k ? (int)__umulhi((uint32_t)j, per_k) : (int)j;
-            places[j] = slot++;
+            for (int u = 0; u < 4; ++u) {
+                const uint64_t who = __ballot(c[b][u] == e);
+                slot += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                at += __builtin_popcountll(who);
+                any |= who;
+            }
+            if (!any) continue;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (c[b][u] != e) continue;
+                const int64_t j = i + 256 * b + 4 * lane + u;
+                tokens[slot] = per_k ? (int)__umulhi((uint32_t)j, per_k) : (int)j;
+                places[j] = slot++;
+            }
         }
     }
 }

@@ -36,6 +36,10 @@ struct W8Args {
     int64_t K, N, total, s_off;
     int na, np, experts;
     int bf;                  // C is bfloat16
+    // K in parts, the sums of each in parts[part][M][N], added and scaled by a launch of
+    // their own; 1: none
+    int splits;
+    int32_t* parts;
 };
 
 #ifdef __HIPCC__

@@ -35,6 +35,7 @@ struct Form {
     static constexpr int kDma = RB / 4;                      // direct loads of a wave and step
     static constexpr int kSlots = RB * CB;                   // matrix instructions of a wave and step
     static constexpr bool kAhead = kSlots <= 8;              // two sets of fragments
+    static constexpr bool kSplits = kSlots <= 4;             // the form that K is split for
     static constexpr bool kOften = kSlots >= 64;             // a barrier every step: see the loop
     static constexpr int kRowGroup = 2048 / BM;              // row tiles that share the columns' order
     static_assert((P & (P - 1)) == 0 && R % 4 == 0, "buffers by a mask, whole pairs a pass of the loop");
@@ -141,6 +142,7 @@ struct Tile {
     const uint8_t* packed;
     int64_t row0, col0;
     int rows;
+    int from, steps, part;   // where K is split: the part's steps
 };
 
 // Tile number `at` of row tiles x column tiles, rows in groups of kRowGroup.
@@ -154,23 +156,24 @@ __device__ __forceinline__ void tile_of(int at, int tiles_m, int tiles_n, int& t
 
 // Tiles next(0), next(1), ... (false: no more).  The loads that a tile begins with are
 // issued before the outputs of the one before are scaled and stored.
-template <class F, bool GATHER, class Next>
+template <class F, bool GATHER, bool SPLIT, class Next>
 __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile, TileShared<F>& sm) {
     constexpr int RB = F::RB, CB = F::CB, P = F::P, R = F::R, S = F::kSlots;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kg = lane >> 4;
-    const int steps = a.na, pairs = steps / 2;
+    const int pairs = a.na / 2;
+    int from = 0, steps = a.na;                       // this tile's steps of K
 
     __amdgpu_buffer_rsrc_t ar, wr[CB];
     uint32_t avoff[RB / 2];
     float row_scale = 0.f, column_scale = 0.f;
     // Direct load r of wave w fills rows 4 RB w + 8 r .. + 7 of a buffer, eight lanes a row.
     auto dma_a = [&](int pair, int buf, int r) {
-        dma16(ar, sm.a + buf * F::kPairBytes + (RB / 2 * wave + r) * 1024, avoff[r] + (uint32_t)min(pair, pairs - 1) * 128u);
+        dma16(ar, sm.a + buf * F::kPairBytes + (RB / 2 * wave + r) * 1024, avoff[r] + (uint32_t)min(from / 2 + pair, pairs - 1) * 128u);
     };
     u32x4 ring[R][CB];
-    auto load_b = [&](int step, int t, u32x4& v) { v = load16(wr[t], (uint32_t)(lane * 16 + step * kW8AtomBytes)); };
+    auto load_b = [&](int step, int t, u32x4& v) { v = load16(wr[t], (uint32_t)(lane * 16 + (from + step) * kW8AtomBytes)); };
 
     constexpr int kOps = F::kDma + CB;                // vector-memory operations of a wave and step
     constexpr int kHalf0 = F::kOften ? 2 * P - 2 : 2 * P - 3;      // half of a pair that step 0 brings
@@ -212,6 +215,10 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
             const int64_t n = t.col0 + tid;
             column_scale = reinterpret_cast<const float*>(t.packed + a.s_off)[n < a.np * 16 ? n : 0];
         }
+        if constexpr (SPLIT) {
+            from = t.from;
+            steps = t.steps;
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int h = 0; h < kBefore; ++h)
@@ -238,7 +245,7 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
     Tile tile;
     if (!next_tile(0, tile)) return;
     begin(tile);
-    constexpr int kStores = RB * CB / 2;              // of a wave and tile
+    constexpr int kStores = SPLIT ? RB * CB : CB > 1 ? RB * CB / 2 : RB;      // of a wave and tile
     for (int turn = 0;; ++turn) {
     i32x4 acc[RB][CB];
 #pragma unroll
@@ -333,7 +340,24 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
     // rows of 16 lanes swapped between blocks t and t + 1 make that eight columns a lane,
     // 64 bytes of a row of C a store.  Rows and columns past the end have offsets that the
     // buffer drops: the number of stores is the same for every tile.
-    {
+    if constexpr (SPLIT) {
+        const int lane = again(threadIdx.x & 63), c = lane & 15, kg = lane >> 4;
+        const __amdgpu_buffer_rsrc_t pr = make_rsrc(a.parts + (done.part * a.M + done.row0) * a.N,
+                                                    (uint32_t)done.rows * (uint32_t)a.N * 4u);
+        const int64_t n0 = done.col0 + 16 * CB * wave + 4 * kg;
+        uint32_t row = ((uint32_t)c * (uint32_t)a.N + (uint32_t)n0) * 4u, sixteen = 64u * (uint32_t)a.N;
+        int left = done.rows;
+#pragma unroll
+        for (int i = 0; i < RB; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < CB; ++t)
+                store16(pr, __builtin_bit_cast(u32x4, whole(acc[i][t])),
+                        c < left && n0 + 16 * t < a.N ? row + 64u * t : kNowhere);
+            row += sixteen;
+            left -= 16;
+        }
+    } else {
     const int lane = again(threadIdx.x & 63), c = lane & 15, kg = lane >> 4;
     const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.C + done.row0 * a.N, (uint32_t)done.rows * (uint32_t)a.N * 2u);
     const float* sr = sm.rows[turn & 1];
@@ -386,12 +410,19 @@ __device__ __forceinline__ int place_of(int b, int grid, int k, int total) {
     return i < per + (x < rem ? 1 : 0) ? x * per + min(x, rem) + i : -1;
 }
 
-template <class F>
+template <class F, bool SPLIT>
 __global__ __launch_bounds__(kThreads, F::WGS) void w8a8_tile_kernel(W8Args a, int tiles_m, int tiles_n) {
     __shared__ __align__(16) TileShared<F> sm;
     auto next_tile = [&](int k, Tile& t) {
-        const int at = place_of(blockIdx.x, gridDim.x, k, tiles_m * tiles_n);
+        int at = place_of(blockIdx.x, gridDim.x, k, tiles_m * tiles_n * (SPLIT ? a.splits : 1));
         if (at < 0) return false;
+        if constexpr (SPLIT) {                        // parts of whole passes of the loop
+            const int passes = (a.na + F::R - 1) / F::R;
+            t.part = __builtin_amdgcn_readfirstlane(at % a.splits);
+            t.from = passes * t.part / a.splits * F::R;
+            t.steps = passes * (t.part + 1) / a.splits * F::R - t.from;
+            at /= a.splits;
+        }
         int tm, tn;
         tile_of<F>(at, tiles_m, tiles_n, tm, tn);
         t.packed = a.packed;
@@ -400,7 +431,26 @@ __global__ __launch_bounds__(kThreads, F::WGS) void w8a8_tile_kernel(W8Args a, i
         t.rows = (int)min((int64_t)F::BM, a.M - t.row0);
         return true;
     };
-    tile_products<F, false>(a, next_tile, sm);
+    tile_products<F, false, SPLIT>(a, next_tile, sm);
+}
+
+// The parts' sums added, scaled and rounded: eight columns of a row a thread.
+__global__ __launch_bounds__(256) void w8a8_join_kernel(W8Args a) {
+    const int per_row = (int)(a.N / 8);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.M * per_row) return;
+    const int64_t m = i / per_row, n = (i - m * per_row) * 8;
+    const i32x4* p = reinterpret_cast<const i32x4*>(a.parts + m * a.N + n);
+    i32x4 lo = p[0], hi = p[1];
+    for (int s = 1; s < a.splits; ++s) {
+        p += a.M * a.N / 4;
+        lo += p[0];
+        hi += p[1];
+    }
+    const float4_t* sw = reinterpret_cast<const float4_t*>(a.packed + a.s_off + n * 4);
+    const float sa = a.a_scale[m];
+    const uint2 x = w8_scaled(a.bf, lo, sa, sw[0]), y = w8_scaled(a.bf, hi, sa, sw[1]);
+    *reinterpret_cast<u32x4*>(a.C + m * a.N + n) = u32x4{x.x, x.y, y.x, y.y};
 }
 
 // By expert: the row tiles of all experts in one list, found from the offsets by
@@ -476,7 +526,7 @@ __global__ __launch_bounds__(kThreads, F::WGS) void w8a8_tile_experts_kernel(W8A
         t.col0 = (int64_t)__builtin_amdgcn_readfirstlane(tn) * F::BN;
         return true;                                  // (barriers follow before the next call)
     };
-    tile_products<F, GATHER>(a, next_tile, sm);
+    tile_products<F, GATHER, false>(a, next_tile, sm);
 }
 
 template <class F>
@@ -486,8 +536,15 @@ int launch_form(const W8Args& a, hipStream_t s) {
                                       : (a.M + F::BM - 1) / F::BM;
     // as many workgroups as run at a time, whole eights
     const int64_t most = (int64_t)device_cus(s) * F::WGS;
-    const dim3 grid((unsigned)((std::min(tiles_m * tiles_n, most) + kXcds - 1) / kXcds * kXcds));
-    if (!a.experts) return launch(w8a8_tile_kernel<F>, grid, dim3(kThreads), 0, s, a, (int)tiles_m, (int)tiles_n);
+    const dim3 grid((unsigned)((std::min(tiles_m * tiles_n * a.splits, most) + kXcds - 1) / kXcds * kXcds));
+    if constexpr (F::kSplits) {
+        if (a.splits > 1) {
+            const int rc = launch(w8a8_tile_kernel<F, true>, grid, dim3(kThreads), 0, s, a, (int)tiles_m, (int)tiles_n);
+            if (rc) return rc;
+            return launch(w8a8_join_kernel, dim3((unsigned)((a.M * (a.N / 8) + 255) / 256)), dim3(256), 0, s, a);
+        }
+    }
+    if (!a.experts) return launch(w8a8_tile_kernel<F, false>, grid, dim3(kThreads), 0, s, a, (int)tiles_m, (int)tiles_n);
     return a.rows ? launch(w8a8_tile_experts_kernel<F, true>, grid, dim3(kThreads), 0, s, a, (int)tiles_n)
                   : launch(w8a8_tile_experts_kernel<F, false>, grid, dim3(kThreads), 0, s, a, (int)tiles_n);
 }

@@ -37,8 +37,8 @@ EXPORTS = (
     "tf_w8a16_gemv_bf16", "tf_unpack", "tf_dequant", "tf_silu_mul", "tf_silu_mul_bf16",
     "tf_add_rms_norm", "tf_kv4_cache_bytes", "tf_kv4_append", "tf_kv4_read",
     "tf_kv4_attention_workspace_bytes", "tf_kv4_attention", "tf_prompt_attention_workspace_bytes",
-    "tf_prompt_attention", "tf_quantize_rows", "tf_w8a8_packed_bytes", "tf_pack_w8a8", "tf_w8a8_gemm",
-    "tf_route_experts", "tf_w8a8_expert_gemm", "tf_combine_experts",
+    "tf_prompt_attention", "tf_quantize_rows", "tf_w8a8_packed_bytes", "tf_pack_w8a8", "tf_w8a8_workspace_bytes",
+    "tf_w8a8_gemm",     "tf_route_experts", "tf_w8a8_expert_gemm", "tf_combine_experts",
 )
 
 
@@ -102,7 +102,8 @@ def load() -> ctypes.CDLL:
         "tf_quantize_rows": (I, [I, P, I64, I64, I64, I, P, P, P]),
         "tf_w8a8_packed_bytes": (I64, [I64, I64]),
         "tf_pack_w8a8": (I, [P, P, I, I64, I64, I64, P, P]),
-        "tf_w8a8_gemm": (I, [I, P, P, P, P, I64, I64, I64, P]),
+        "tf_w8a8_workspace_bytes": (I64, [I64, I64, I64]),
+        "tf_w8a8_gemm": (I, [I, P, P, P, P, I64, I64, I64, P, SZ, P]),
         "tf_route_experts": (I, [I, P, I64, P, I64, I, I, I, I, I, I, I, F, P, P, P, P, P, P]),
         "tf_w8a8_expert_gemm": (I, [I, P, P, I64, P, P, P, P, I64, I64, I64, I64, P]),
         "tf_combine_experts": (I, [I, P, I64, P, P, P, I64, I, I64, P, P]),
@@ -784,9 +785,10 @@ def _native_experts():
                           "on the host; build it with `python -m paper_2606_11357_amd.build`", RuntimeWarning, stacklevel=4)
             return _experts
         at = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value  # noqa: E731
-        native.bind(tuple(at(n) for n in ("tf_quantize_rows", "tf_w8a8_packed_bytes", "tf_w8a8_gemm", "tf_route_experts",
-                                          "tf_w8a8_expert_gemm", "tf_combine_experts")),
-                    torch._C._cuda_getCurrentRawStream)
+        native.bind(tuple(at(n) for n in ("tf_quantize_rows", "tf_w8a8_packed_bytes", "tf_w8a8_workspace_bytes",
+                                          "tf_w8a8_gemm", "tf_route_experts", "tf_w8a8_expert_gemm",
+                                          "tf_combine_experts", "hipStreamGetCaptureInfo")),
+                    torch._C._cuda_getCurrentRawStream, _w8a8_ws, _w8a8_workspace)
         _experts = {n: getattr(native, n) for n in names}
     return _experts
 
@@ -878,17 +880,49 @@ def _product_out(out, dtype, device, shape):
     return out
 
 
-def w8a8_gemm(codes, scales, packed, K: int, N: int, dtype=None, out=None):
+def w8a8_workspace_bytes(M: int, K: int, N: int) -> int:
+    n = load().tf_w8a8_workspace_bytes(M, K, N)
+    if n < 0:
+        raise TileFuseError(int(n), "tf_w8a8_workspace_bytes")
+    return int(n)
+
+
+_w8a8_ws = {}
+
+
+def _w8a8_workspace(device, nbytes):
+    """The 8-bit products' workspace for the current stream (or its capture), which
+    needs no counters."""
+    return _stream_workspace(_w8a8_ws, device, nbytes, False)
+
+
+def w8a8_gemm(codes, scales, packed, K: int, N: int, dtype=None, out=None, workspace=None):
     """The product of int8 codes [M, K] with a scale a row (quantize_rows) and a packed
-    weight (pack_w8a8): [M, N] of dtype (fp16 unless given, or bf16).  Sums are exact."""
-    got = _expert_call("gemm", "tf_w8a8_gemm", codes, scales, packed, K, N, dtype, out)
+    weight (pack_w8a8): [M, N] of dtype (fp16 unless given, or bf16).  Sums are exact.
+    workspace: None for a cached one of the current stream (under torch.cuda.graph one
+    of the graph's), False for none (K is then never split over workgroups), or bytes
+    (w8a8_workspace_bytes) of the caller's, which calls that may run concurrently must
+    not share."""
+    got = _expert_call("gemm", "tf_w8a8_gemm", codes, scales, packed, K, N, dtype, out, workspace)
     if got is not NotImplemented:
         return got
     dtype, code = _codes_of(codes, scales, packed, K, N, 1, dtype if out is None else dtype or out.dtype)
     M = codes.shape[0]
     out = _product_out(out, dtype, codes.device, (M, N))
     if M > 0:
-        _launch("tf_w8a8_gemm", codes.device, code, _ptr(codes), _ptr(scales), _ptr(packed), _ptr(out), M, K, N)
+        if workspace is None:
+            need = w8a8_workspace_bytes(M, K, N)
+            workspace = _w8a8_workspace(codes.device, need) if need else False
+        ws_bytes = 0
+        if workspace is False:
+            workspace = None
+        else:
+            _need_cuda(workspace)
+            if workspace.device != codes.device:
+                raise ValueError(f"the workspace must be on {codes.device}")
+            ws_bytes = workspace.numel() * workspace.element_size()
+        _launch("tf_w8a8_gemm", codes.device, code, _ptr(codes), _ptr(scales), _ptr(packed), _ptr(out), M, K, N,
+                _ptr(workspace), ws_bytes)
     return out
 
 

@@ -53,15 +53,23 @@ def test_pack_rejects(lib, kw, want):
     assert lib.tf_pack_w8a8(*(PACK | kw).values(), NULL) == want
 
 
-GEMM = dict(dtype=1, A=P, scales=P, packed=P, C=P, M=4, K=64, N=64)
+GEMM = dict(dtype=1, A=P, scales=P, packed=P, C=P, M=4, K=64, N=64, ws=NULL, ws_bytes=0)
 
 
 @pytest.mark.parametrize("kw,want", [
     (dict(A=NULL), NONE), (dict(scales=NULL), NONE), (dict(packed=NULL), NONE), (dict(C=NULL), NONE), (dict(dtype=2), ARG),
     (dict(M=0), SHAPE), (dict(M=(1 << 20) + 1), SHAPE), (dict(K=72), SHAPE), (dict(N=68), SHAPE), (dict(A=P_8), ALIGN),
-    (dict(C=P_8), ALIGN), (dict(packed=P_16), ALIGN), (dict(scales=P_2), ALIGN)], ids=str)
+    (dict(C=P_8), ALIGN), (dict(packed=P_16), ALIGN), (dict(scales=P_2), ALIGN), (dict(ws=P_8, ws_bytes=1 << 30), ALIGN),
+    (dict(M=64, K=14336, N=4096, ws=P, ws_bytes=64), ARG)], ids=str)
 def test_gemm_rejects(lib, kw, want):
     assert lib.tf_w8a8_gemm(*(GEMM | kw).values(), NULL) == want
+
+
+@pytest.mark.parametrize("M,K,N,want", [
+    (64, 14336, 4096, 4 * 64 * 4096 * 4), (1, 14336, 4096, 0), (64, 4096, 4096, 0), (2048, 14336, 4096, 0),
+    (0, 64, 64, SHAPE), (1, 24, 64, SHAPE), (1, 64, 4, SHAPE), ((1 << 20) + 1, 64, 64, SHAPE)])
+def test_gemm_workspace(lib, M, K, N, want):
+    assert lib.tf_w8a8_workspace_bytes(M, K, N) == want
 
 
 ROUTE = dict(dtype=1, logits=P, stride=8, bias=NULL, T=4, experts=8, top_k=2, scoring=0, groups=1, top_groups=1,

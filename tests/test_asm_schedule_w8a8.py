@@ -47,8 +47,8 @@ def fns():
         out = T._compile_asm(os.path.join(T.B.CSRC, "tf_w8a8_tile.hip"), os.path.join(tmp, "tile.s"))
         text = open(out).read()
     got = [(m.group(1), cut(m.group(2))) for m in re.finditer(r"^(_Z\S+):[^\n]*\n(.*?)^\.Lfunc_end", text, re.S | re.M)
-           if "w8a8_tile" in m.group(1)]
-    assert len(got) == 3 * len(FORMS)                 # dense, experts with rows and without
+           if "w8a8_tile_" in m.group(1)]
+    assert len(got) == 3 * len(FORMS) + 1             # dense, experts with rows and without; K split
     return got
 
 

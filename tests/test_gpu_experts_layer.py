@@ -149,6 +149,70 @@ def test_rows_of_many_sizes_agree(tf):
         assert torch.equal(tf.w8a8_gemm(q[:M], s[:M], packed, K, N, dtype=torch.bfloat16), want[:M]), M
 
 
+@pytest.mark.parametrize("path", ["native", "general"])
+@pytest.mark.parametrize("M,K,N", [(17, 14336, 4096), (49, 14336, 1032), (64, 8208, 264), (70, 14336, 4096), (128, 16384, 520)])
+def test_split_over_k(tf, monkeypatch, path, M, K, N):
+    """With the cached workspace, one of the caller's that starts as noise, and none: the
+    same bits; rows behind the output stay as they are."""
+    if path == "general":
+        monkeypatch.setattr(tf, "_experts", {"gemm": lambda *call: NotImplemented})
+    q = torch.randint(-128, 128, (M, K), device="cuda").to(torch.int8)
+    w, ws = torch.randint(-128, 128, (K, N), device="cuda").to(torch.int8), torch.rand(N, device="cuda")
+    s, packed = torch.rand(M, device="cuda") * 1e-5, tf.pack_w8a8(w, ws)
+    need = tf.w8a8_workspace_bytes(M, K, N)
+    assert need > 0
+    big = torch.full((M + 2, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    one = tf.w8a8_gemm(q, s, packed, K, N, out=big[:M], workspace=False)
+    own = torch.randint(-2 ** 31, 2 ** 31, (need // 4 + 16,), dtype=torch.int32, device="cuda")
+    keep = own[need // 4:].clone()
+    for ws in (None, own, None, own[:need // 4]):
+        out = torch.full((M + 2, N), 7.0, dtype=torch.bfloat16, device="cuda")
+        tf.w8a8_gemm(q, s, packed, K, N, out=out[:M], workspace=ws)
+        assert torch.equal(out, big)
+    assert (big[M:] == 7).all() and torch.equal(own[need // 4:], keep)
+    got = down(one)
+    want = oracle.w8a8(q.cpu().numpy(), down(s), w.cpu().numpy(), packed_scales(tf, packed, K, N))
+    assert (np.abs(got - want) <= (U["bf16"] + 4 * E32) * np.abs(want)).all()
+    with pytest.raises(tf.TileFuseError) as err:
+        tf.w8a8_gemm(q, s, packed, K, N, workspace=own[:8])
+    assert err.value.status == tf.TF_ERR_ARG
+
+
+def packed_scales(tf, packed, K, N):
+    """The columns' scales at the end of a packed weight."""
+    at = (N + 15) // 16 * ((K + 127) // 128 * 2) * 1024
+    return packed[at:at + 4 * N].view(torch.float32).double().cpu().numpy()
+
+
+def test_split_over_k_in_graphs(tf):
+    """Two graphs and eager calls, larger ones too, between their replays: each has a
+    workspace of its own."""
+    K, N = 14336, 1024
+    packed = tf.pack_w8a8(torch.randint(-127, 128, (K, N), device="cuda").to(torch.int8), torch.rand(N, device="cuda"))
+    make = lambda M: torch.randint(-127, 128, (M, K), device="cuda").to(torch.int8)  # noqa: E731
+    s, graphs = torch.rand(128, device="cuda") * 1e-5, []
+    assert all(tf.w8a8_workspace_bytes(M, K, N) for M in (50, 64, 128))
+    for M in (50, 64):
+        q = make(M)
+        tf.w8a8_gemm(q, s[:M], packed, K, N)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = tf.w8a8_gemm(q, s[:M], packed, K, N)
+        graphs.append((g, q, out, M))
+    side = torch.cuda.Stream()
+    for _ in range(4):
+        with torch.cuda.stream(side):
+            other = make(128)
+            got = tf.w8a8_gemm(other, s, packed, K, N)
+        for g, q, out, M in graphs:
+            q.copy_(make(M))
+            g.replay()
+            assert torch.equal(out, tf.w8a8_gemm(q, s[:M], packed, K, N, workspace=False))
+        side.synchronize()
+        assert torch.equal(got, tf.w8a8_gemm(other, s, packed, K, N, workspace=False))
+
+
 @pytest.fixture(params=["native", "general"])
 def path(request, tf, monkeypatch):
     if request.param == "general":
