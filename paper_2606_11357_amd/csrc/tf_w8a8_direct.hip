@@ -5,7 +5,10 @@
 // they are added does not change them.  A workgroup owns 16 MB rows and 16 PN
 // columns and deals K's atoms of 64 to its waves in turn; each wave takes both
 // operands straight into registers, a ring of D atoms ahead, and the waves' sums
-// are added in LDS.
+// are added in LDS.  Memory-bound: weights are read once, and every workgroup reads all
+// of its rows.  16 columns and four waves a workgroup: N = 4096 is then one a compute
+// unit.  One row, 4096 x 4096: 6.0 us (of which 3.3 are the memory's; 32 columns 6.6, eight
+// waves 6.0), 14336 x 4096: 13.6 us (4.3 TB/s; 32 columns 16.8); 16 rows 6.4 and 17.3 us.
 #include <algorithm>
 
 #include "tf_w8a8.h"
