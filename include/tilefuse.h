@@ -470,9 +470,9 @@ int tf_w8a8_gemm(int dtype, const int8_t* A, const float* a_scales, const void* 
  * token's experts, in that order.  Of equal groups or choices the lower index goes
  * first.  weights = score * scale, with `renormalize` divided by the sum of the
  * token's chosen scores before (zeros where that is 0).  An expert whose logit is
- * -infinity or NaN (or whose choice is NaN) comes after all others, with weight 0
- * where it is chosen for want of them, and is left out of a group's sum; infinite logits share the
- * softmax.  Outputs:
+ * -infinity or NaN, or whose choice is, comes after all others, with weight 0 where it
+ * is chosen for want of them, and is left out of a group's sum; infinite logits share
+ * the softmax.  Outputs:
  *   weights fp32 [T, top_k], chosen int32 [T, top_k],
  *   offsets int32 [experts + 1]  expert e has the slots offsets[e] .. offsets[e+1] - 1,
  *   tokens  int32 [T * top_k]    the token of each slot, ascending within an expert,

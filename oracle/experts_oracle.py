@@ -62,7 +62,7 @@ def route(logits, k, bias=None, scoring="softmax", groups=1, top_groups=None, gr
         if scoring == "softmax" and score.sum() > 0:
             score = score / score.sum()
         choice = score + (0.0 if bias is None else np.asarray(bias, np.float64))
-        masked |= np.isnan(choice)
+        masked |= np.isnan(choice) | (choice == -np.inf)
         choice = np.where(masked, -np.inf, choice)
         part = np.arange(E) // (E // groups)
         value = []

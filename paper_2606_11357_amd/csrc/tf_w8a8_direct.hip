@@ -30,7 +30,7 @@ __device__ __forceinline__ void direct_block(const W8Args& a, const uint8_t* pac
     const int c = lane & 15, g = lane >> 4;
     // A: from its first row here on, or all of it where rows are gathered
     const int64_t base = a.rows ? 0 : row0;
-    const int64_t a_bytes = (a.a_rows - base) * a.K;
+    const int64_t a_bytes = max((a.a_rows - base) * a.K, (int64_t)0);        // (0: all of these rows are missing)
     const __amdgpu_buffer_rsrc_t ar = make_rsrc(a.A + base * a.K, (uint32_t)min(a_bytes, (int64_t)kNowhere));
     uint32_t a_off[MB];
     int64_t a_row[MB];

@@ -941,8 +941,8 @@ def route_experts(logits, top_k: int, *, bias=None, scoring="softmax", groups=1,
     [experts]), within the top_groups best of `groups` neighbouring groups where
     given, a group's value being the sum of its two largest choices ("top2") or the
     largest ("max"); ties go to the lower index.  weights = score, divided by the sum
-    of the chosen ones with renormalize, times scale.  An expert whose logit is
-    -infinity or NaN comes last, with weight 0.  Returns a Routing."""
+    of the chosen ones with renormalize, times scale.  An expert whose logit or choice
+    is -infinity or NaN comes last, with weight 0.  Returns a Routing."""
     if scoring not in ("softmax", "sigmoid"):
         raise ValueError("scoring must be softmax or sigmoid")
     if group_score not in ("top2", "max"):

@@ -244,6 +244,15 @@ def test_route_masked(tf, share, kw):
     check_routing(tf, put(x), x.astype(np.float64), 5, bias=bias, **kw)
 
 
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_route_bias_that_masks(tf, scoring):
+    """Experts that a bias takes out are chosen for want of others only, with weight 0."""
+    x = np.random.default_rng(4).standard_normal((20, 6)).astype(np.float32)
+    bias = np.array([-np.inf, 0.1, np.nan, -np.inf, 0.0, -0.1], np.float32)
+    for k in (2, 3, 4, 6):
+        check_routing(tf, put(x), x.astype(np.float64), k, bias=bias, scoring=scoring, renormalize=True)
+
+
 def test_route_large_logits(tf):
     """The type's lowest and highest values, and differences that underflow."""
     big = float(np.finfo(np.float32).max)
@@ -317,6 +326,24 @@ def test_expert_gemm_rows_of_no_expert(tf, S):
     for wild in ([-5, S, S + 9, 2 ** 31 - 1, S + 1], [0, S, -7, 5, 4]):
         got = tf.w8a8_expert_gemm(put(q), put(s), packed, K, N, put(np.array(wild, np.int32)), dtype=torch.bfloat16)
         check_product(down(got), oracle.w8a8(q, s, w[0], np.full(N, 2.0 ** -12)), "bf16")
+
+
+@pytest.mark.parametrize("slots,a_rows", [(40, 5), (40, 1), (600, 300), (3000, 2), (3000, 2600)])
+def test_expert_gemm_more_slots_than_rows(tf, slots, a_rows):
+    """Slots past the last row of A, without rows, are rows that do not exist: zeros (the
+    C entry; the binding has a slot for each row)."""
+    rng = np.random.default_rng(slots)
+    E, K, N = 2, 272, 72
+    q, w = weight(rng, (a_rows, K)), weight(rng, (E, K, N))
+    s, packed = np.ones(a_rows, np.float32), tf.pack_w8a8(put(w), torch.full((E, N), 2.0 ** -12, device="cuda"))
+    offsets = np.array([0, slots // 2, slots], np.int32)
+    out = torch.full((slots + 1, N), 9.0, dtype=torch.bfloat16, device="cuda")
+    qd, sd, od = put(q), put(s), put(offsets)
+    tf._launch("tf_w8a8_expert_gemm", out.device, tf.TF_BF16, tf._ptr(qd), tf._ptr(sd), a_rows, tf._ptr(packed),
+               tf._ptr(od), None, tf._ptr(out), slots, K, N, E)
+    want = oracle.expert_products(q, s, w, np.full((E, N), 2.0 ** -12), offsets, np.arange(slots))
+    check_product(down(out)[:slots], want, "bf16")
+    assert (out[slots:] == 9).all() and (out[a_rows:slots] == 0).all()
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])

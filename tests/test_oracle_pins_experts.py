@@ -62,6 +62,8 @@ def check_routing(ns):
     assert ns.route(x, 4, groups=4, top_groups=3)[1].tolist() == [[4, 5, 6, 7]]
     w, e = ns.route(np.array([[-np.inf, 0.0, np.nan, -np.inf]]), 3, renormalize=True)
     assert e.tolist() == [[1, 0, 2]] and w.tolist() == [[1.0, 0.0, 0.0]]
+    w, e = ns.route(np.zeros((1, 3)), 3, bias=np.array([-np.inf, 0.0, np.nan]))
+    assert e.tolist() == [[1, 0, 2]] and w.tolist() == [[1 / 3, 0.0, 0.0]]
     w, e = ns.route(np.full((1, 3), -np.inf), 2, renormalize=True)
     assert e.tolist() == [[0, 1]] and w.tolist() == [[0.0, 0.0]]
     w, e = ns.route(np.array([[np.inf, 0.0, np.inf, 5.0]]), 3)
