@@ -261,6 +261,19 @@ def test_route_large_logits(tf):
         check_routing(tf, put(x), x.astype(np.float64), 3, scoring=scoring, renormalize=True)
 
 
+def test_order_of_many_choices(tf):
+    """Whole blocks of choices for every wave, a few more, and several times as many."""
+    for T, E, k in ((8192, 16, 8), (8200, 16, 8), (70000, 5, 3)):
+        x = torch.randn(T, E, device="cuda")
+        r = tf.route_experts(x, k)
+        assert torch.equal(r.experts.long(), x.double().sort(dim=1, descending=True, stable=True).indices[:, :k])
+        flat = r.experts.flatten().long()
+        order = torch.argsort(flat, stable=True)
+        assert torch.equal(r.tokens.long(), order // k)
+        assert torch.equal(r.places.flatten().long()[order], torch.arange(T * k, device="cuda"))
+        assert r.offsets.tolist() == [0] + torch.bincount(flat, minlength=E).cumsum(0).tolist()
+
+
 def test_route_strided_and_empty(tf):
     wide = torch.randn(9, 40, device="cuda")
     a, b = tf.route_experts(wide[:, 3:27], 4), tf.route_experts(wide[:, 3:27].contiguous(), 4)
