@@ -5,11 +5,13 @@
 // in the largest form one a compute unit, one wave a SIMD with the whole register file:
 // 256 rows by 64 columns (256 accumulators) of v_mfma_i32_16x16x64_i8, 64 of them a step.
 //  - A goes global -> LDS by direct loads, two steps (128 bytes of a row, whole cache
-//    lines) at a time into one of four buffers, three such pairs ahead; 16-byte
-//    chunks are XOR-swizzled by row, so that fragment reads meet no bank twice.
-//  - A fragments are read half a step ahead of their use, in two bursts a step.
+//    lines) at a time into one of four or eight buffers, all but one or two of them
+//    ahead; 16-byte chunks are XOR-swizzled by row, so that fragment reads meet no bank
+//    twice.
+//  - A fragments are read a step ahead of their use, one beside every few matrix
+//    instructions.
 //  - Weights are stored in the order of the matrix instruction's operand: a wave
-//    loads its own columns straight into a ring of registers, three steps ahead.
+//    loads its own columns straight into a ring of registers, three or seven steps ahead.
 //  - Workgroups are dealt to the XCDs so that the 32 tiles that one runs at a time
 //    are about 8 by 4: each L2 then serves 12 operand tiles to 32.
 //  - Outputs are scaled and stored from the accumulators, past the L2 (one tile of K = 512
@@ -174,10 +176,13 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
     float row_scale = 0.f, column_scale = 0.f;
     // Direct load r of wave w fills rows 4 RB w + 8 r .. + 7 of a buffer, eight lanes a row.
     auto dma_a = [&](int pair, int buf, int r) {
-        dma16(ar, sm.a + buf * F::kPairBytes + (RB / 2 * wave + r) * 1024, avoff[r] + (uint32_t)min(from / 2 + pair, pairs - 1) * 128u);
+        dma16(ar, sm.a + buf * F::kPairBytes + (RB / 2 * wave + r) * 1024,
+              avoff[r] + (uint32_t)min(from / 2 + pair, pairs - 1) * 128u);
     };
     u32x4 ring[R][CB];
-    auto load_b = [&](int step, int t, u32x4& v) { v = load16(wr[t], (uint32_t)(lane * 16 + (from + step) * kW8AtomBytes)); };
+    auto load_b = [&](int step, int t, u32x4& v) {
+        v = load16(wr[t], (uint32_t)(lane * 16 + (from + step) * kW8AtomBytes));
+    };
 
     constexpr int kOps = F::kDma + CB;                // vector-memory operations of a wave and step
     constexpr int kHalf0 = F::kOften ? 2 * P - 2 : 2 * P - 3;      // half of a pair that step 0 brings
@@ -208,7 +213,8 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
         for (int u = 0; u < CB; ++u) {
             const int64_t panel = t.col0 / kW8Panel + CB * wave + u;
             const bool here = panel < a.np;
-            wr[u] = make_rsrc(t.packed + (here ? panel : 0) * a.na * kW8AtomBytes, here ? (uint32_t)a.na * kW8AtomBytes : 0u);
+            wr[u] = make_rsrc(t.packed + (here ? panel : 0) * a.na * kW8AtomBytes,
+                              here ? (uint32_t)a.na * kW8AtomBytes : 0u);
         }
         if (tid < F::BM) {
             const int at = row_of(tid);
@@ -251,158 +257,160 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
     begin(tile);
     constexpr int kStores = SPLIT ? RB * CB : CB > 1 ? RB * CB / 2 : RB;      // of a wave and tile
     for (int turn = 0;; ++turn) {
-    i32x4 acc[RB][CB];
+        i32x4 acc[RB][CB];
 #pragma unroll
-    for (int i = 0; i < RB; ++i)
+        for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[i][t] = i32x4{0, 0, 0, 0};
-    if (tid < F::BM) sm.rows[turn & 1][tid] = row_scale;
-    if (tid < F::BN) sm.columns[turn & 1][tid] = column_scale;
-    lds_wait();
-    // (the outputs of the tile before were stored after these loads were issued)
-    constexpr int kFirst = (R - 1) * kOps, kNext = kFirst + kStores;
-    if (turn == 0) barrier_after_loads<kFirst < 63 ? kFirst : 63>();
-    else barrier_after_loads<kNext < 63 ? kNext : 63>();
-    u32x4 af[F::kAhead ? 2 : 1][RB];
+            for (int t = 0; t < CB; ++t) acc[i][t] = i32x4{0, 0, 0, 0};
+        if (tid < F::BM) sm.rows[turn & 1][tid] = row_scale;
+        if (tid < F::BN) sm.columns[turn & 1][tid] = column_scale;
+        lds_wait();
+        // (the outputs of the tile before were stored after these loads were issued)
+        constexpr int kFirst = (R - 1) * kOps, kNext = kFirst + kStores;
+        if (turn == 0) barrier_after_loads<kFirst < 63 ? kFirst : 63>();
+        else barrier_after_loads<kNext < 63 ? kNext : 63>();
+        u32x4 af[F::kAhead ? 2 : 1][RB];
 #pragma unroll
-    for (int i = 0; i < (F::kAhead ? RB : RB - 1); ++i) af[0][i] = lds_read_block(a_lane[0], i);
-    lds_wait();
+        for (int i = 0; i < (F::kAhead ? RB : RB - 1); ++i) af[0][i] = lds_read_block(a_lane[0], i);
+        lds_wait();
 
-    // Steps in turn, R to a pass of the loop (so that the ring has fixed places; steps
-    // past K multiply zeros), S slots each of one matrix instruction (row block q / CB,
-    // column block q % CB) and at most one of the others beside it, which are spread over
-    // the step: four waves at once ask LDS and the memory pipe for four times what one
-    // does, and an instruction that has to wait for its turn holds up those behind it.
-    //  - before slot CB i: wait for the fragment of row block i
-    //  - at slot CB i: read that of block i - 1 for the next step (block RB - 1 of this
-    //    step at slot 0).  Small forms (kAhead) read all of the next step's into a second
-    //    set.
-    //  - every S / kOps slots: a direct load (half a pair a step) or one of the weights of
-    //    step s + R - 1.
-    // Pair p is read from step 2 p - 1 on: at the end of step 2 p - 2 its direct loads
-    // have to have landed, which leaves this wave's later operations on their way (they
-    // complete in order).  After the barrier there no wave reads pair p - 2 any more, and
-    // the next two steps fill its buffer with pair p - 2 + P: one barrier for two steps.
-    // With kOften a second barrier ends the odd steps, after which pair p - 1 is done, and
-    // steps 2 p and 2 p + 1 fill its buffer: a step earlier, where four buffers of 32 KB
-    // are all there is.
-    constexpr int kLater = CB + (F::kOften ? 2 * P - 5 : 2 * P - 6) * kOps;
-    for (int s0 = 0; s0 < steps; s0 += R) {
+        // Steps in turn, R to a pass of the loop (so that the ring has fixed places; steps
+        // past K multiply zeros), S slots each of one matrix instruction (row block q / CB,
+        // column block q % CB) and at most one of the others beside it, which are spread over
+        // the step: four waves at once ask LDS and the memory pipe for four times what one
+        // does, and an instruction that has to wait for its turn holds up those behind it.
+        //  - before slot CB i: wait for the fragment of row block i
+        //  - at slot CB i: read that of block i - 1 for the next step (block RB - 1 of this
+        //    step at slot 0).  Small forms (kAhead) read all of the next step's into a second
+        //    set.
+        //  - every S / kOps slots: a direct load (half a pair a step) or one of the weights of
+        //    step s + R - 1.
+        // Pair p is read from step 2 p - 1 on: at the end of step 2 p - 2 its direct loads
+        // have to have landed, which leaves this wave's later operations on their way (they
+        // complete in order).  After the barrier there no wave reads pair p - 2 any more, and
+        // the next two steps fill its buffer with pair p - 2 + P: one barrier for two steps.
+        // With kOften a second barrier ends the odd steps, after which pair p - 1 is done, and
+        // steps 2 p and 2 p + 1 fill its buffer: a step earlier, where four buffers of 32 KB
+        // are all there is.
+        constexpr int kLater = CB + (F::kOften ? 2 * P - 5 : 2 * P - 6) * kOps;
+        for (int s0 = 0; s0 < steps; s0 += R) {
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int step = s0 + j, odd = j & 1;
-            auto place = [&](int pair) { return (uint32_t)((s0 / 2 + pair) & (P - 1)) * F::kPairBytes; };
-            const uint32_t cur = place(j / 2), next = place((j + 1) / 2);
-            // the pair whose half is filled in this step
-            const int fill = s0 / 2 + (F::kOften ? j / 2 + P - 1 : (j + 1) / 2 + P - 2);
-            const int half = F::kOften ? odd : odd ^ 1;
-            constexpr int kSets = F::kAhead ? 2 : 1;
-            u32x4 (&now)[RB] = af[j % kSets];
-            u32x4 (&nxt)[RB] = af[(j + 1) % kSets];
-            if (j == 0) asm volatile("s_nop 1");     // (after the accumulators' zeros)
+            for (int j = 0; j < R; ++j) {
+                const int step = s0 + j, odd = j & 1;
+                auto place = [&](int pair) { return (uint32_t)((s0 / 2 + pair) & (P - 1)) * F::kPairBytes; };
+                const uint32_t cur = place(j / 2), next = place((j + 1) / 2);
+                // the pair whose half is filled in this step
+                const int fill = s0 / 2 + (F::kOften ? j / 2 + P - 1 : (j + 1) / 2 + P - 2);
+                const int half = F::kOften ? odd : odd ^ 1;
+                constexpr int kSets = F::kAhead ? 2 : 1;
+                u32x4 (&now)[RB] = af[j % kSets];
+                u32x4 (&nxt)[RB] = af[(j + 1) % kSets];
+                if (j == 0) asm volatile("s_nop 1");     // (after the accumulators' zeros)
 #pragma unroll
-            for (int q = 0; q < S; ++q) {
-                const int i = q / CB, t = q % CB;
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (F::kAhead) {
-                    if (q == 0) lds_wait();
-                } else {
-                    if (t == 0) lds_wait_but<RB - 2>();
+                for (int q = 0; q < S; ++q) {
+                    const int i = q / CB, t = q % CB;
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (F::kAhead) {
+                        if (q == 0) lds_wait();
+                    } else {
+                        if (t == 0) lds_wait_but<RB - 2>();
+                    }
+                    mfma_i8(acc[i][t], ring[j % R][t], now[i]);
+                    if constexpr (F::kAhead) {
+#pragma unroll
+                        for (int r = q * RB / S; r < (q + 1) * RB / S; ++r)
+                            nxt[r] = lds_read_block(a_lane[odd ^ 1] + next, r);
+                    } else if (t == 0) {
+                        if (i == 0) now[RB - 1] = lds_read_block(a_lane[odd] + cur, RB - 1);
+                        else nxt[i - 1] = lds_read_block(a_lane[odd ^ 1] + next, i - 1);
+                    }
+#pragma unroll
+                    for (int o = 0; o < kOps; ++o) {
+                        if (q != o * S / kOps + CB / 2) continue;
+                        if (o < F::kDma) dma_a(fill, fill & (P - 1), F::kDma * half + o);
+                        else load_b(step + R - 1, o - F::kDma, ring[(j + R - 1) % R][o - F::kDma]);
+                    }
                 }
-                mfma_i8(acc[i][t], ring[j % R][t], now[i]);
-                if constexpr (F::kAhead) {
-#pragma unroll
-                    for (int r = q * RB / S; r < (q + 1) * RB / S; ++r) nxt[r] = lds_read_block(a_lane[odd ^ 1] + next, r);
-                } else if (t == 0) {
-                    if (i == 0) now[RB - 1] = lds_read_block(a_lane[odd] + cur, RB - 1);
-                    else nxt[i - 1] = lds_read_block(a_lane[odd ^ 1] + next, i - 1);
-                }
-#pragma unroll
-                for (int o = 0; o < kOps; ++o) {
-                    if (q != o * S / kOps + CB / 2) continue;
-                    if (o < F::kDma) dma_a(fill, fill & (P - 1), F::kDma * half + o);
-                    else load_b(step + R - 1, o - F::kDma, ring[(j + R - 1) % R][o - F::kDma]);
-                }
+                // what follows the loop may read the accumulators at once
+                if (j == R - 1) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1");
+                if (!odd) barrier_after_loads<kLater < 63 ? kLater : 63>();
+                else if (F::kOften) barrier_only();
             }
-            // what follows the loop may read the accumulators at once
-            if (j == R - 1) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1");
-            if (!odd) barrier_after_loads<kLater < 63 ? kLater : 63>();
-            else if (F::kOften) barrier_only();
         }
-    }
-    // The last step's reads, which nothing uses, keep their registers until they are done.
-    lds_wait();
+        // The last step's reads, which nothing uses, keep their registers until they are done.
+        lds_wait();
 #pragma unroll
-    for (int i = 0; i < RB; ++i) asm volatile("" ::"v"(af[0][i]), "v"(af[F::kAhead ? 1 : 0][i]));
-    __builtin_amdgcn_s_waitcnt(0);       // the direct loads past the end have landed
-    __syncthreads();                     // and no wave reads the buffers
-    const Tile done = tile;
-    const bool more = next_tile(turn + 1, tile);
-    if (more) begin(tile);
+        for (int i = 0; i < RB; ++i) asm volatile("" ::"v"(af[0][i]), "v"(af[F::kAhead ? 1 : 0][i]));
+        __builtin_amdgcn_s_waitcnt(0);       // the direct loads past the end have landed
+        __syncthreads();                     // and no wave reads the buffers
+        const Tile done = tile;
+        const bool more = next_tile(turn + 1, tile);
+        if (more) begin(tile);
 
-    // Outputs.  Lane (c, kg) holds row 16 i + c, columns 16 t + 4 kg + 0..3 of the wave's;
-    // rows of 16 lanes swapped between blocks t and t + 1 make that eight columns a lane,
-    // 64 bytes of a row of C a store.  Rows and columns past the end have offsets that the
-    // buffer drops: the number of stores is the same for every tile.
-    if constexpr (SPLIT) {
-        const int lane = again(threadIdx.x & 63), c = lane & 15, kg = lane >> 4;
-        const __amdgpu_buffer_rsrc_t pr = make_rsrc(a.parts + (done.part * a.M + done.row0) * a.N,
-                                                    (uint32_t)done.rows * (uint32_t)a.N * 4u);
-        const int64_t n0 = done.col0 + 16 * CB * wave + 4 * kg;
-        uint32_t row = ((uint32_t)c * (uint32_t)a.N + (uint32_t)n0) * 4u, sixteen = 64u * (uint32_t)a.N;
-        int left = done.rows;
+        // Outputs.  Lane (c, kg) holds row 16 i + c, columns 16 t + 4 kg + 0..3 of the wave's;
+        // rows of 16 lanes swapped between blocks t and t + 1 make that eight columns a lane,
+        // 64 bytes of a row of C a store.  Rows and columns past the end have offsets that the
+        // buffer drops: the number of stores is the same for every tile.
+        if constexpr (SPLIT) {
+            const int lane = again(threadIdx.x & 63), c = lane & 15, kg = lane >> 4;
+            const __amdgpu_buffer_rsrc_t pr = make_rsrc(a.parts + (done.part * a.M + done.row0) * a.N,
+                                                        (uint32_t)done.rows * (uint32_t)a.N * 4u);
+            const int64_t n0 = done.col0 + 16 * CB * wave + 4 * kg;
+            uint32_t row = ((uint32_t)c * (uint32_t)a.N + (uint32_t)n0) * 4u, sixteen = 64u * (uint32_t)a.N;
+            int left = done.rows;
 #pragma unroll
-        for (int i = 0; i < RB; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < RB; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < CB; ++t)
-                store16(pr, __builtin_bit_cast(u32x4, whole(acc[i][t])),
-                        c < left && n0 + 16 * t < a.N ? row + 64u * t : kNowhere);
-            row += sixteen;
-            left -= 16;
-        }
-    } else {
-    const int lane = again(threadIdx.x & 63), c = lane & 15, kg = lane >> 4;
-    const __amdgpu_buffer_rsrc_t cr = make_rsrc(a.C + done.row0 * a.N, (uint32_t)done.rows * (uint32_t)a.N * 2u);
-    const float* sr = sm.rows[turn & 1];
-    const float* sc = sm.columns[turn & 1] + 16 * CB * wave + 4 * kg;
-    float4_t sw[CB];
+                for (int t = 0; t < CB; ++t)
+                    store16(pr, __builtin_bit_cast(u32x4, whole(acc[i][t])),
+                            c < left && n0 + 16 * t < a.N ? row + 64u * t : kNowhere);
+                row += sixteen;
+                left -= 16;
+            }
+        } else {
+            const int lane = again(threadIdx.x & 63), c = lane & 15, kg = lane >> 4;
+            const __amdgpu_buffer_rsrc_t cr =
+                make_rsrc(a.C + done.row0 * a.N, (uint32_t)done.rows * (uint32_t)a.N * 2u);
+            const float* sr = sm.rows[turn & 1];
+            const float* sc = sm.columns[turn & 1] + 16 * CB * wave + 4 * kg;
+            float4_t sw[CB];
 #pragma unroll
-    for (int t = 0; t < CB; ++t) sw[t] = *reinterpret_cast<const float4_t*>(sc + 16 * t);
-    uint32_t to[(CB + 1) / 2];
-#pragma unroll
-    for (int t = 0; t < CB; t += 2) {
-        const int64_t n = done.col0 + 16 * CB * wave + (CB > 1 ? 16 * (t + (kg & 1)) + 8 * (kg >> 1) : 4 * kg);
-        to[t / 2] = n < a.N ? (uint32_t)n * 2u : kNowhere;
-    }
-    uint32_t row = (uint32_t)c * (uint32_t)a.N * 2u, sixteen = 32u * (uint32_t)a.N;
-    int left = done.rows;
-    auto store_all = [&](auto is_bf) {
-        constexpr bool bf = decltype(is_bf)::value;
-#pragma unroll
-        for (int i = 0; i < RB; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
-            const float sa = sr[16 * i + c];
-            const bool here = c < left;
+            for (int t = 0; t < CB; ++t) sw[t] = *reinterpret_cast<const float4_t*>(sc + 16 * t);
+            uint32_t to[(CB + 1) / 2];
 #pragma unroll
             for (int t = 0; t < CB; t += 2) {
-                const uint32_t off = here && to[t / 2] != kNowhere ? row + to[t / 2] : kNowhere;
-                const uint2 x = w8_scaled(bf, whole(acc[i][t]), sa, sw[t]);
-                if constexpr (CB > 1) {
-                    const uint2 y = w8_scaled(bf, whole(acc[i][t + 1]), sa, sw[t + 1]);
-                    store16(cr, rows_swapped(x, y), off);
-                } else {
-                    store8(cr, x, off);
-                }
+                const int64_t n = done.col0 + 16 * CB * wave + (CB > 1 ? 16 * (t + (kg & 1)) + 8 * (kg >> 1) : 4 * kg);
+                to[t / 2] = n < a.N ? (uint32_t)n * 2u : kNowhere;
             }
-            row += sixteen;
-            left -= 16;
+            uint32_t row = (uint32_t)c * (uint32_t)a.N * 2u, sixteen = 32u * (uint32_t)a.N;
+            int left = done.rows;
+            auto store_all = [&](auto is_bf) {
+                constexpr bool bf = decltype(is_bf)::value;
+#pragma unroll
+                for (int i = 0; i < RB; ++i) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const float sa = sr[16 * i + c];
+                    const bool here = c < left;
+#pragma unroll
+                    for (int t = 0; t < CB; t += 2) {
+                        const uint32_t off = here && to[t / 2] != kNowhere ? row + to[t / 2] : kNowhere;
+                        const uint2 x = w8_scaled(bf, whole(acc[i][t]), sa, sw[t]);
+                        if constexpr (CB > 1) {
+                            const uint2 y = w8_scaled(bf, whole(acc[i][t + 1]), sa, sw[t + 1]);
+                            store16(cr, rows_swapped(x, y), off);
+                        } else {
+                            store8(cr, x, off);
+                        }
+                    }
+                    row += sixteen;
+                    left -= 16;
+                }
+            };
+            if (a.bf) store_all(std::true_type{});
+            else store_all(std::false_type{});
         }
-    };
-    if (a.bf) store_all(std::true_type{});
-    else store_all(std::false_type{});
-    }
-    if (!more) return;
+        if (!more) return;
     }
 }
 
@@ -548,7 +556,8 @@ int launch_form(const W8Args& a, hipStream_t s) {
             return launch(w8a8_join_kernel, dim3((unsigned)((a.M * (a.N / 8) + 255) / 256)), dim3(256), 0, s, a);
         }
     }
-    if (!a.experts) return launch(w8a8_tile_kernel<F, false>, grid, dim3(kThreads), 0, s, a, (int)tiles_m, (int)tiles_n);
+    if (!a.experts)
+        return launch(w8a8_tile_kernel<F, false>, grid, dim3(kThreads), 0, s, a, (int)tiles_m, (int)tiles_n);
     return a.rows ? launch(w8a8_tile_experts_kernel<F, true>, grid, dim3(kThreads), 0, s, a, (int)tiles_n)
                   : launch(w8a8_tile_experts_kernel<F, false>, grid, dim3(kThreads), 0, s, a, (int)tiles_n);
 }
