@@ -21,13 +21,21 @@ struct QuantArgs {
     float* scale;
 };
 
-// g / (1 + e^-g).  The quotient is a reciprocal with one Newton step (with an
-// IEEE division 16 gated rows of 14336 took 6.5 us, so 5.9; 2048 rows 37.8 and 33.7):
-// within one unit in the last place.  e^-g is kept finite, where g e^g is nothing.
+// g / (1 + e^-g) for g >= kFarGate.  The quotient is a reciprocal with one Newton step
+// (with an IEEE division 16 gated rows of 14336 took 6.5 us, so 5.9; 2048 rows 37.8 and
+// 33.7): within one unit in the last place.
 __device__ __forceinline__ float silu(float g) {
-    const float d = 1.0f + expf(fminf(-g, 87.0f));
+    const float d = 1.0f + expf(-g);
     const float r = __builtin_amdgcn_rcpf(d);
     return g * fmaf(r, fmaf(-d, r, 1.0f), r);
+}
+// Below it silu(g) u = g e^g u: 1 + e^g is 1 in fp32.  e^g, or its reciprocal, leaves
+// fp32 below -87, where g e^g u may still be far within it, so e^(g / 2) comes in
+// twice, the second time last.
+constexpr float kFarGate = -64.0f;
+__device__ __forceinline__ float far_silu_mul(float g, float u) {
+    const float w = expf(0.5f * g);
+    return g * w * u * w;
 }
 
 // The largest |h| and a sum that is NaN where some h is not finite, over the WR
@@ -74,15 +82,33 @@ __global__ __launch_bounds__(WR == 1 ? 256 : 64 * WR) void quantize_rows_kernel(
         }
     }
     float h[V][8], top = 0.f, odd = 0.f;
+    if constexpr (GATED) {
+        float least = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float g = scale_f32<BF>(xv[i][j]);
+                least = fminf(least, g);
+                h[i][j] = silu(g) * scale_f32<BF>(uv[i][j]);
+            }
+        if (least < kFarGate) {                      // (rare)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float g = scale_f32<BF>(xv[i][j]);
+                    if (g < kFarGate) h[i][j] = far_silu_mul(g, scale_f32<BF>(uv[i][j]));
+                }
+        }
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float t = scale_f32<BF>(xv[i][j]);
-            if (GATED) t = silu(t) * scale_f32<BF>(uv[i][j]);
-            h[i][j] = t;
-            top = fmaxf(top, fabsf(t));
-            odd = fmaf(t, 0.f, odd);
+            if constexpr (!GATED) h[i][j] = scale_f32<BF>(xv[i][j]);
+            top = fmaxf(top, fabsf(h[i][j]));
+            odd = fmaf(h[i][j], 0.f, odd);
         }
     row_top<WR>(top, odd, red);
     // A row under 2^-100 is one of zeros (127 / top would leave fp32); one with a
