@@ -27,8 +27,11 @@
  *    Calls only enqueue work on `stream` and return; the caller synchronizes.
  *  - The caller allocates and frees every buffer; the library keeps no device
  *    memory.  Its only global state is a per-device cache of the compute-unit
- *    count (read atomically; the launch plans depend on it), so calls are
- *    thread-safe.  Plans are made for the device of the `stream` argument.
+ *    count (read atomically; the launch plans depend on it) and the locks that
+ *    let calls with one workspace take turns, so calls are thread-safe: several
+ *    threads may call on one stream with one workspace.  Calls on streams that
+ *    run at the same time need workspaces of their own.  Plans are made for the
+ *    device of the `stream` argument.
  *  - Arguments are validated before any HIP call; a rejected call enqueues
  *    nothing.  Only TF_ERR_HIP comes from the runtime (launch failure).
  *  - Outputs must not overlap inputs.

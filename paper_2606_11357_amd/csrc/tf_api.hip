@@ -46,6 +46,13 @@ void log_plan(const char* fmt, ...) {
     std::fprintf(stderr, "[tilefuse] %s\n", line);
 }
 
+std::unique_lock<std::mutex> workspace_turn(const void* ws) {
+    constexpr int kTurns = 61;              // workspaces seldom share one
+    static std::mutex turns[kTurns];
+    if (!ws) return {};
+    return std::unique_lock<std::mutex>(turns[reinterpret_cast<uintptr_t>(ws) / 256 % kTurns]);
+}
+
 }  // namespace tf
 
 namespace {
@@ -100,6 +107,7 @@ int gemm_entry(int bits, const uint16_t* A, const void* packed, uint16_t* C, int
     rc = check_workspace(L, M, ws, ws_bytes);
     if (rc) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const auto turn = tf::workspace_turn(ws);
     if (M < tf::kSkinnyMinM) return tf::launch_gemv(L, A, packed, C, M, ws, s, bf);
     if (M <= tf::kStreamMaxM || tf::stream64_size(L, M))
         return tf::launch_skinny_gemm(L, A, packed, C, M, ws, s, bf);
@@ -114,6 +122,7 @@ int gemv_entry(int bits, const uint16_t* A, const void* packed, uint16_t* C, int
     Layout L = tf::make_layout(bits, K, N, group);
     rc = check_workspace(L, M, ws, ws_bytes);
     if (rc) return rc;
+    const auto turn = tf::workspace_turn(ws);
     return tf::launch_gemv(L, A, packed, C, M, ws, static_cast<hipStream_t>(stream), bf);
 }
 

@@ -145,6 +145,7 @@ int tf_kv4_attention(const tf_kv4_cache* cache, const void* Q, int64_t q_stride,
     if (attention_items(batch, q_len, q_heads, cache->kv_heads) > INT32_MAX / pieces) return TF_ERR_SHAPE;
     if (bad_scale(scale) || (int64_t)workspace_bytes < need) return TF_ERR_ARG;
     if (misaligned(Q) || misaligned(O) || misaligned(workspace) || misaligned(lens, 4)) return TF_ERR_ALIGN;
+    const auto turn = tf::workspace_turn(workspace);
     return tf::launch_kv4_attention(*cache, Q, q_stride, lens, batch, q_len, q_heads, scale, O, workspace,
                                     static_cast<hipStream_t>(stream));
 }
@@ -177,6 +178,7 @@ int tf_prompt_attention(int dtype, const void* Q, int64_t q_stride, const void* 
         misaligned(cu_k, 4) || misaligned(workspace))
         return TF_ERR_ALIGN;
     if (workspace && (int64_t)workspace_bytes < need) return TF_ERR_ARG;
+    const auto turn = tf::workspace_turn(need > 0 ? workspace : nullptr);
     return tf::launch_prompt_attention(dtype == TF_BF16, Q, q_stride, K, k_stride, V, v_stride, cu_q, cu_k, batch,
                                        tokens_q, tokens_k, q_heads, kv_heads, head_dim, scale, causal != 0, O,
                                        need > 0 ? workspace : nullptr, static_cast<hipStream_t>(stream));

@@ -72,6 +72,7 @@ int tf_w8a8_gemm(int dtype, const int8_t* A, const float* a_scales, const void* 
     const tf::W8Layout L = tf::w8_layout(K, N);
     const tf::W8Args a{A, a_scales, static_cast<const uint8_t*>(packed), static_cast<uint16_t*>(C), nullptr, nullptr,
                        M, M, K, N, L.total, L.s_off, (int)L.na, (int)L.np, 0, dtype == TF_BF16, 1, nullptr};
+    const auto turn = tf::workspace_turn(workspace);
     return tf::launch_w8a8(a, workspace, (int64_t)workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
