@@ -104,9 +104,10 @@ int launch_w8a8(W8Args a, void* ws, int64_t ws_bytes, hipStream_t s) {
     a.splits = p.splits;
     a.parts = static_cast<int32_t*>(ws);
     if (log_enabled())
-        log_plan("w8a8 M=%lld K=%lld N=%lld experts=%d: %s, %d rows a tile, K in %d, expected %.1f us", (long long)a.M,
-                 (long long)a.K, (long long)a.N, a.experts, p.kernel < kForms ? "w8a8_tile_kernel" : "w8a8_direct_kernel",
-                 p.kernel < kForms ? kForm[p.kernel].bm : 16, p.splits, p.expected);
+        log_plan("w8a8 M=%lld K=%lld N=%lld experts=%d%s: %s, %d x %d tiles, K in %d, expected %.1f us", (long long)a.M,
+                 (long long)a.K, (long long)a.N, a.experts, a.rows ? " gathered" : "",
+                 p.kernel < kForms ? "w8a8_tile_kernel" : "w8a8_direct_kernel", p.kernel < kForms ? kForm[p.kernel].bm : 16,
+                 p.kernel < kForms ? kForm[p.kernel].bn : 16, p.splits, p.expected);
     return p.kernel < kForms ? launch_w8a8_tile(a, p.kernel, s) : launch_w8a8_direct(a, s);
 }
 
