@@ -416,8 +416,10 @@ int tf_prompt_attention(int dtype, const void* Q, int64_t q_stride, const void* 
  * codes of tf_pack_w8_sym with a scale of its own, and the product is one of
  * integers:
  *   C[m, n] = s_a[m] * s_w[n] * sum_k qa[m, k] * qw[k, n].
- * The sums are exact (int32); each output is rounded once.  `dtype` is TF_F16 or
- * TF_BF16, the type of the 16-bit tensors of a call.
+ * The sums are exact (int32).  An output is the sum as fp32 times the product of its
+ * two scales in fp32, rounded once more to its type (four roundings in all); scales
+ * may be as large or small as fp32 holds, and their product may leave it.  `dtype` is
+ * TF_F16 or TF_BF16, the type of the 16-bit tensors of a call.
  * ---------------------------------------------------------------------------
  */
 

@@ -60,12 +60,30 @@ __device__ __forceinline__ uint2 w8_round(bool bf, const float (&v)[4]) {
     return bf ? uint2{round_out2<true>(v[0], v[1]), round_out2<true>(v[2], v[3])}
               : uint2{round_out2<false>(v[0], v[1]), round_out2<false>(v[2], v[3])};
 }
-// Four sums of one row (columns n .. n + 3) as outputs: the two scales' product, then
-// the sum's, in fp32, one rounding of the result.
+// Outputs from four sums of one row (columns n .. n + 3): the sum as fp32, times the
+// product of its two scales in fp32, rounded once more to the output's type.
+//
+// Scales whose product with another such one, and with any sum, loses nothing to the
+// ends of fp32.
+__device__ __forceinline__ bool w8_near(float s) {
+    return (fabsf(s) >= 0x1p-60f && fabsf(s) <= 0x1p60f) || s == 0.f;
+}
+// For scales that are near.
 __device__ __forceinline__ uint2 w8_scaled(bool bf, const i32x4& sum, float sa, const float4_t& sw) {
     float v[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[r] = (float)sum[r] * (sa * sw[r]);
+    return w8_round(bf, v);
+}
+// For any: products of significands, the exponents last (of near scales the same
+// bits).  there: the row exists; else zeros, by columns that are not finite too.
+__device__ __forceinline__ uint2 w8_scaled_far(bool bf, const i32x4& sum, float sa, const float4_t& sw, bool there) {
+    float v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float p = (float)sum[r] * (__builtin_amdgcn_frexp_mantf(sa) * __builtin_amdgcn_frexp_mantf(sw[r]));
+        v[r] = there ? ldexpf(p, __builtin_amdgcn_frexp_expf(sa) + __builtin_amdgcn_frexp_expf(sw[r])) : 0.f;
+    }
     return w8_round(bf, v);
 }
 #endif

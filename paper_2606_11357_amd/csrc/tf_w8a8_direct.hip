@@ -33,7 +33,16 @@ __device__ __forceinline__ void direct_block(const W8Args& a, const uint8_t* pac
     const __amdgpu_buffer_rsrc_t ar = make_rsrc(a.A + base * a.K, (uint32_t)min(a_bytes, (int64_t)kNowhere));
     int64_t at = -1;
     if (c < rows) at = a.rows ? a.rows[row0 + c] : row0 + c;
-    const uint32_t a_off = at >= 0 && at < a.a_rows ? (uint32_t)((at - base) * a.K) + 16 * g : kNowhere;
+    const bool there = at >= 0 && at < a.a_rows;
+    const uint32_t a_off = there ? (uint32_t)((at - base) * a.K) + 16 * g : kNowhere;
+    // The scales of the outputs, which the first wave stores: their loads go ahead.
+    const int n = kW8Panel * panel + 4 * g;
+    float sa = 0.f;
+    float4_t sw{};
+    if (wave == 0) {
+        if (there) sa = a.a_scale[at];
+        sw = *reinterpret_cast<const float4_t*>(packed + a.s_off + 4 * n);
+    }
     const __amdgpu_buffer_rsrc_t br =
         make_rsrc(packed + (int64_t)panel * a.na * kW8AtomBytes, (uint32_t)a.na * kW8AtomBytes);
 
@@ -62,11 +71,8 @@ __device__ __forceinline__ void direct_block(const W8Args& a, const uint8_t* pac
     i32x4 sum = red[tid];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) sum += red[w * 64 + tid];
-    const int n = kW8Panel * panel + 4 * g;
     if (c >= rows || n >= a.N) return;
-    const float sa = at >= 0 && at < a.a_rows ? a.a_scale[at] : 0.f;
-    const float4_t sw = *reinterpret_cast<const float4_t*>(packed + a.s_off + 4 * n);
-    *reinterpret_cast<uint2*>(a.C + (row0 + c) * a.N + n) = w8_scaled(a.bf, sum, sa, sw);
+    *reinterpret_cast<uint2*>(a.C + (row0 + c) * a.N + n) = w8_scaled_far(a.bf, sum, sa, sw, there);
 }
 
 // Dense: workgroup b has the columns of panel b % 8 + 8 (i / blocks) and the rows of

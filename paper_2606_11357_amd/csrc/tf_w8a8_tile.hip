@@ -16,6 +16,8 @@
 //    are about 8 by 4: each L2 then serves 12 operand tiles to 32.
 //  - Outputs are scaled and stored from the accumulators, past the L2 (one tile of K = 512
 //    16.4 us through it, 14.5 past it), after the next tile's first loads are issued.
+//    Tiles with a scale that is not near take a second form of that (w8_scaled_far in
+//    place of w8_scaled: two operations an output more, 256 of them in the largest tile).
 // The matrix cores and their power bound the large tile: 8192 x 8192 x 8192 384 us (2.87
 // POP/s; torch's library product of int8 524), 8192 x 4096 x 28672 755 to 790 us from
 // card to card (2.45 to 2.55 POP/s at 1.95 GHz, matrix cores 68% busy; of zeros 621 us
@@ -139,6 +141,7 @@ template <class F>
 struct TileShared {
     uint8_t a[F::P * F::kPairBytes];
     float rows[2][F::BM], columns[2][F::BN];          // scales of this tile and the next
+    int far[2][4];                                    // whether some of them are not near, as each wave saw
     int found[4];
 };
 
@@ -264,6 +267,10 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
             for (int t = 0; t < CB; ++t) acc[i][t] = i32x4{0, 0, 0, 0};
         if (tid < F::BM) sm.rows[turn & 1][tid] = row_scale;
         if (tid < F::BN) sm.columns[turn & 1][tid] = column_scale;
+        if constexpr (!SPLIT) {
+            const uint64_t far = __ballot((tid < F::BM && !w8_near(row_scale)) || (tid < F::BN && !w8_near(column_scale)));
+            if (lane == 0) sm.far[turn & 1][wave] = far != 0;
+        }
         lds_wait();
         // (the outputs of the tile before were stored after these loads were issued)
         constexpr int kFirst = (R - 1) * kOps, kNext = kFirst + kStores;
@@ -343,6 +350,12 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
         for (int i = 0; i < RB; ++i) asm volatile("" ::"v"(af[0][i]), "v"(af[F::kAhead ? 1 : 0][i]));
         __builtin_amdgcn_s_waitcnt(0);       // the direct loads past the end have landed
         __syncthreads();                     // and no wave reads the buffers
+        // (read here: after the next loads are issued the compiler would wait for them)
+        bool far = false;
+        if constexpr (!SPLIT) {
+            const int4 seen = *reinterpret_cast<const int4*>(sm.far[turn & 1]);
+            far = __builtin_amdgcn_readfirstlane(seen.x | seen.y | seen.z | seen.w);
+        }
         const Tile done = tile;
         const bool more = next_tile(turn + 1, tile);
         if (more) begin(tile);
@@ -385,19 +398,29 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
             }
             uint32_t row = (uint32_t)c * (uint32_t)a.N * 2u, sixteen = 32u * (uint32_t)a.N;
             int left = done.rows;
-            auto store_all = [&](auto is_bf) {
+            auto store_all = [&](auto is_bf, auto is_far) {
                 constexpr bool bf = decltype(is_bf)::value;
 #pragma unroll
                 for (int i = 0; i < RB; ++i) {
                     __builtin_amdgcn_sched_barrier(0);
                     const float sa = sr[16 * i + c];
                     const bool here = c < left;
+                    bool there = false;
+                    if constexpr (decltype(is_far)::value) {
+                        int64_t at = done.row0 + 16 * i + c;
+                        if (GATHER && here) at = a.rows[at];
+                        there = at >= 0 && at < a.a_rows;
+                    }
+                    auto scaled = [&](int t) {
+                        if constexpr (decltype(is_far)::value) return w8_scaled_far(bf, whole(acc[i][t]), sa, sw[t], there);
+                        else return w8_scaled(bf, whole(acc[i][t]), sa, sw[t]);
+                    };
 #pragma unroll
                     for (int t = 0; t < CB; t += 2) {
                         const uint32_t off = here && to[t / 2] != kNowhere ? row + to[t / 2] : kNowhere;
-                        const uint2 x = w8_scaled(bf, whole(acc[i][t]), sa, sw[t]);
+                        const uint2 x = scaled(t);
                         if constexpr (CB > 1) {
-                            const uint2 y = w8_scaled(bf, whole(acc[i][t + 1]), sa, sw[t + 1]);
+                            const uint2 y = scaled(t + 1);
                             store16(cr, rows_swapped(x, y), off);
                         } else {
                             store8(cr, x, off);
@@ -407,8 +430,13 @@ __device__ __forceinline__ void tile_products(const W8Args& a, Next&& next_tile,
                     left -= 16;
                 }
             };
-            if (a.bf) store_all(std::true_type{});
-            else store_all(std::false_type{});
+            if (__builtin_expect(far, 0)) {
+                if (a.bf) store_all(std::true_type{}, std::true_type{});
+                else store_all(std::false_type{}, std::true_type{});
+            } else {
+                if (a.bf) store_all(std::true_type{}, std::false_type{});
+                else store_all(std::false_type{}, std::false_type{});
+            }
         }
         if (!more) return;
     }
@@ -452,6 +480,9 @@ __global__ __launch_bounds__(256) void w8a8_join_kernel(W8Args a) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= a.M * per_row) return;
     const int64_t m = i / per_row, n = (i - m * per_row) * 8;
+    const float4_t* scales = reinterpret_cast<const float4_t*>(a.packed + a.s_off + n * 4);
+    const float sa = a.a_scale[m];
+    const float4_t sw[2] = {scales[0], scales[1]};
     const i32x4* p = reinterpret_cast<const i32x4*>(a.parts + m * a.N + n);
     i32x4 lo = p[0], hi = p[1];
     for (int s = 1; s < a.splits; ++s) {
@@ -459,9 +490,7 @@ __global__ __launch_bounds__(256) void w8a8_join_kernel(W8Args a) {
         lo += p[0];
         hi += p[1];
     }
-    const float4_t* sw = reinterpret_cast<const float4_t*>(a.packed + a.s_off + n * 4);
-    const float sa = a.a_scale[m];
-    const uint2 x = w8_scaled(a.bf, lo, sa, sw[0]), y = w8_scaled(a.bf, hi, sa, sw[1]);
+    const uint2 x = w8_scaled_far(a.bf, lo, sa, sw[0], true), y = w8_scaled_far(a.bf, hi, sa, sw[1], true);
     *reinterpret_cast<u32x4*>(a.C + m * a.N + n) = u32x4{x.x, x.y, y.x, y.y};
 }
 
