@@ -802,6 +802,14 @@ def _expert_call(name, where, *args):
     return got
 
 
+def _refuse(name, *args):
+    """The library's refusals of a call's sizes, before memory is made for them and for
+    calls without rows: one without pointers, which it refuses last."""
+    status = getattr(load(), name)(*args, None)
+    if status != TF_ERR_NULL:
+        _check(status, name)
+
+
 def quantize_rows(x, gated=False, codes=None, scales=None):
     """Codes (int8 [M, N]) and scales (fp32 [M]) of the rows of a fp16 or bf16 [M, N]
     matrix: scale = max|row| / 127, codes = round(row * 127 / max|row|).  gated: x
@@ -819,6 +827,8 @@ def quantize_rows(x, gated=False, codes=None, scales=None):
     M, N = x.shape[0], x.shape[1] // (2 if gated else 1)
     if x.shape[1] > 1 and x.stride(1) != 1 and not x.is_contiguous():
         raise ValueError("the rows of x must be contiguous")
+    if M == 0:
+        _refuse("tf_quantize_rows", code, None, x.shape[1], 1, N, int(gated), None, None)
     codes = torch.empty((M, N), dtype=torch.int8, device=x.device) if codes is None else codes
     scales = torch.empty((M,), dtype=torch.float32, device=x.device) if scales is None else scales
     _need_cuda(codes, scales)
@@ -964,6 +974,9 @@ def route_experts(logits, top_k: int, *, bias=None, scoring="softmax", groups=1,
     if bias is not None:
         _need_cuda(bias)
         _same(bias, torch.float32, dev, (E,), "bias")
+    if max(map(abs, (top_k, *by))) >= 2 ** 31:           # (more than the library's integers hold)
+        raise TileFuseError(TF_ERR_SHAPE, "tf_route_experts")
+    _refuse("tf_route_experts", code, None, E, None, 1, E, top_k, *by, int(renormalize), scale, *[None] * 5)
     make = lambda n, dt=torch.int32: torch.empty(n, dtype=dt, device=dev)  # noqa: E731
     r = Routing(make((T, top_k), torch.float32), make((T, top_k)), make(E + 1), make(T * top_k), make((T, top_k)))
     if T == 0:
@@ -994,6 +1007,8 @@ def w8a8_expert_gemm(codes, scales, packed, K: int, N: int, offsets, rows=None, 
     if rows is not None:
         slots = rows.numel()
         _int32(rows, (slots,), codes.device, "rows")
+    if slots == 0:
+        _refuse("tf_w8a8_expert_gemm", code, None, None, 1, None, None, None, None, 1, K, N, E)
     out = _product_out(out, dtype, codes.device, (slots, N))
     if slots > 0 and codes.shape[0] == 0:        # no row exists: one that none asks for, for the call's checks
         codes = torch.zeros((1, K), dtype=torch.int8, device=out.device)
@@ -1022,6 +1037,8 @@ def combine_experts(y, weights, places, add=None, out=None):
     _same(weights, torch.float32, dev, (T, k), "weights")
     if add is not None:
         _same(add, y.dtype, dev, (T, N), "add")
+    if T == 0:
+        _refuse("tf_combine_experts", code, None, 1, None, None, None, 1, k, N, None)
     out = _product_out(out, y.dtype, dev, (T, N))
     if T > 0 and y.shape[0] == 0:                # no row exists: one that none asks for, for the call's checks
         y, places = torch.zeros((1, N), dtype=y.dtype, device=dev), torch.full_like(places, -1)
