@@ -78,12 +78,15 @@ class Layer:
     [experts, N], and "router" int8 [hidden, experts] with its scales."""
 
     def __init__(self, cfg: Config, weights: dict):
+        from torch.nn.functional import pad
         self.cfg = cfg
         self.eight_bit = {n for n in cfg.linears() if len(weights[n]) == 2}
         if cfg.experts:
             if not {"gate_up", "down"} <= self.eight_bit:
                 raise ValueError("experts' weights are int8 with a scale a column")
-            self.router = tf.pack_w8a8(*weights["router"])
+            # (columns of zeros up to a whole eight, as the product takes them)
+            self.router_columns = -(-cfg.experts // 8) * 8
+            self.router = tf.pack_w8a8(*(pad(t, (0, self.router_columns - cfg.experts)) for t in weights["router"]))
         self.packed = {n: tf.pack_w8a8(*weights[n]) if n in self.eight_bit else tf.pack_w4(*weights[n], K, N, cfg.group)
                        for n, (K, N) in cfg.linears().items()}
         self.norm_in, self.norm_mlp = weights["norm_in"], weights["norm_mlp"]
@@ -102,8 +105,8 @@ class Layer:
         if not c.experts:
             return self._linear("down", self._linear("gate_up", n), gated=True)
         codes, scales = tf.quantize_rows(n)
-        logits = tf.w8a8_gemm(codes, scales, self.router, c.hidden, c.experts, dtype=n.dtype)
-        route = tf.route_experts(logits, c.top_k, renormalize=True)
+        logits = tf.w8a8_gemm(codes, scales, self.router, c.hidden, self.router_columns, dtype=n.dtype)
+        route = tf.route_experts(logits[:, :c.experts], c.top_k, renormalize=True)
         g = tf.w8a8_expert_gemm(codes, scales, self.packed["gate_up"], *c.linears()["gate_up"], route.offsets,
                                 route.tokens, dtype=n.dtype)
         y = tf.w8a8_expert_gemm(*tf.quantize_rows(g, gated=True), self.packed["down"], *c.linears()["down"],
@@ -196,7 +199,7 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=16, help="decode steps")
     ap.add_argument("--dtype", choices=("f16", "bf16"), default="bf16")
     ap.add_argument("--eight-bit", action="store_true", help="8-bit weights and activations in the linear layers")
-    ap.add_argument("--experts", type=int, default=0, help="experts of an MLP (a multiple of 8; 0: a dense MLP)")
+    ap.add_argument("--experts", type=int, default=0, help="experts of an MLP (0: a dense MLP)")
     ap.add_argument("--top-k", type=int, default=2, help="experts of a token")
     a = ap.parse_args(argv)
     cfg, page = Config(experts=a.experts, top_k=a.top_k), 64
