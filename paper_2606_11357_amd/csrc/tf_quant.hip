@@ -1,11 +1,12 @@
 // Rows of 16-bit activations as int8 codes with one fp32 scale a row, and the
 // rearrangement of int8 weights for the matmuls that take those codes.
 //   h = x or silu(g) u,   s = max|h| / 127,   q = round(h * (127 / max|h|))
-// HBM-bound: x is read once (2 or 4 bytes a code), codes are written once; the row
-// stays in registers between its maximum and its codes.  8192 rows of 4096 take 16.7 us
-// (6.0 TB/s), 8192 of 14336 gated 121 us (4.9 TB/s), one of 4096 2.9 us, the latency
-// of its loads and one reduction; 16 gated rows 5.9 us, one compute unit's exponentials
-// each.
+// x is read once (2 or 4 bytes a code), codes are written once; the row stays in
+// registers between its maximum and its codes.  Many rows are bound by memory, with the
+// vector unit 74% busy: 8192 rows of 4096 take 20.8 us (4.8 TB/s, inputs and outputs of
+// ten calls in turn; 16.7 where one input lies in the MALL), 8192 of 14336 gated 122 us (4.8
+// TB/s).  One row of 4096 takes 2.3 us, the latency of its loads and one reduction; 16
+// gated ones of 14336 5.9 us, one compute unit's exponentials each.
 #include "tf_w8a8.h"
 
 namespace tf {

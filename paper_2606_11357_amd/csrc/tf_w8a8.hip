@@ -21,6 +21,8 @@ namespace {
 // A tile's step of 64 of K takes what its operands take through a compute unit's L1, some
 // 25 bytes a cycle (misses in the L2 bound it, not the number of loads on their way:
 // twice the depth changes nothing); 256 x 256 is the one that the matrix cores bound.
+// Its step is that of few tiles: with all compute units at work the power's limit on the
+// clock makes it a third longer (171 us of 129 above), which the rule leaves out.
 constexpr int kForms = 5;
 struct FormCost {
     int bm, bn, wgs;

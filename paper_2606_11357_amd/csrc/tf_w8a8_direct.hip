@@ -7,8 +7,9 @@
 // straight into registers, a ring of eight atoms ahead, and the waves' sums are added
 // in LDS.  Memory-bound: weights are read once for 16 rows, and every workgroup reads
 // all of its rows.  16 columns and four waves a workgroup: N = 4096 is then one a compute
-// unit.  One row, 4096 x 4096: 6.0 us (of which 3.3 are the memory's; 32 columns 6.6, eight
-// waves 6.0), 14336 x 4096: 13.6 us (4.3 TB/s; 32 columns 16.8); 16 rows 6.4 and 17.3 us.
+// unit.  One row, 4096 x 4096: 5.8 us (of which 3.3 are the memory's; with the outputs' scales
+// loaded at the end 6.0, then 32 columns 6.6 and eight waves 6.0), 14336 x 4096: 13.6 us
+// (4.3 TB/s; 32 columns 16.8); 16 rows 6.4 and 17.5 us.
 #include "tf_w8a8.h"
 
 namespace tf {

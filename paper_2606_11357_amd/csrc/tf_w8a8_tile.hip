@@ -19,8 +19,8 @@
 //    Tiles with a scale that is not near take a second form of that (w8_scaled_far in
 //    place of w8_scaled: two operations an output more, 256 of them in the largest tile).
 // The matrix cores and their power bound the large tile: 8192 x 8192 x 8192 384 us (2.87
-// POP/s; torch's library product of int8 524), 8192 x 4096 x 28672 755 to 790 us from
-// card to card (2.45 to 2.55 POP/s at 1.95 GHz, matrix cores 68% busy; of zeros 621 us
+// POP/s; torch's library product of int8 524), 8192 x 4096 x 28672 737 to 790 us from
+// card to card (2.44 to 2.61 POP/s at 1.95 GHz, matrix cores 68% busy; of zeros 621 us
 // at 2.4).  A step of its 64 takes 0.53 us, 97% of it matrix instructions; a tile's beginning and
 // end some 7 us.  The smaller forms' steps take what their operands take through L1.
 #include <algorithm>
