@@ -493,9 +493,10 @@ int tf_route_experts(int dtype, const void* logits, int64_t stride, const float*
  * The experts' products: row i of C [slots, N], offsets[e] <= i < offsets[e + 1], is
  * row rows[i] (rows NULL: i) of the codes A [a_rows, K] times weight e of `packed`.
  * offsets int32 [experts + 1] and rows int32 [slots] stay on the device; an offset
- * outside 0..slots counts as the nearer end, one below an earlier one as that.  Rows of C that no expert has are not
- * written; one whose row of A is outside 0..a_rows - 1 is zeros.  With rows, A
- * holds less than 2^32 - 256 bytes.
+ * outside 0..slots counts as the nearer end, one below an earlier one as that.  Rows
+ * of C that no expert has are not written; one whose row of A is outside 0..a_rows - 1
+ * is zeros, whatever the columns' scales are.  With rows, A holds less than 2^32 - 256
+ * bytes.
  */
 int tf_w8a8_expert_gemm(int dtype, const int8_t* A, const float* a_scales, int64_t a_rows, const void* packed,
                         const int32_t* offsets, const int32_t* rows, void* C, int64_t slots, int64_t K, int64_t N,

@@ -38,7 +38,7 @@ EXPORTS = (
     "tf_add_rms_norm", "tf_kv4_cache_bytes", "tf_kv4_append", "tf_kv4_read",
     "tf_kv4_attention_workspace_bytes", "tf_kv4_attention", "tf_prompt_attention_workspace_bytes",
     "tf_prompt_attention", "tf_quantize_rows", "tf_w8a8_packed_bytes", "tf_pack_w8a8", "tf_w8a8_workspace_bytes",
-    "tf_w8a8_gemm",     "tf_route_experts", "tf_w8a8_expert_gemm", "tf_combine_experts",
+    "tf_w8a8_gemm", "tf_route_experts", "tf_w8a8_expert_gemm", "tf_combine_experts",
 )
 
 
